@@ -1,5 +1,6 @@
 """ctypes binding of libspike_proj.so (C ABI in include/spike_proj.h,
-include/dense_proj.h, include/quantize.h and include/head_verify.h).
+include/dense_proj.h, include/quantize.h, include/head_verify.h,
+include/dense_fused.h, include/spike_embed.h and include/head_draft.h).
 
 Argument marshalling only: every step of the projection runs in the HIP
 kernels of the library.  Tensors are torch device tensors; their data
@@ -27,6 +28,12 @@ DENSE_MAX_K, DENSE_MAX_B = 16128, 65535
 DENSE_KERNEL_STAGED, DENSE_KERNEL_REGISTER = 1, 2
 DENSE_TUNE_KERNEL, DENSE_TUNE_WG_PER_CU = 1, 2
 SPIKE_LAYOUT_ROW_MAJOR, SPIKE_LAYOUT_COL_MAJOR = 0, 1
+SPIKE_TYPE_F32, SPIKE_TYPE_BF16, SPIKE_TYPE_F16, SPIKE_TYPE_I8, SPIKE_TYPE_I32, SPIKE_TYPE_I64 = 0, 1, 2, 3, 4, 5
+DENSE_ACT_NONE, DENSE_ACT_RELU, DENSE_ACT_GELU, DENSE_ACT_SILU = 0, 1, 2, 3
+DENSE_FUSED_BACKWARD = 1
+FUSED_MAX_DIM, FUSED_MAX_B = 1 << 20, 1 << 22
+EMBED_MAX_V, EMBED_MAX_D, EMBED_MAX_T = 1 << 28, 65536, 1 << 22
+DRAFT_MAX_S, DRAFT_MAX_G, DRAFT_MAX_V = 4096, 31, 1 << 30
 
 
 def SPIKE_SHAPE(V: int, LG: int, U: int, BLOCK: int, NT: bool = False, I16: bool = False) -> int:
@@ -42,13 +49,16 @@ EXPORTED = (
     "spike_proj_abi_version", "spike_proj_forward_noalloc", "spike_proj_create_reserved",
     "spike_stack_forward_fused", "dense_proj_forward", "dense_proj_plan", "dense_proj_tune",
     "spike_quantize_int8", "spike_check_scale_shape", "head_verify_forward", "head_verify_workspace_bytes",
+    "dense_fused_create", "dense_fused_destroy", "dense_fused_forward", "dense_fused_workspace_bytes",
+    "dense_fused_backward", "spike_embed_forward", "spike_embed_workspace_bytes", "spike_embed_backward",
+    "head_draft_workspace_bytes", "head_draft_verify",
 )
 
 if not os.path.exists(LIB):
     raise ImportError(f"{LIB} is not built; run __graft_entry__.build() (python -m paper_2606_03026_amd.build)")
 
 _lib = ctypes.CDLL(LIB)
-_p, _i32 = ctypes.c_void_p, ctypes.c_int32
+_p, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _sig = {
     "spike_proj_create": [_p, _p, _i32, _i32, ctypes.POINTER(_p)],
     "spike_proj_create_reserved": [_p, _p, _i32, _i32, _i32, _i32, ctypes.POINTER(_p)],
@@ -76,13 +86,25 @@ _sig = {
     "spike_check_scale_shape": [_i32, _i32, _i32, _i32, _i32],
     "head_verify_forward": [_p, _p, _i32, _i32, _p, _i32, ctypes.c_float, _p, _p, _p, _p, _p, _p],
     "head_verify_workspace_bytes": [],
+    "dense_fused_create": [_p, _p, _i32, _i32, _i32, ctypes.POINTER(_p)],
+    "dense_fused_destroy": [_p],
+    "dense_fused_forward": [_p, _p, _i32, _i64, _i32, _p, _i32, _p, _i64, _p, _i32, _i64, _p, _i64, _p],
+    "dense_fused_workspace_bytes": [_p, _i32, _i32],
+    "dense_fused_backward": [_p, _p, _i32, _i64, _p, _i64, _i32, _i32, _p, _i32, _i64, _p, _p, _i64, _p],
+    "spike_embed_forward": [_p, _i32, _p, _i32, _i32, _i64, _p, _i32, _i32, _f32, _p, _i32, _i64, _p],
+    "spike_embed_workspace_bytes": [_i32, _i32],
+    "spike_embed_backward": [_p, _i32, _i64, _p, _i32, _i32, _i32, _i32, _f32, _i32, _p, _i32, _i64, _p, _i64, _p],
+    "head_draft_workspace_bytes": [_i32, _i32, _i32],
+    "head_draft_verify": [_p, _i64, _p, _i64, _i32, _p, _p, _p, _p, _i64, _p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _i64, _p],
 }
 for _name, _args in _sig.items():
     getattr(_lib, _name).argtypes = _args
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.spike_proj_last_error.argtypes = []
 _lib.spike_proj_last_error.restype = ctypes.c_char_p
-_lib.head_verify_workspace_bytes.restype = ctypes.c_int64
+for _name in ("head_verify_workspace_bytes", "dense_fused_workspace_bytes", "spike_embed_workspace_bytes",
+              "head_draft_workspace_bytes"):
+    getattr(_lib, _name).restype = ctypes.c_int64
 
 
 class SpikeError(RuntimeError):
@@ -110,6 +132,49 @@ def _dev_ptr(t: torch.Tensor, name: str, nbytes: int | None = None) -> int:
     if nbytes is not None and t.numel() * t.element_size() < nbytes:
         raise ValueError(f"{name} holds {t.numel() * t.element_size()} bytes, needs {nbytes}")
     return t.data_ptr()
+
+
+_FLOAT_TYPES = {torch.float32: SPIKE_TYPE_F32, torch.bfloat16: SPIKE_TYPE_BF16, torch.float16: SPIKE_TYPE_F16}
+_ID_TYPES = {torch.int32: SPIKE_TYPE_I32, torch.int64: SPIKE_TYPE_I64}
+
+
+def _type_of(t: torch.Tensor, name: str) -> int:
+    code = _FLOAT_TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16")
+    return code
+
+
+def _rows(t: torch.Tensor, name: str, rows: int, cols: int):
+    """(address, elements between rows) of a device tensor [rows, cols] whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be [{rows}, {cols}], is {list(t.shape)}")
+    step, one = t.stride()
+    if (one != 1 and cols > 1) or (step < cols and rows > 1):
+        raise ValueError(f"{name} must have contiguous rows")
+    return t.data_ptr(), max(step, cols)
+
+
+def _vector(t: torch.Tensor | None, name: str, n: int, dtype=torch.float32):
+    """Address of a contiguous device tensor of n elements; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise TypeError(f"{name} must be {dtype} with {n} entries")
+    return _dev_ptr(t, name)
+
+
+def _workspace(given: torch.Tensor | None, nbytes: int, device, stream) -> torch.Tensor:
+    """`given`, or fresh memory that belongs to the stream of the call."""
+    if given is not None:
+        return given
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    st = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+    with torch.cuda.stream(st):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def words_per_row(K: int) -> int:
@@ -406,6 +471,185 @@ def head_verify_forward(Q: torch.Tensor, scale: torch.Tensor, x: torch.Tensor, t
                                     _dev_ptr(cand, "cand", k * 4), _dev_ptr(cand_logits, "cand_logits", k * 4),
                                     _dev_ptr(result, "result", 8), _dev_ptr(workspace, "workspace", n_ws),
                                     _stream(stream)), "head_verify_forward")
+
+
+class DenseFused:
+    """Handle returned by dense_fused_create: the weights laid out for the matrix cores."""
+
+    def __init__(self, ptr: int, K: int, M: int):
+        self.ptr, self.K, self.M = ptr, K, M
+
+    def close(self):
+        if self.ptr:
+            _check(_lib.dense_fused_destroy(self.ptr), "dense_fused_destroy")
+            self.ptr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def dense_fused_create(Q: torch.Tensor, scale: torch.Tensor, backward: bool = False) -> DenseFused:
+    """Q: int8 [M, K] row-major, scale: float32 [M] (dense_fused.h); both may be freed afterwards.
+    backward: also lay the weights out for dense_fused_backward's dx."""
+    if Q.dtype != torch.int8 or Q.dim() != 2:
+        raise TypeError("Q must be a 2-D int8 tensor [M][K]")
+    M, K = Q.shape
+    if scale.dtype != torch.float32 or scale.numel() != M:
+        raise TypeError("scale must be float32 with M entries")
+    out = _p()
+    _check(_lib.dense_fused_create(_dev_ptr(Q, "Q"), _dev_ptr(scale, "scale"), int(K), int(M),
+                                   DENSE_FUSED_BACKWARD if backward else 0, ctypes.byref(out)), "dense_fused_create")
+    return DenseFused(out.value, int(K), int(M))
+
+
+def dense_fused_destroy(h: DenseFused) -> None:
+    h.close()
+
+
+def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None,
+                        act: int = DENSE_ACT_NONE, residual: torch.Tensor | None = None,
+                        pre: torch.Tensor | None = None, stream=None) -> None:
+    """y = act(z) + residual, z = scale * (x @ float(Q).T) + bias (dense_fused.h); z also to `pre`.
+    x: [B, K]; y, residual, pre: [B, M] of one type; rows may be strided."""
+    B = x.shape[0]
+    xp, ldx = _rows(x, "x", B, h.K)
+    yp, ldy = _rows(y, "y", B, h.M)
+    rp = pp = None
+    ldr = ldp = 0
+    if residual is not None:
+        rp, ldr = _rows(residual, "residual", B, h.M)
+    if pre is not None:
+        pp, ldp = _rows(pre, "pre", B, h.M)
+    if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
+        raise TypeError("residual and pre must have y's type")
+    _check(_lib.dense_fused_forward(h.ptr, xp, _type_of(x, "x"), ldx, B, _vector(bias, "bias", h.M), act, rp, ldr, yp,
+                                    _type_of(y, "y"), ldy, pp, ldp, _stream(stream)), "dense_fused_forward")
+
+
+def dense_fused_workspace_bytes(h: DenseFused, B: int, dtype: torch.dtype) -> int:
+    """Workspace of dense_fused_backward for B rows of dy of `dtype`."""
+    n = int(_lib.dense_fused_workspace_bytes(h.ptr, int(B), _FLOAT_TYPES.get(dtype, -1)))
+    if n < 0:
+        raise ValueError(f"no workspace for B = {B}, {dtype}")
+    return n
+
+
+def dense_fused_backward(h: DenseFused, dy: torch.Tensor, dx: torch.Tensor | None = None,
+                         dbias: torch.Tensor | None = None, pre: torch.Tensor | None = None,
+                         act: int = DENSE_ACT_NONE, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Gradients of dense_fused_forward with respect to x ([B, K]) and bias (float32 [M]); dy and pre
+    are [B, M] of y's type."""
+    B = dy.shape[0]
+    gp, ldg = _rows(dy, "dy", B, h.M)
+    pp = xp = None
+    ldp = ldx = 0
+    y_type = x_type = _type_of(dy, "dy")
+    if pre is not None:
+        pp, ldp = _rows(pre, "pre", B, h.M)
+        if pre.dtype != dy.dtype:
+            raise TypeError("pre must have dy's type")
+    if dx is not None:
+        xp, ldx = _rows(dx, "dx", B, h.K)
+        x_type = _type_of(dx, "dx")
+    ws = _workspace(workspace, int(_lib.dense_fused_workspace_bytes(h.ptr, B, y_type)), dy.device, stream)
+    _check(_lib.dense_fused_backward(h.ptr, gp, y_type, ldg, pp, ldp, act, B, xp, x_type, ldx,
+                                     _vector(dbias, "dbias", h.M), _dev_ptr(ws, "workspace"),
+                                     ws.numel() * ws.element_size(), _stream(stream)), "dense_fused_backward")
+
+
+def spike_embed_forward(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+                        row_scale: torch.Tensor | None = None, stream=None) -> None:
+    """out[t] = scale * table[ids[t]] (spike_embed.h), zeros for an id outside the table.  table: [V, D]
+    float32, bfloat16, float16, or int8 with row_scale float32 [V]; ids: int32 or int64 [T]; out: [T, D]."""
+    V, D = table.shape
+    T = ids.numel()
+    tp, ldt = _rows(table, "table", V, D)
+    op, ldo = _rows(out, "out", T, D)
+    id_type = _ID_TYPES.get(ids.dtype)
+    if id_type is None:
+        raise TypeError("ids must be int32 or int64")
+    t_type = SPIKE_TYPE_I8 if table.dtype == torch.int8 else _type_of(table, "table")
+    _check(_lib.spike_embed_forward(tp, t_type, _vector(row_scale, "row_scale", V), V, D, ldt, _dev_ptr(ids, "ids"),
+                                    id_type, T, scale, op, _type_of(out, "out"), ldo, _stream(stream)),
+           "spike_embed_forward")
+
+
+def spike_embed_workspace_bytes(T: int, D: int) -> int:
+    """Workspace of spike_embed_backward for T tokens and rows of D elements."""
+    n = int(_lib.spike_embed_workspace_bytes(int(T), int(D)))
+    if n < 0:
+        raise ValueError(f"no workspace for T = {T}, D = {D}")
+    return n
+
+
+def spike_embed_backward(grad: torch.Tensor, ids: torch.Tensor, dtable: torch.Tensor, scale: float = 1.0,
+                         accumulate: bool = False, workspace: torch.Tensor | None = None, stream=None) -> None:
+    """dtable[v] (+)= scale * sum of grad[t] over ids[t] = v (spike_embed.h).  grad: [T, D]; dtable: [V, D]."""
+    V, D = dtable.shape
+    T = ids.numel()
+    gp, ldg = _rows(grad, "grad", T, D)
+    dp, ldd = _rows(dtable, "dtable", V, D)
+    id_type = _ID_TYPES.get(ids.dtype)
+    if id_type is None:
+        raise TypeError("ids must be int32 or int64")
+    ws = _workspace(workspace, spike_embed_workspace_bytes(T, D), dtable.device, stream)
+    _check(_lib.spike_embed_backward(gp, _type_of(grad, "grad"), ldg, _dev_ptr(ids, "ids"), id_type, T, V, D, scale,
+                                     1 if accumulate else 0, dp, _type_of(dtable, "dtable"), ldd,
+                                     _dev_ptr(ws, "workspace"), ws.numel() * ws.element_size(), _stream(stream)),
+           "spike_embed_backward")
+
+
+def head_draft_workspace_bytes(S: int, G: int, V: int) -> int:
+    """Workspace of head_draft_verify for S sequences of up to G drafts over V tokens."""
+    n = int(_lib.head_draft_workspace_bytes(int(S), int(G), int(V)))
+    if n < 0:
+        raise ValueError(f"no workspace for S = {S}, G = {G}, V = {V}")
+    return n
+
+
+def _logit_rows(t: torch.Tensor, name: str, S: int, n: int, V: int):
+    """(address, elements between rows) of logits [S, n, V] with evenly spaced rows."""
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if tuple(t.shape) != (S, n, V):
+        raise ValueError(f"{name} must be [{S}, {n}, {V}], is {list(t.shape)}")
+    seq, row, one = t.stride()
+    ld = row if n > 1 else seq if S > 1 else V
+    if (one != 1 and V > 1) or ld < V or (S > 1 and n > 0 and seq != n * ld):
+        raise ValueError(f"{name} must have contiguous, evenly spaced rows")
+    return t.data_ptr(), ld
+
+
+def head_draft_verify(target: torch.Tensor, draft: torch.Tensor | None, drafts: torch.Tensor, uniform: torch.Tensor,
+                      noise: torch.Tensor, tokens: torch.Tensor, n_accepted: torch.Tensor,
+                      accept: torch.Tensor | None = None, prob: torch.Tensor | None = None,
+                      n_draft: torch.Tensor | None = None, temperature: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None, stream=None) -> None:
+    """Check drafted tokens against the target's logits and draw the next token (head_draft.h).  target:
+    [S, G + 1, V]; draft: [S, G, V] of the same type, or None for a drafter without probabilities; drafts:
+    int32 [S, G]; uniform: float32 [S, G]; noise: float32 [S, V]; tokens: int32 [S, G + 1]; n_accepted: int32 [S]."""
+    S, G1, V = target.shape
+    G = G1 - 1
+    tp, ldt = _logit_rows(target, "target", S, G1, V)
+    dp, ldd = None, 0
+    if draft is not None and G > 0:
+        dp, ldd = _logit_rows(draft, "draft", S, G, V)
+        if draft.dtype != target.dtype:
+            raise TypeError("draft must have target's type")
+    np_, ldn = _rows(noise, "noise", S, V)
+    if noise.dtype != torch.float32:
+        raise TypeError("noise must be float32")
+    i32 = torch.int32
+    ws = _workspace(workspace, head_draft_workspace_bytes(S, G, V), target.device, stream)
+    _check(_lib.head_draft_verify(tp, ldt, dp, ldd, _type_of(target, "target"), _vector(drafts, "drafts", S * G, i32),
+                                  _vector(n_draft, "n_draft", S, i32), _vector(uniform, "uniform", S * G), np_, ldn,
+                                  _vector(temperature, "temperature", S), S, G, V, _vector(tokens, "tokens", S * G1, i32),
+                                  _vector(n_accepted, "n_accepted", S, i32), _vector(accept, "accept", S * G),
+                                  _vector(prob, "prob", S * G1), _dev_ptr(ws, "workspace"),
+                                  ws.numel() * ws.element_size(), _stream(stream)), "head_draft_verify")
 
 
 def spike_proj_abi_version() -> int:

@@ -1,0 +1,294 @@
+// Embedding lookup and the gradient of its table (C ABI in
+// include/spike_embed.h).
+//
+// Lookup: one wave per token, its lanes along the row; bound by memory (the
+// distinct rows read once, T rows written).
+//
+// Gradient, by sorted tokens: the ids are sorted with their positions (equal
+// ids in ascending position), the sorted list is cut into runs of a fixed
+// length, and a wave adds up a run's rows for a block of columns, writing a
+// row whenever the id changes.  A row whose tokens lie in one run is written
+// at once; the others leave one partial sum per run, joined afterwards in
+// ascending order.  No atomics: the order of every sum is fixed by the ids.
+#pragma once
+
+#include "types.hpp"
+
+namespace spk {
+
+constexpr int kEmbedBlock = 256;
+constexpr uint32_t kNoToken = 0xffffffffu;  // key of a token outside the table: sorts last
+
+template <typename ID>
+__device__ inline uint32_t token_key(const ID* ids, int64_t t, int V)
+{
+    const ID id = ids[t];
+    return id >= 0 && id < (ID)V ? (uint32_t)id : kNoToken;
+}
+
+// VEC: 8 where every row starts on a 16-byte (I8: 8-byte) boundary and holds
+// whole vectors, else 1.
+template <typename TI, typename TO, int VEC, typename ID>
+__global__ __launch_bounds__(kEmbedBlock) void k_embed(const TI* __restrict__ table, const float* __restrict__ row_scale,
+                                                       int V, int D, int64_t ld_table, const ID* __restrict__ ids,
+                                                       int T, float scale, TO* __restrict__ out, int64_t ld_out)
+{
+    const int t = blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64;
+    if (t >= T)
+        return;
+    const uint32_t id = __builtin_amdgcn_readfirstlane(token_key(ids, t, V));
+    const bool live = id != kNoToken;
+    const TI* row = table + (live ? id : 0) * ld_table;
+    const float rs = sizeof(TI) == 1 && live ? row_scale[id] : 1.0f;
+    TO* to = out + (int64_t)t * ld_out;
+    const int lane = threadIdx.x % 64;
+    for (int d = lane * VEC; d < D; d += 64 * VEC) {
+        if constexpr (VEC == 8) {
+            f32x8 v = {};
+            if (live) {
+                v = load8(row + d);
+                if (sizeof(TI) == 1)
+                    v *= rs;
+                v *= scale;
+            }
+            store8(to + d, v);
+        } else {
+            float v = 0.0f;
+            if (live) {
+                v = (float)row[d];
+                if (sizeof(TI) == 1)
+                    v *= rs;
+                v *= scale;
+            }
+            to[d] = (TO)v;
+        }
+    }
+}
+
+// --- sorting ---------------------------------------------------------------
+
+constexpr int kSortChunk = 2048;   // tokens sorted among themselves by counting
+constexpr int kSortParts = 8;      // lanes that share one token's count
+constexpr int kSortTokens = kEmbedBlock / kSortParts;
+constexpr int kSortPartKeys = kSortChunk / kSortParts;
+constexpr int kSortPartStride = kSortPartKeys + 4;  // the parts' reads fall into different LDS banks
+
+// Sorts each chunk of kSortChunk tokens by (key, position): a token's place
+// is the number of tokens of its chunk that come before it.  2,048
+// comparisons a token, shared by 8 lanes.
+template <typename ID>
+__global__ __launch_bounds__(kEmbedBlock) void k_embed_sort(const ID* __restrict__ ids, int T, int V,
+                                                            uint32_t* __restrict__ keys, int* __restrict__ order)
+{
+    __shared__ uint32_t s[kSortParts * kSortPartStride];
+    const int t0 = blockIdx.x * kSortTokens;
+    const int c0 = t0 / kSortChunk * kSortChunk;
+    const int n = min(kSortChunk, T - c0);
+    for (int i = threadIdx.x; i < kSortChunk; i += kEmbedBlock)
+        s[i / kSortPartKeys * kSortPartStride + i % kSortPartKeys] = i < n ? token_key(ids, c0 + i, V) : kNoToken;
+    __syncthreads();
+    const int part = threadIdx.x % kSortParts;
+    const int i = t0 - c0 + threadIdx.x / kSortParts;  // this token's place in the chunk
+    const uint32_t key = s[i / kSortPartKeys * kSortPartStride + i % kSortPartKeys];
+    const uint32_t* p = s + part * kSortPartStride;
+    const int j0 = part * kSortPartKeys;
+    int before = 0;
+    for (int j = 0; j < kSortPartKeys; j += 4) {
+        const u32x4 k = *reinterpret_cast<const u32x4*>(p + j);
+        for (int e = 0; e < 4; ++e)
+            before += k[e] < key || (k[e] == key && j0 + j + e < i);
+    }
+    for (int m = 1; m < kSortParts; m *= 2)
+        before += __shfl_xor(before, m);
+    if (part == 0 && i < n) {
+        keys[c0 + before] = key;
+        order[c0 + before] = c0 + i;
+    }
+}
+
+// Places every token of the sorted chunks in the whole list: its place in its
+// own chunk, plus what the others hold before it (their equal keys too where
+// they lie earlier), found by bisection.  8 lanes share a token's chunks.
+__global__ __launch_bounds__(kEmbedBlock) void k_embed_merge(const uint32_t* __restrict__ keys,
+                                                             const int* __restrict__ order, int T,
+                                                             uint32_t* __restrict__ out_keys,
+                                                             int* __restrict__ out_order)
+{
+    const int i = blockIdx.x * kSortTokens + threadIdx.x / kSortParts;
+    const int part = threadIdx.x % kSortParts;
+    const bool live = i < T;
+    const uint32_t key = live ? keys[i] : 0;
+    const int own = i / kSortChunk;
+    const int chunks = (T + kSortChunk - 1) / kSortChunk;
+    int place = 0;
+    if (live)
+        for (int c = part; c < chunks; c += kSortParts) {
+            if (c == own) {
+                place += i - own * kSortChunk;
+                continue;
+            }
+            // keys below, or up to, this one
+            const uint32_t* p = keys + (int64_t)c * kSortChunk;
+            int lo = 0, hi = min(kSortChunk, T - c * kSortChunk);
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                const uint32_t k = p[mid];
+                if (k < key || (k == key && c < own))
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            place += lo;
+        }
+    for (int m = 1; m < kSortParts; m *= 2)
+        place += __shfl_xor(place, m);
+    if (live && part == 0) {
+        out_keys[place] = key;
+        out_order[place] = order[i];
+    }
+}
+
+// --- sums ------------------------------------------------------------------
+
+template <typename TG, int VEC>
+__device__ inline void load_cols(const TG* p, float (&v)[VEC])
+{
+    if constexpr (VEC == 8) {
+        const f32x8 x = load8(p);
+        for (int e = 0; e < 8; ++e)
+            v[e] = x[e];
+    } else {
+        for (int e = 0; e < VEC; ++e)
+            v[e] = (float)p[e];
+    }
+}
+
+template <typename TD, int VEC>
+__device__ inline void put_row(TD* p, const float (&v)[VEC], float scale, bool accumulate)
+{
+    if constexpr (VEC == 8) {
+        f32x8 x;
+        for (int e = 0; e < 8; ++e)
+            x[e] = v[e] * scale;
+        if (accumulate)
+            x += load8(p);
+        store8(p, x);
+    } else {
+        for (int e = 0; e < VEC; ++e)
+            p[e] = (TD)(v[e] * scale + (accumulate ? (float)p[e] : 0.0f));
+    }
+}
+
+constexpr int kFillRows = 32;  // rows of the table that a filling workgroup looks at
+
+// Workgroups below sum_wgs: each wave adds up one run (`run` tokens of the
+// sorted list) for 64 VEC columns.  partial[2 r] holds run r's sum of a row that began in an
+// earlier run, partial[2 r + 1] that of a row that begins in run r and goes
+// on.  The other workgroups write zeros to the rows that no token names.
+template <typename TG, typename TD, int VEC>
+__global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict__ grad, int64_t ld_grad,
+                                                           const uint32_t* __restrict__ keys,
+                                                           const int* __restrict__ order, int T, int V, int D, int run,
+                                                           int sum_wgs, float scale, int accumulate,
+                                                           TD* __restrict__ dtable, int64_t ld_table,
+                                                           float* __restrict__ partial)
+{
+    if ((int)blockIdx.x >= sum_wgs) {
+        __shared__ int named[kFillRows];
+        const int v0 = ((int)blockIdx.x - sum_wgs) * kFillRows;
+        if (threadIdx.x < kFillRows) {
+            const uint32_t key = (uint32_t)v0 + threadIdx.x;
+            int lo = 0, hi = T;
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (keys[mid] < key)
+                    lo = mid + 1;
+                else
+                    hi = mid;
+            }
+            named[threadIdx.x] = lo < T && keys[lo] == key;
+        }
+        __syncthreads();
+        const float zero[VEC] = {};
+        for (int r = threadIdx.x / 64; r < kFillRows && r < V - v0; r += kEmbedBlock / 64) {
+            if (named[r])
+                continue;
+            TD* p = dtable + (int64_t)(v0 + r) * ld_table;
+            for (int d = threadIdx.x % 64 * VEC; d < D; d += 64 * VEC)
+                put_row<TD, VEC>(p + d, zero, 0.0f, false);
+        }
+        return;
+    }
+    const int blocks = (D + 64 * VEC - 1) / (64 * VEC);
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
+    const int r = unit / blocks;
+    const int d = (unit % blocks * 64 + threadIdx.x % 64) * VEC;
+    const int i0 = r * run, i1 = min(T, i0 + run);
+    if (i0 >= T)
+        return;
+    float sum[VEC] = {};
+    bool from_before = i0 > 0 && keys[i0 - 1] == keys[i0];
+    constexpr int U = 8;  // rows in flight
+    for (int i = i0; i < i1; i += U) {
+        float g[U][VEC] = {};
+        uint32_t key[U + 1];
+        for (int u = 0; u <= U; ++u)
+            key[u] = i + u < T ? keys[i + u] : kNoToken;
+        if (d < D)
+            for (int u = 0; u < U; ++u)
+                if (i + u < i1 && key[u] != kNoToken)
+                    load_cols<TG, VEC>(grad + (int64_t)order[i + u] * ld_grad + d, g[u]);
+        for (int u = 0; u < U; ++u) {
+            if (i + u >= i1 || key[u] == kNoToken)
+                continue;
+            for (int e = 0; e < VEC; ++e)
+                sum[e] += g[u][e];
+            const bool ends = i + u + 1 >= T || key[u + 1] != key[u];
+            if (!ends && i + u + 1 < i1)
+                continue;
+            if (d < D) {
+                if (ends && !from_before)
+                    put_row<TD, VEC>(dtable + (int64_t)key[u] * ld_table + d, sum, scale, accumulate);
+                else
+                    put_row<float, VEC>(partial + (int64_t)(2 * r + (from_before ? 0 : 1)) * D + d, sum, 1.0f, false);
+            }
+            for (int e = 0; e < VEC; ++e)
+                sum[e] = 0.0f;
+            from_before = false;
+        }
+    }
+}
+
+// Joins the partial sums of the rows that several runs share: the wave of the
+// run in which such a row begins adds the following runs' sums to its own.
+template <typename TD, int VEC>
+__global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __restrict__ keys, int T, int D, int run,
+                                                            float scale, int accumulate, TD* __restrict__ dtable,
+                                                            int64_t ld_table, const float* __restrict__ partial)
+{
+    const int blocks = (D + 64 * VEC - 1) / (64 * VEC);
+    const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
+    const int r = unit / blocks;
+    const int d = (unit % blocks * 64 + threadIdx.x % 64) * VEC;
+    const int64_t i0 = (int64_t)r * run, i1 = i0 + run;
+    if (i1 >= T)
+        return;
+    const uint32_t key = keys[i1 - 1];
+    if (key == kNoToken || keys[i1] != key)
+        return;  // no row goes on
+    if (i0 > 0 && keys[i0 - 1] == key)
+        return;  // it began earlier
+    if (d >= D)
+        return;
+    float sum[VEC];
+    load_cols<float, VEC>(partial + (int64_t)(2 * r + 1) * D + d, sum);
+    for (int64_t i = i1, q = r + 1; i < T && keys[i] == key; i += run, ++q) {
+        float p[VEC];
+        load_cols<float, VEC>(partial + (2 * q) * D + d, p);
+        for (int e = 0; e < VEC; ++e)
+            sum[e] += p[e];
+    }
+    put_row<TD, VEC>(dtable + (int64_t)key * ld_table + d, sum, scale, accumulate);
+}
+
+}  // namespace spk
