@@ -245,7 +245,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return fail(SPIKE_EINVAL, "neither dx nor dbias is asked for");
     if (dx && !h->Pt)
         return fail(SPIKE_EINVAL, "the handle was created without DENSE_FUSED_BACKWARD");
-    if (ld_dy < h->M || (act != DENSE_ACT_NONE && ld_pre < h->M) || (dx && ld_dx < h->K))
+    if (ld_dy < h->M || (act != DENSE_ACT_NONE && pre && ld_pre < h->M) || (dx && ld_dx < h->K))
         return fail(SPIKE_EINVAL, "a row stride is below K = %d or M = %d", h->K, h->M);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     if (B > 0) {

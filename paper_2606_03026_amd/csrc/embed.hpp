@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed(const TI* __restrict__ ta
                     v *= rs;
                 v *= scale;
             }
-            to[d] = (TO)v;
+            to[d] = (TO)in_fp32<TO>(v);
         }
     }
 }
@@ -175,7 +175,7 @@ __device__ inline void put_row(TD* p, const float (&v)[VEC], float scale, bool a
         store8(p, x);
     } else {
         for (int e = 0; e < VEC; ++e)
-            p[e] = (TD)(v[e] * scale + (accumulate ? (float)p[e] : 0.0f));
+            p[e] = (TD)in_fp32<TD>(v[e] * scale + (accumulate ? (float)p[e] : 0.0f));
     }
 }
 

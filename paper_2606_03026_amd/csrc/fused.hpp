@@ -233,6 +233,8 @@ __device__ inline f32x4 read4(const T* p, bool vec, int n)
 template <typename T>
 __device__ inline void write4(T* p, f32x4 v, bool vec, int n)
 {
+    for (int e = 0; e < 4; ++e)
+        v[e] = in_fp32<T>(v[e]);
     if (vec) {
         typedef T t4 __attribute__((ext_vector_type(4)));
         *reinterpret_cast<t4*>(p) = __builtin_convertvector(v, t4);

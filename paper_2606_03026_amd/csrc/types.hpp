@@ -31,9 +31,22 @@ __device__ inline f32x8 load8(const T* p)
     return __builtin_convertvector(v, f32x8);
 }
 
+// v as a value of its own: without this the compiler may fold the FP32
+// product before it and the rounding to F16 into one mixed-precision
+// instruction, in some kernels and not in others.
+template <typename T>
+__device__ inline float in_fp32(float v)
+{
+    if constexpr (__is_same(T, f16))
+        asm("" : "+v"(v));
+    return v;
+}
+
 template <typename T>
 __device__ inline void store8(T* p, f32x8 v)
 {
+    for (int e = 0; e < 8; ++e)
+        v[e] = in_fp32<T>(v[e]);
     *reinterpret_cast<typename Vec8<T>::type*>(p) = __builtin_convertvector(v, typename Vec8<T>::type);
 }
 

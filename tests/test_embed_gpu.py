@@ -1,0 +1,224 @@
+"""GPU parity of the embedding lookup and its table's gradient (spike_embed.h).
+
+The lookup is one or two FP32 products and one rounding: bit for bit.  A
+gradient row is an FP32 sum of n gradients (any order: within n u sum |g|,
+u = 2^-24), one product and one rounding; with integer gradients and a
+power-of-two scale it is exact.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import step_oracle as so
+from tests.launches import kernels
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "i8": torch.int8}
+HALF_UNIT = {k: torch.finfo(TYPES[k]).eps / 2 for k in ("f32", "bf16", "f16")}
+
+
+@pytest.fixture(scope="module")
+def sp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2606_03026_amd import _binding
+    return _binding
+
+
+def rows(a, kind, pad=0, offset=0):
+    a = torch.as_tensor(np.ascontiguousarray(a)).to(TYPES[kind])
+    n = a.shape[1]
+    buf = torch.zeros(a.shape[0] * (n + pad) + offset, dtype=TYPES[kind], device="cuda")
+    view = buf[offset:].view(a.shape[0], n + pad)[:, :n]
+    view.copy_(a)
+    return view
+
+
+def tokens(r, T, V, hot=0.3):
+    """Ids of which some come often, some are padding: -1, V, and far outside."""
+    ids = r.integers(0, V, T)
+    ids = np.where(r.random(T) < hot, r.integers(0, max(1, V // 50), T), ids)
+    return np.where(r.random(T) < 0.05, r.choice([-1, V, -2 ** 31, 2 ** 31 - 1], T), ids)
+
+
+@pytest.mark.parametrize("V,D,T", [(1, 1, 1), (5, 3, 9), (100, 64, 33), (300, 1536, 70), (57, 129, 200), (40, 80, 1), (9, 4096, 12)])
+@pytest.mark.parametrize("table,out", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("i8", "f32"), ("i8", "bf16"), ("f32", "f16")])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (3, 1)])
+def test_lookup(sp, V, D, T, table, out, pad, offset):
+    r = np.random.default_rng([21, V, D, T])
+    ids = tokens(r, T, V)
+    scale, row_scale = np.float32(1.7), r.uniform(0.01, 0.1, V).astype(np.float32)
+    w = r.integers(-128, 128, (V, D)) if table == "i8" else r.normal(size=(V, D))
+    tab = rows(w, table, pad, offset)
+    got = rows(np.full((T, D), 9.0), out, pad, offset)
+    rs = torch.from_numpy(row_scale).cuda() if table == "i8" else None
+    for dtype in (torch.int32, torch.int64):
+        got.fill_(9.0)
+        sp.spike_embed_forward(tab, torch.from_numpy(ids).to(dtype).cuda(), got, scale=float(scale), row_scale=rs)
+        torch.cuda.synchronize()
+        t = tab.float().cpu().numpy()
+        ok = (ids >= 0) & (ids < V)
+        want = np.zeros((T, D), np.float32)
+        want[ok] = t[ids[ok]]
+        if table == "i8":
+            want[ok] = want[ok] * row_scale[ids[ok]][:, None]
+        want = want * scale
+        assert torch.equal(got.cpu(), torch.from_numpy(want).to(TYPES[out]))
+
+
+GRADS = [(1, 1, 1), (5, 3, 9), (100, 64, 33), (64, 1536, 300), (57, 129, 2048), (700, 72, 2049), (33, 40, 5000), (3, 17, 4097),
+         (2, 8, 9000), (1000, 256, 20001)]
+
+
+@pytest.mark.parametrize("V,D,T", GRADS)
+@pytest.mark.parametrize("grad,table", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f16", "f32"), ("f32", "f16")])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_integers_is_exact(sp, V, D, T, grad, table, accumulate):
+    """Sums of small integers are exact: every row, padding, runs cut anywhere."""
+    r = np.random.default_rng([22, V, D, T])
+    ids = tokens(r, T, V)
+    # the narrow tables hold the sums exactly only while these are small
+    g = r.integers(-2, 3, (T, D)).astype(np.float32) if table == "f32" else (r.random((T, D)) < 0.01).astype(np.float32)
+    start = r.integers(-5, 6, (V, D)).astype(np.float32)
+    dt = rows(start, table)
+    sp.spike_embed_backward(rows(g, grad), torch.from_numpy(ids).cuda(), dt, scale=0.5, accumulate=accumulate)
+    torch.cuda.synchronize()
+    want = so.embed_backward(g, ids, V, 0.5, start if accumulate else None)
+    assert torch.equal(dt.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[table]))
+
+
+@pytest.mark.parametrize("V,D,T", [(100, 64, 33), (57, 129, 2048), (700, 72, 2049), (300, 200, 9000)])
+@pytest.mark.parametrize("grad,table", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("pad,offset", [(0, 0), (3, 1), (8, 8)])
+def test_gradient(sp, V, D, T, grad, table, pad, offset):
+    r = np.random.default_rng([23, V, D, T])
+    ids = tokens(r, T, V)
+    g = rows(r.normal(size=(T, D)), grad, pad, offset)
+    dt = rows(np.full((V, D), 5.0), table, pad, offset)
+    ids_d = torch.from_numpy(ids).to(torch.int32).cuda()
+    sp.spike_embed_backward(g, ids_d, dt, scale=1.3)
+    torch.cuda.synchronize()
+    gh = g.double().cpu().numpy()
+    want = so.embed_backward(gh, ids, V, 1.3)
+    n = np.bincount(ids[(ids >= 0) & (ids < V)], minlength=V)[:, None]
+    lim = (n + 4) * U * so.embed_backward(np.abs(gh), ids, V, 1.3) + HALF_UNIT[table] * np.abs(want) * 1.01
+    got = dt.double().cpu().numpy()
+    assert (np.abs(got - want) <= lim).all()
+    assert (got[n[:, 0] == 0] == 0).all()
+    again = torch.empty_like(dt)
+    sp.spike_embed_backward(g, ids_d, again, scale=1.3)
+    torch.cuda.synchronize()
+    assert torch.equal(again, dt), "equal calls give equal bits"
+
+
+def test_gradient_against_differences(sp):
+    """Along a direction of the table: sum(out * w) is linear, so differences are exact to rounding."""
+    r = np.random.default_rng(24)
+    ids = tokens(r, 400, 50)
+    w, v = r.normal(size=(400, 96)).astype(np.float32), r.normal(size=(50, 96))
+    dt = torch.empty((50, 96), device="cuda")
+    sp.spike_embed_backward(rows(w, "f32"), torch.from_numpy(ids).cuda(), dt, scale=2.0)
+    f = lambda t: (so.embed_forward(t * v, ids, 2.0) * w).sum()  # noqa: E731
+    got = (dt.double().cpu().numpy() * v).sum()
+    assert abs(got - (f(1.0) - f(-1.0)) / 2) <= 400 * U * (np.abs(so.embed_backward(np.abs(w), ids, 50, 2.0) * v)).sum()
+
+
+def test_one_token_everywhere_and_none(sp):
+    for T in (1, 31, 32, 33, 2048, 6000):
+        g = torch.ones((T, 40), device="cuda")
+        dt = torch.full((6, 40), 3.0, device="cuda")
+        sp.spike_embed_backward(g, torch.full((T,), 4, dtype=torch.int64, device="cuda"), dt)
+        assert (dt[4] == T).all() and (dt[[0, 1, 2, 3, 5]] == 0).all()
+        dt.fill_(3.0)
+        sp.spike_embed_backward(g, torch.full((T,), -1, dtype=torch.int64, device="cuda"), dt, accumulate=True)
+        assert (dt == 3).all()
+        sp.spike_embed_backward(g, torch.full((T,), 6, dtype=torch.int64, device="cuda"), dt)
+        assert (dt == 0).all()
+
+
+def test_masked_gradients_are_not_read(sp):
+    """NaN and infinite gradients of padding tokens change nothing."""
+    g = torch.ones((100, 24), device="cuda")
+    ids = torch.arange(100, device="cuda") % 10
+    ids[::7] = -1
+    g[::7] = float("nan")
+    dt = torch.empty((10, 24), device="cuda")
+    sp.spike_embed_backward(g, ids, dt)
+    assert torch.equal(dt[:, 0].cpu(), torch.bincount(ids[ids >= 0], minlength=10).float().cpu())
+
+
+def test_no_tokens(sp):
+    ids = torch.empty(0, dtype=torch.int32, device="cuda")
+    dt = torch.full((5, 12), 3.0, device="cuda")
+    sp.spike_embed_forward(dt, ids, torch.empty((0, 12), device="cuda"))
+    sp.spike_embed_backward(torch.empty((0, 12), device="cuda"), ids, dt, accumulate=True)
+    assert (dt == 3).all()
+    sp.spike_embed_backward(torch.empty((0, 12), device="cuda"), ids, dt)
+    assert (dt == 0).all()
+
+
+def test_graph_replays_and_streams(sp):
+    r = np.random.default_rng(25)
+    ids = torch.from_numpy(tokens(r, 3000, 200)).cuda()
+    g, table = rows(r.normal(size=(3000, 64)), "f32"), rows(r.normal(size=(200, 64)), "f32")
+    out, dt = torch.empty((3000, 64), device="cuda"), torch.empty((200, 64), device="cuda")
+    ws = torch.empty(sp.spike_embed_workspace_bytes(3000, 64), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        sp.spike_embed_forward(table, ids, out, scale=3.0, stream=stream)
+        sp.spike_embed_backward(g, ids, dt, scale=3.0, workspace=ws, stream=stream)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(4):
+        ids.copy_(torch.from_numpy(tokens(r, 3000, 200)))
+        step()
+        torch.cuda.synchronize()
+        want = out.clone(), dt.clone()
+        for t in (out, dt, ws):
+            t.zero_()
+        if i % 2:
+            st = torch.cuda.Stream()
+            st.wait_stream(torch.cuda.current_stream())
+            step(st)
+        else:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(dt, want[1])
+
+
+def test_launches(sp):
+    """Vectors where rows allow, one sorting kernel for up to 2,048 tokens, two above."""
+    def names(T, D):
+        g, dt = torch.zeros((T, D), device="cuda"), torch.zeros((50, D), device="cuda")
+        ids = torch.zeros(T, dtype=torch.int32, device="cuda")
+        ws = torch.empty(sp.spike_embed_workspace_bytes(T, D), dtype=torch.uint8, device="cuda")
+        return [k.split("<")[0] for k in kernels(lambda st: sp.spike_embed_backward(g, ids, dt, workspace=ws, stream=st))]
+
+    assert names(2048, 64)[:2] == ["k_embed_sort", "k_embed_sum"]
+    assert names(2049, 64)[:3] == ["k_embed_sort", "k_embed_merge", "k_embed_sum"]
+
+
+def test_refusals(sp):
+    t, ids = torch.zeros((5, 12), device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    out = torch.zeros((3, 12), device="cuda")
+    with pytest.raises(TypeError, match="ids"):
+        sp.spike_embed_forward(t, ids.float(), out)
+    with pytest.raises(ValueError, match="out"):
+        sp.spike_embed_forward(t, ids, out[:2])
+    with pytest.raises(sp.SpikeError, match="row scales"):
+        sp.spike_embed_forward(t.to(torch.int8), ids, out)
+    with pytest.raises(sp.SpikeError, match="row scales"):
+        sp.spike_embed_forward(t, ids, out, row_scale=torch.ones(5, device="cuda"))
+    with pytest.raises(sp.SpikeError, match="finite"):
+        sp.spike_embed_forward(t, ids, out, scale=float("nan"))
+    with pytest.raises(TypeError, match="dtable"):
+        sp.spike_embed_backward(out, ids, t.to(torch.int8))
+    with pytest.raises(ValueError, match="grad"):
+        sp.spike_embed_backward(out[:, :11], ids, t)
+    with pytest.raises(sp.SpikeError, match="workspace"):
+        sp.spike_embed_backward(out, ids, t, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
