@@ -47,8 +47,8 @@
  * DENSE_FUSED_BACKWARD); calls on it only read them, so it may be used on
  * several streams at once.  forward and backward enqueue kernels on `stream`
  * (a hipStream_t, NULL for the default stream), allocate nothing, do not
- * synchronise and can be captured in a HIP graph.  backward's workspace
- * (dense_fused_workspace_bytes, 16-byte aligned, no initial contents) is the
+ * synchronise and can be captured in a HIP graph.  The workspaces (their sizes
+ * from the two queries below, 16-byte aligned, no initial contents) are the
  * caller's; calls that share one must not overlap.
  *
  * Errors: SPIKE_OK (0) or a negative code from spike_proj.h, with the message
@@ -88,7 +88,14 @@ int dense_fused_destroy(dense_fused_t handle);
 
 int dense_fused_forward(dense_fused_t handle, const void *x, int32_t x_type, int64_t ld_x, int32_t B,
                         const float *bias, int32_t act, const void *residual, int64_t ld_residual, void *y,
-                        int32_t y_type, int64_t ld_y, void *pre, int64_t ld_pre, void *stream);
+                        int32_t y_type, int64_t ld_y, void *pre, int64_t ld_pre, void *workspace,
+                        int64_t workspace_bytes, void *stream);
+
+/* Workspace of dense_fused_forward for these rows: 0 (it may then be NULL)
+ * for few rows, and for 16-bit ones that start on 16-byte boundaries with K a
+ * multiple of 8; -1 for a null handle or a size or type it refuses. */
+int64_t dense_fused_forward_workspace_bytes(dense_fused_t handle, const void *x, int32_t x_type, int64_t ld_x,
+                                            int32_t B);
 
 /* Workspace of dense_fused_backward for B rows; -1 for a null handle or a size or type it refuses. */
 int64_t dense_fused_workspace_bytes(dense_fused_t handle, int32_t B, int32_t y_type);

@@ -50,7 +50,7 @@ EXPORTED = (
     "spike_stack_forward_fused", "dense_proj_forward", "dense_proj_plan", "dense_proj_tune",
     "spike_quantize_int8", "spike_check_scale_shape", "head_verify_forward", "head_verify_workspace_bytes",
     "dense_fused_create", "dense_fused_destroy", "dense_fused_forward", "dense_fused_workspace_bytes",
-    "dense_fused_backward", "spike_embed_forward", "spike_embed_workspace_bytes", "spike_embed_backward",
+    "dense_fused_forward_workspace_bytes", "dense_fused_backward", "spike_embed_forward", "spike_embed_workspace_bytes", "spike_embed_backward",
     "head_draft_workspace_bytes", "head_draft_verify",
 )
 
@@ -88,7 +88,8 @@ _sig = {
     "head_verify_workspace_bytes": [],
     "dense_fused_create": [_p, _p, _i32, _i32, _i32, ctypes.POINTER(_p)],
     "dense_fused_destroy": [_p],
-    "dense_fused_forward": [_p, _p, _i32, _i64, _i32, _p, _i32, _p, _i64, _p, _i32, _i64, _p, _i64, _p],
+    "dense_fused_forward": [_p, _p, _i32, _i64, _i32, _p, _i32, _p, _i64, _p, _i32, _i64, _p, _i64, _p, _i64, _p],
+    "dense_fused_forward_workspace_bytes": [_p, _p, _i32, _i64, _i32],
     "dense_fused_workspace_bytes": [_p, _i32, _i32],
     "dense_fused_backward": [_p, _p, _i32, _i64, _p, _i64, _i32, _i32, _p, _i32, _i64, _p, _p, _i64, _p],
     "spike_embed_forward": [_p, _i32, _p, _i32, _i32, _i64, _p, _i32, _i32, _f32, _p, _i32, _i64, _p],
@@ -102,8 +103,8 @@ for _name, _args in _sig.items():
     getattr(_lib, _name).restype = ctypes.c_int
 _lib.spike_proj_last_error.argtypes = []
 _lib.spike_proj_last_error.restype = ctypes.c_char_p
-for _name in ("head_verify_workspace_bytes", "dense_fused_workspace_bytes", "spike_embed_workspace_bytes",
-              "head_draft_workspace_bytes"):
+for _name in ("head_verify_workspace_bytes", "dense_fused_forward_workspace_bytes", "dense_fused_workspace_bytes",
+              "spike_embed_workspace_bytes", "head_draft_workspace_bytes"):
     getattr(_lib, _name).restype = ctypes.c_int64
 
 
@@ -511,7 +512,7 @@ def dense_fused_destroy(h: DenseFused) -> None:
 
 def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: torch.Tensor | None = None,
                         act: int = DENSE_ACT_NONE, residual: torch.Tensor | None = None,
-                        pre: torch.Tensor | None = None, stream=None) -> None:
+                        pre: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None) -> None:
     """y = act(z) + residual, z = scale * (x @ float(Q).T) + bias (dense_fused.h); z also to `pre`.
     x: [B, K]; y, residual, pre: [B, M] of one type; rows may be strided."""
     B = x.shape[0]
@@ -525,8 +526,19 @@ def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: t
         pp, ldp = _rows(pre, "pre", B, h.M)
     if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
         raise TypeError("residual and pre must have y's type")
-    _check(_lib.dense_fused_forward(h.ptr, xp, _type_of(x, "x"), ldx, B, _vector(bias, "bias", h.M), act, rp, ldr, yp,
-                                    _type_of(y, "y"), ldy, pp, ldp, _stream(stream)), "dense_fused_forward")
+    x_type = _type_of(x, "x")
+    wp, n_ws = None, int(_lib.dense_fused_forward_workspace_bytes(h.ptr, xp, x_type, ldx, B))
+    if n_ws > 0:
+        workspace = _workspace(workspace, n_ws, x.device, stream)
+        wp, n_ws = _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    _check(_lib.dense_fused_forward(h.ptr, xp, x_type, ldx, B, _vector(bias, "bias", h.M), act, rp, ldr, yp,
+                                    _type_of(y, "y"), ldy, pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward")
+
+
+def dense_fused_forward_workspace_bytes(h: DenseFused, x: torch.Tensor) -> int:
+    """Workspace of dense_fused_forward for these activations [B, K]."""
+    xp, ldx = _rows(x, "x", x.shape[0], h.K)
+    return int(_lib.dense_fused_forward_workspace_bytes(h.ptr, xp, _type_of(x, "x"), ldx, x.shape[0]))
 
 
 def dense_fused_workspace_bytes(h: DenseFused, B: int, dtype: torch.dtype) -> int:

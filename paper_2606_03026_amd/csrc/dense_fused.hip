@@ -78,57 +78,195 @@ int check_device(int want)
     return SPIKE_OK;
 }
 
-template <typename XT, int NS, bool VECX>
-void launch_product(FusedArgs a, hipStream_t st)
+constexpr int kCUs = 256;
+
+// Rows up to which a call reads the activations straight from memory.
+constexpr int kFewRows = 32;
+
+template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
+void launch_tile(FusedArgs a, hipStream_t st)
 {
-    if (a.B <= 32) {
-        constexpr int WK = 8;
-        const int tiles = (a.n_out + 15) / 16;
-        hipLaunchKernelGGL((spk::k_fused_rows<XT, NS, 1, 1, WK, VECX>), dim3((unsigned)tiles, (unsigned)((a.B + 15) / 16)),
-                           dim3(64 * WK), 0, st, a);
-        return;
-    }
-    constexpr int MT = 2, NT = 2, WM = 2, WN = 2;
     a.out_tiles = (a.n_out + 16 * MT * WM - 1) / (16 * MT * WM);
     a.row_tiles = (a.B + 16 * NT * WN - 1) / (16 * NT * WN);
-    const int64_t total = (int64_t)a.out_tiles * a.row_tiles;
-    hipLaunchKernelGGL((spk::k_fused_tile<XT, NS, MT, NT, WM, WN, VECX>), dim3((unsigned)((total + 7) / 8 * 8)),
-                       dim3(64 * WM * WN), 0, st, a);
+    const int64_t total = (int64_t)a.out_tiles * a.row_tiles * a.splits;
+    constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D>();
+    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D>), dim3((unsigned)((total + 7) / 8 * 8)),
+                       dim3(64 * WM * WN), lds, st, a);
+}
+
+// A tile shape of k_fused_tile, and what a step of 64 inputs of one of its
+// tiles takes: `alone` on its compute unit (latency), and `among` others that
+// keep the unit busy (throughput), in us.
+struct TileShape {
+    int outs, rows;
+    float alone, among;
+};
+
+// Measured over 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 33 to 8192 rows:
+// BF16 and F16 (one plane), FP32 (three).
+constexpr TileShape kShapes1[] = {
+    {256, 128, 0.79f, 0.95f}, {128, 128, 0.58f, 0.50f}, {128, 64, 0.35f, 0.34f}, {64, 64, 0.28f, 0.209f}, {64, 32, 0.22f, 0.131f}};
+constexpr TileShape kShapes3[] = {{256, 64, 1.03f, 1.22f}, {128, 32, 0.42f, 0.43f}, {64, 32, 0.34f, 0.285f}};
+
+struct TilePlan {
+    int shape, splits;
+};
+
+// The shape, and the workgroups that share a tile's steps, with the least
+// estimated time: steps of the tiles that come to one compute unit, and for a
+// split the join (a launch, and the FP32 sums written and read at 3.9 MB/us).
+// What the estimate stands for, in us at 1536 inputs, BF16: 1536 outputs and 64 rows
+// 8.7 in tiles of 64 x 32, 25 in 256 x 128; 6144 outputs and 2500 rows 98 and 51. With
+// 6144 inputs, 1536 outputs and 64 rows 24.6 in one part, 14 in four; with 2500
+// rows 59 in one, 80 in two.
+TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
+{
+    const TileShape* shapes = ns == 1 ? kShapes1 : kShapes3;
+    const int n = ns == 1 ? 5 : 3;
+    const float parts = ns == 2 ? 2.0f / 3.0f : 1.0f;
+    TilePlan best{0, 1};
+    float least = 0.0f;
+    for (int i = 0; i < n; ++i)
+        for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 8); ++splits) {
+            const int64_t tiles = (((int64_t)n_out + shapes[i].outs - 1) / shapes[i].outs) *
+                                  (((int64_t)B + shapes[i].rows - 1) / shapes[i].rows) * splits;
+            const float per_unit = (float)((tiles + kCUs - 1) / kCUs) * shapes[i].among;
+            float us = (float)((steps + splits - 1) / splits) * parts * std::max(shapes[i].alone, per_unit);
+            if (splits > 1)
+                us += 3.5f + (float)splits * (float)B * (float)n_out * (4.0f / 3.9e6f);
+            if ((i == 0 && splits == 1) || us < least)
+                least = us, best = TilePlan{i, splits};
+        }
+    // only parts that have steps
+    const int each = (steps + best.splits - 1) / best.splits;
+    best.splits = (steps + each - 1) / each;
+    return best;
+}
+
+// The sums of a split product: rows of n_out rounded up to 8 elements.
+int64_t split_bytes(const TilePlan& p, int32_t B, int32_t n_out)
+{
+    return p.splits > 1 ? p.splits * spk::fused_pad(n_out, 8) * B * 4 : 0;
+}
+
+// The product of NS planes of activations; `part`: split_bytes for a split one.
+template <typename OT, int NS>
+void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
+{
+    const TilePlan p = tile_plan(NS, a.B, a.n_out, a.steps);
+    FusedArgs t = a;
+    t.splits = p.splits;
+    t.split_steps = (a.steps + p.splits - 1) / p.splits;
+    if (p.splits > 1) {
+        t.y = part, t.y_type = SPIKE_TYPE_F32, t.ld_y = spk::fused_pad(a.n_out, 8), t.split_stride = t.ld_y * a.B;
+        t.scale = t.bias = nullptr, t.act = 0, t.residual = t.pre = nullptr, t.vec_out = 1;
+    }
+    if constexpr (NS == 1) {
+        switch (p.shape) {
+        case 0: launch_tile<OT, NS, 4, 8, 4, 1, 2>(t, st); break;
+        case 1: launch_tile<OT, NS, 2, 8, 4, 1, 2>(t, st); break;
+        case 2: launch_tile<OT, NS, 2, 4, 4, 1, 4>(t, st); break;
+        case 3: launch_tile<OT, NS, 1, 4, 4, 1, 4>(t, st); break;
+        default: launch_tile<OT, NS, 1, 2, 4, 1, 4>(t, st); break;
+        }
+    } else {
+        switch (p.shape) {
+        case 0: launch_tile<OT, NS, 4, 4, 4, 1, 2>(t, st); break;
+        case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4>(t, st); break;
+        default: launch_tile<OT, NS, 1, 2, 4, 1, 4>(t, st); break;
+        }
+    }
+    if (p.splits > 1) {
+        t = a;
+        t.splits = p.splits;
+        const int64_t ld = spk::fused_pad(a.n_out, 8), groups = ld / 8 * a.B;
+        hipLaunchKernelGGL(spk::k_fused_join, dim3((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16)), dim3(256), 0,
+                           st, t, part, ld);
+    }
+}
+
+template <typename XT, int NS, int NB, int MT, bool VECX>
+void launch_rows(const FusedArgs& a, hipStream_t st)
+{
+    constexpr int WK = 8;
+    const dim3 grid((unsigned)((a.n_out + 16 * MT - 1) / (16 * MT)), (unsigned)((a.B + 16 * NB - 1) / (16 * NB)));
+    hipLaunchKernelGGL((spk::k_fused_rows<XT, NS, NB, MT, WK, VECX>), grid, dim3(64 * WK), 0, st, a);
+}
+
+// Few rows.  Tiles of outputs that a workgroup takes together share what it does
+// to the activations (the cutting of FP32 ones costs more than a tile's weights),
+// and the 17th to 32nd row share the weights: FP32, 1536 -> 6144, one row 5.9 us
+// one by one and 5.1 by twos; 1536 -> 57,344 41 and 17.4 by fours, 16 rows 55 and
+// 18.2.  Fewer outputs than that leave compute units idle.
+template <typename XT, int NS, bool VECX>
+void launch_few(const FusedArgs& a, hipStream_t st)
+{
+    const int tiles = (a.n_out + 15) / 16;
+    if (tiles < kCUs)
+        launch_rows<XT, NS, 1, 1, VECX>(a, st);
+    else if (tiles < 8 * kCUs)
+        launch_rows<XT, NS, 1, 2, VECX>(a, st);
+    else if (a.B <= 16)
+        launch_rows<XT, NS, 1, 4, VECX>(a, st);
+    else
+        launch_rows<XT, NS, 2, 4, VECX>(a, st);
+}
+
+// Whether the rows of p start on 16-byte boundaries.
+bool whole(const void* p, int type, int64_t ld) { return !p || (aligned_to(p, 16) && ld * type_bytes(type) % 16 == 0); }
+
+// Rows that go in groups of 8, 256 of them within a buffer resource.
+bool in_chunks(const void* x, int type, int64_t ld, int32_t n)
+{
+    return whole(x, type, ld) && n % 8 == 0 && ld < spk::kBufMaxBytes / (256 * (int64_t)type_bytes(type));
 }
 
 template <typename XT, int NS>
-void launch_aligned(const FusedArgs& a, hipStream_t st)
+void few_rows(const FusedArgs& a, bool chunks, hipStream_t st)
 {
-    if (aligned_to(a.x, 16) && a.ld_x * sizeof(XT) % 16 == 0)
-        launch_product<XT, NS, true>(a, st);
-    else
-        launch_product<XT, NS, false>(a, st);
+    chunks ? launch_few<XT, NS, true>(a, st) : launch_few<XT, NS, false>(a, st);
 }
 
-// Four elements of a row of p at a time (8 bytes of the narrow types, 16 of FP32).
-bool fours(const void* p, int type, int64_t ld) { return !p || (aligned_to(p, 4 * type_bytes(type)) && ld % 4 == 0); }
+// Planes of cut activations or gradients: their rows are padded to whole chunks.
+int64_t plane_stride(int32_t n) { return spk::fused_pad(n, 8); }
+int64_t planes_bytes(int ns, int32_t B, int32_t n) { return spk::fused_pad(ns * plane_stride(n) * B * 2, 16); }
 
-// Rows of g * scale in the workspace: whole vectors, at 16-byte boundaries.
-int64_t gate_stride(int32_t M) { return spk::fused_pad(M, 8); }
-int gate_bytes(int y_type) { return y_type == SPIKE_TYPE_BF16 ? 2 : 4; }
+template <typename XT, int NS>
+void cut_rows(FusedArgs& a, void* workspace, hipStream_t st)
+{
+    const int64_t ld = plane_stride(a.n_in), groups = ld / 8 * a.B;
+    uint16_t* out = static_cast<uint16_t*>(workspace);
+    hipLaunchKernelGGL((spk::k_fused_cut<XT, NS>), dim3((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16)), dim3(256),
+                       0, st, static_cast<const XT*>(a.x), a.ld_x, a.B, a.n_in, ld, ld * a.B, out,
+                       (int)whole(a.x, NS == 3 ? SPIKE_TYPE_F32 : SPIKE_TYPE_BF16, a.ld_x));
+    a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld;
+}
+
 // Rows of a workgroup of the gate, and the parts the bias gradient comes in: at most 32.
 int gate_rows(int32_t B) { return (int)std::max<int64_t>(16, ((int64_t)B + 31) / 32); }
 int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 
-template <typename T, typename TG>
+// What g * scale is kept in between the gate and the product: planes, or FP32
+// rows where the product takes few of them (BF16: one plane, also then).
+int gate_planes(int y_type, int32_t B)
+{
+    return y_type == SPIKE_TYPE_BF16 ? 1 : B <= kFewRows ? 0 : y_type == SPIKE_TYPE_F32 ? 3 : 2;
+}
+int64_t gate_bytes(int y_type, int32_t B, int32_t M)
+{
+    const int ns = gate_planes(y_type, B);
+    return ns == 0 ? spk::fused_pad(plane_stride(M) * B * 4, 16) : planes_bytes(ns, B, M);
+}
+
+template <typename T, int NS>
 void launch_gate(const dense_fused* h, const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre, int act, int32_t B,
-                 TG* gs, float* partial, int y_type, hipStream_t st)
+                 void* gs, float* partial, int y_type, hipStream_t st)
 {
     const dim3 grid((unsigned)((h->M + spk::kGateCols - 1) / spk::kGateCols), (unsigned)gate_parts(B));
-    auto whole = [&](const void* p, int64_t ld) { return !p || (aligned_to(p, 16) && ld * type_bytes(y_type) % 16 == 0); };
-    if (whole(dy, ld_dy) && whole(pre, ld_pre))
-        hipLaunchKernelGGL((spk::k_fused_gate<T, TG, true>), grid, dim3(256), 0, st, static_cast<const T*>(dy), ld_dy,
-                           static_cast<const T*>(pre), ld_pre, act, B, h->M, gate_rows(B), h->scale, gs, gate_stride(h->M),
-                           partial);
-    else
-        hipLaunchKernelGGL((spk::k_fused_gate<T, TG, false>), grid, dim3(256), 0, st, static_cast<const T*>(dy), ld_dy,
-                           static_cast<const T*>(pre), ld_pre, act, B, h->M, gate_rows(B), h->scale, gs, gate_stride(h->M),
-                           partial);
+    const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
+    hipLaunchKernelGGL(vec ? (spk::k_fused_gate<T, NS, true>) : (spk::k_fused_gate<T, NS, false>), grid, dim3(256), 0, st,
+                       static_cast<const T*>(dy), ld_dy, static_cast<const T*>(pre), ld_pre, act, B, h->M, gate_rows(B),
+                       h->scale, static_cast<uint16_t*>(gs), plane_stride(h->M), plane_stride(h->M) * B, partial);
 }
 
 int check_rows(int32_t B, int32_t act, int x_type, int y_type)
@@ -158,6 +296,7 @@ int dense_fused_create(const int8_t* Q, const float* scale, int32_t K, int32_t M
         return fail(SPIKE_EINVAL, "scale must be 4-byte aligned");
     if (K < 1 || K > FUSED_MAX_DIM || M < 1 || M > FUSED_MAX_DIM)
         return fail(SPIKE_EINVAL, "K = %d, M = %d outside [1, %d]", K, M, FUSED_MAX_DIM);
+    // (rows of K or M elements, 256 of them, also stay within a buffer resource)
     if (spk::fused_pad(K, 64) * spk::fused_pad(M, 64) >= ((int64_t)1 << 31))
         return fail(SPIKE_EUNSUPPORTED, "K * M = %lld, each rounded up to 64, reaches 2^31", (long long)K * M);
     if (flags & ~DENSE_FUSED_BACKWARD)
@@ -189,9 +328,20 @@ int dense_fused_destroy(dense_fused_t h)
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "hipDeviceSynchronize");
 }
 
+int64_t dense_fused_forward_workspace_bytes(dense_fused_t h, const void* x, int32_t x_type, int64_t ld_x, int32_t B)
+{
+    if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(x_type))
+        return -1;
+    if (B <= kFewRows)
+        return 0;
+    const int ns = x_type == SPIKE_TYPE_F32 ? 3 : 1;
+    const int64_t sums = split_bytes(tile_plan(ns, B, h->M, (h->K + spk::kFusedStep - 1) / spk::kFusedStep), B, h->M);
+    return sums + (ns == 1 && in_chunks(x, x_type, ld_x, h->K) ? 0 : planes_bytes(ns, B, h->K));
+}
+
 int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t ld_x, int32_t B, const float* bias,
                         int32_t act, const void* residual, int64_t ld_residual, void* y, int32_t y_type, int64_t ld_y,
-                        void* pre, int64_t ld_pre, void* stream)
+                        void* pre, int64_t ld_pre, void* workspace, int64_t workspace_bytes, void* stream)
 {
     spk::last_error.clear();
     if (!h)
@@ -207,6 +357,10 @@ int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t 
     if (!aligned_to(x, type_bytes(x_type)) || !aligned_to(y, type_bytes(y_type)) || !aligned_to(bias, 4) ||
         !aligned_to(residual, type_bytes(y_type)) || !aligned_to(pre, type_bytes(y_type)))
         return fail(SPIKE_EINVAL, "a pointer is not aligned to its element");
+    const int64_t need = dense_fused_forward_workspace_bytes(h, x, x_type, ld_x, B);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)))
+        return fail(SPIKE_EINVAL, "workspace of %lld bytes at %p, needs %lld, 16-byte aligned",
+                    (long long)workspace_bytes, workspace, (long long)need);
     if (int rc = check_device(h->device))
         return rc;
     FusedArgs a{};
@@ -214,12 +368,28 @@ int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t 
     a.x = x, a.ld_x = ld_x, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
     a.residual = residual, a.ld_residual = ld_residual, a.y = y, a.y_type = y_type, a.ld_y = ld_y;
     a.pre = pre, a.ld_pre = ld_pre;
-    a.vec_out = fours(y, y_type, ld_y) && fours(residual, y_type, ld_residual) && fours(pre, y_type, ld_pre);
+    a.vec_out = whole(y, y_type, ld_y) && whole(residual, y_type, ld_residual) && whole(pre, y_type, ld_pre);
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    switch (x_type) {
-    case SPIKE_TYPE_F32: launch_aligned<float, 3>(a, st); break;
-    case SPIKE_TYPE_BF16: launch_aligned<spk::bf16, 1>(a, st); break;
-    default: launch_aligned<spk::f16, 1>(a, st); break;
+    const bool chunks = in_chunks(x, x_type, ld_x, h->K);
+    if (B <= kFewRows) {
+        switch (x_type) {
+        case SPIKE_TYPE_F32: few_rows<float, 3>(a, chunks, st); break;
+        case SPIKE_TYPE_BF16: few_rows<spk::bf16, 1>(a, chunks, st); break;
+        default: few_rows<spk::f16, 1>(a, chunks, st); break;
+        }
+    } else {
+        // first the planes where x has to be cut, then the sums of a split product
+        const int ns = x_type == SPIKE_TYPE_F32 ? 3 : 1;
+        float* part = static_cast<float*>(workspace);
+        if (ns == 3 || !chunks) {
+            part = reinterpret_cast<float*>(static_cast<char*>(workspace) + planes_bytes(ns, B, h->K));
+            ns == 3 ? cut_rows<float, 3>(a, workspace, st) : cut_rows<uint16_t, 1>(a, workspace, st);
+        }
+        switch (x_type) {
+        case SPIKE_TYPE_F32: launch_planes<spk::bf16, 3>(a, part, st); break;
+        case SPIKE_TYPE_BF16: launch_planes<spk::bf16, 1>(a, part, st); break;
+        default: launch_planes<spk::f16, 1>(a, part, st); break;
+        }
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "fused projection launch");
@@ -229,7 +399,11 @@ int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
 {
     if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(y_type))
         return -1;
-    return spk::fused_pad(gate_stride(h->M) * B * gate_bytes(y_type), 16) + (int64_t)gate_parts(B) * h->M * 4;
+    const int64_t sums = B <= kFewRows ? 0
+                                       : split_bytes(tile_plan(gate_planes(y_type, B), B, h->K,
+                                                               (h->M + spk::kFusedStep - 1) / spk::kFusedStep),
+                                                     B, h->K);
+    return gate_bytes(y_type, B, h->M) + sums + spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
 }
 
 int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_t ld_dy, const void* pre, int64_t ld_pre,
@@ -268,19 +442,20 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
     float* partial = nullptr;
     if (B > 0) {
         void* gs = dx ? workspace : nullptr;
-        partial = dbias ? reinterpret_cast<float*>(static_cast<char*>(workspace) +
-                                                   spk::fused_pad(gate_stride(h->M) * B * gate_bytes(y_type), 16))
-                        : nullptr;
+        if (dbias)
+            partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M));
+        const bool few = B <= kFewRows;
         switch (y_type) {
         case SPIKE_TYPE_F32:
-            launch_gate<float, float>(h, dy, ld_dy, pre, ld_pre, act, B, static_cast<float*>(gs), partial, y_type, st);
+            few ? launch_gate<float, 0>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st)
+                : launch_gate<float, 3>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
             break;
         case SPIKE_TYPE_BF16:
-            launch_gate<spk::bf16, spk::bf16>(h, dy, ld_dy, pre, ld_pre, act, B, static_cast<spk::bf16*>(gs), partial,
-                                              y_type, st);
+            launch_gate<spk::bf16, 1>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
             break;
         default:
-            launch_gate<spk::f16, float>(h, dy, ld_dy, pre, ld_pre, act, B, static_cast<float*>(gs), partial, y_type, st);
+            few ? launch_gate<spk::f16, 0>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st)
+                : launch_gate<spk::f16, 2>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
         }
     }
     if (dbias)
@@ -288,14 +463,19 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
                            dbias);
     if (dx && B > 0) {
         FusedArgs a{};
-        a.P = h->Pt, a.n_out = h->K, a.n_in = h->M, a.steps = (h->M + spk::kFusedStep - 1) / spk::kFusedStep;
-        a.x = workspace, a.ld_x = gate_stride(h->M), a.B = B;
+        // the rows of g * scale are padded with zeros, as the weights are
+        a.P = h->Pt, a.n_out = h->K, a.n_in = (int)plane_stride(h->M), a.steps = (h->M + spk::kFusedStep - 1) / spk::kFusedStep;
+        a.x = workspace, a.ld_x = plane_stride(h->M), a.plane = plane_stride(h->M) * B, a.B = B;
         a.y = dx, a.y_type = x_type, a.ld_y = ld_dx;
-        a.vec_out = fours(dx, x_type, ld_dx);
+        a.vec_out = whole(dx, x_type, ld_dx);
+        // the workspace: g * scale, the parts of the bias gradient, the sums of a split product
+        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M) +
+                                               spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
+        const bool few = B <= kFewRows;
         switch (y_type) {
-        case SPIKE_TYPE_F32: launch_aligned<float, 3>(a, st); break;
-        case SPIKE_TYPE_BF16: launch_aligned<spk::bf16, 1>(a, st); break;
-        default: launch_aligned<float, 2>(a, st); break;
+        case SPIKE_TYPE_F32: few ? few_rows<float, 3>(a, true, st) : launch_planes<spk::bf16, 3>(a, part, st); break;
+        case SPIKE_TYPE_BF16: few ? few_rows<spk::bf16, 1>(a, true, st) : launch_planes<spk::bf16, 1>(a, part, st); break;
+        default: few ? few_rows<float, 2>(a, true, st) : launch_planes<spk::bf16, 2>(a, part, st); break;
         }
     }
     const hipError_t e = hipGetLastError();

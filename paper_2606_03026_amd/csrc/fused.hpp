@@ -10,6 +10,8 @@
 // neighbouring outputs of one row.
 #pragma once
 
+#include <type_traits>
+
 #include "types.hpp"
 
 namespace spk {
@@ -59,59 +61,103 @@ __device__ inline uint32_t high_halves(float lo, float hi)
     return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
 
-// 8 codes -> 8 operand values, exactly (a float holding one has its lower half zero).
+// Codes 2 i and 2 i + 1 of a register of four -> two operand values, exactly (a
+// float that holds a code has its lower half zero).
+template <typename OT>
+__device__ inline uint32_t widen_pair(uint32_t w, int i)
+{
+    const float a = (float)(int8_t)(w >> (i * 16)), b = (float)(int8_t)(w >> (i * 16 + 8));
+    if constexpr (__is_same(OT, f16)) {
+        typedef __fp16 h2 __attribute__((ext_vector_type(2)));
+        const h2 p = __builtin_amdgcn_cvt_pkrtz(a, b);
+        return __builtin_bit_cast(uint32_t, p);
+    } else {
+        return high_halves(a, b);
+    }
+}
+
 template <typename OT>
 __device__ inline u32x4 widen_codes(uint32_t w0, uint32_t w1)
 {
-    u32x4 r;
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t w = i < 2 ? w0 : w1;
-        const float a = (float)(int8_t)(w >> (i % 2 * 16)), b = (float)(int8_t)(w >> (i % 2 * 16 + 8));
-        if constexpr (sizeof(OT) == 2 && __is_same(OT, f16)) {
-            typedef __fp16 h2 __attribute__((ext_vector_type(2)));
-            const h2 p = __builtin_amdgcn_cvt_pkrtz(a, b);
-            r[i] = __builtin_bit_cast(uint32_t, p);
-        } else {
-            r[i] = high_halves(a, b);
-        }
-    }
-    return r;
+    return u32x4{widen_pair<OT>(w0, 0), widen_pair<OT>(w0, 1), widen_pair<OT>(w1, 0), widen_pair<OT>(w1, 1)};
 }
 
-// What of x is left after its upper 16 bits are taken off as a BF16 part; nothing of an infinity.
+// What of x is left after its upper 16 bits are taken off as a BF16 part; FIRST:
+// x may be infinite, and nothing is left of it then (of what is left, never).
+template <bool FIRST>
 __device__ inline float below_bf16(float x)
 {
     const float r = x - __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    return __builtin_isinf(x) ? 0.0f : r;
+    return FIRST && __builtin_isinf(x) ? 0.0f : r;
+}
+
+// v as NS BF16 parts at p, p + plane, ..: all but the last cut off, that one rounded.
+template <int NS>
+__device__ inline void put_planes(uint16_t* p, int64_t plane, float (&v)[8])
+{
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        u32x4 part;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (s + 1 < NS) {
+                part[i] = high_halves(v[2 * i], v[2 * i + 1]);
+                v[2 * i] = s == 0 ? below_bf16<true>(v[2 * i]) : below_bf16<false>(v[2 * i]);
+                v[2 * i + 1] = s == 0 ? below_bf16<true>(v[2 * i + 1]) : below_bf16<false>(v[2 * i + 1]);
+            } else {
+                typedef bf16 b2 __attribute__((ext_vector_type(2)));
+                part[i] = __builtin_bit_cast(uint32_t, b2{(bf16)v[2 * i], (bf16)v[2 * i + 1]});
+            }
+        }
+        *reinterpret_cast<u32x4*>(p + s * plane) = part;
+    }
 }
 
 // 8 activations as they were loaded.
 template <typename XT> struct Raw { u32x4 v; };
 template <> struct Raw<float> { f32x4 v[2]; };
 
-// Activations k .. k + 7 of a row that has n; zeros past it.
+// Activations k .. k + 7 of rows of n; zeros past them.  VECX: n is a multiple
+// of 8 and every row starts on a 16-byte boundary, so that a group of 8 lies
+// inside a row or outside as a whole; the rows are read through a buffer
+// resource that starts at `row0`, `at` elements from it.  Otherwise element by
+// element.  No branches: loads stay in flight across the steps.
 template <typename XT, bool VECX>
-__device__ inline Raw<XT> load_raw(const XT* row, int k, int n)
+__device__ inline Raw<XT> load_raw(const XT* row0, __amdgpu_buffer_rsrc_t rsrc, int64_t at, int k, int n)
 {
     Raw<XT> r;
-    if constexpr (sizeof(XT) == 4) {
-        if (VECX && k + 8 <= n) {
-            r.v[0] = *reinterpret_cast<const f32x4*>(row + k);
-            r.v[1] = *reinterpret_cast<const f32x4*>(row + k + 4);
+    if constexpr (VECX) {
+        const uint32_t off = k < n ? (uint32_t)(at + k) * (uint32_t)sizeof(XT) : kOutOfRange;
+        if constexpr (sizeof(XT) == 4) {
+            r.v[0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
+            r.v[1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 16, 0));
         } else {
-            for (int e = 0; e < 8; ++e)
-                r.v[e / 4][e % 4] = k + e < n ? row[k + e] : 0.0f;
+            r.v = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0));
         }
     } else {
-        if (VECX && k + 8 <= n) {
-            r.v = *reinterpret_cast<const u32x4*>(row + k);
+        const XT* row = row0 + at;
+        if constexpr (sizeof(XT) == 4) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = row[min(k + e, n - 1)];
+                r.v[e / 4][e % 4] = k + e < n ? v : 0.0f;
+            }
         } else {
             const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
-            for (int e = 0; e < 4; ++e)
-                r.v[e] = (k + 2 * e < n ? p[k + 2 * e] : 0u) | (k + 2 * e + 1 < n ? (uint32_t)p[k + 2 * e + 1] << 16 : 0u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = p[min(k + 2 * e, n - 1)], hi = p[min(k + 2 * e + 1, n - 1)];
+                r.v[e] = (k + 2 * e < n ? lo : 0u) | (k + 2 * e + 1 < n ? hi << 16 : 0u);
+            }
         }
     }
     return r;
+}
+
+template <typename XT>
+__device__ inline __amdgpu_buffer_rsrc_t rows_resource(const XT* row0)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<XT*>(row0), 0, (int)kBufMaxBytes, kBufferFlags);
 }
 
 // Their NS operand parts.
@@ -119,12 +165,16 @@ template <typename XT, int NS>
 __device__ inline void split_raw(const Raw<XT>& r, u32x4 (&part)[NS])
 {
     if constexpr (sizeof(XT) == 4) {
+#pragma unroll
         for (int i = 0; i < 4; ++i) {
             float a = r.v[i / 2][i % 2 * 2], b = r.v[i / 2][i % 2 * 2 + 1];
+#pragma unroll
             for (int s = 0; s < NS; ++s) {
                 part[s][i] = high_halves(a, b);
-                if (s + 1 < NS)
-                    a = below_bf16(a), b = below_bf16(b);
+                if (s + 1 < NS) {
+                    a = s == 0 ? below_bf16<true>(a) : below_bf16<false>(a);
+                    b = s == 0 ? below_bf16<true>(b) : below_bf16<false>(b);
+                }
             }
         }
     } else {
@@ -163,33 +213,60 @@ __device__ inline float gauss_tail(float a)
     return r * t;
 }
 
-__device__ inline float act_value(float z, int act)
+// act(z) and act'(z) of W values.
+template <int W>
+__device__ inline void act_values(float (&z)[W], int act)
 {
     switch (act) {
-    case 1: return z > 0.0f ? z : z == z ? 0.0f : z;
-    case 2: {
-        const float tail = __builtin_amdgcn_exp2f(z * z * -0.72134752f) * gauss_tail(__builtin_fabsf(z));
-        return z * (z < 0.0f ? tail : 1.0f - tail);
-    }
-    case 3: return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
-    default: return z;
+    case 1:
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            z[e] = z[e] > 0.0f ? z[e] : z[e] == z[e] ? 0.0f : z[e];
+        break;
+    case 2:
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float tail = __builtin_amdgcn_exp2f(z[e] * z[e] * -0.72134752f) * gauss_tail(__builtin_fabsf(z[e]));
+            z[e] *= z[e] < 0.0f ? tail : 1.0f - tail;
+        }
+        break;
+    case 3:
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            z[e] *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z[e] * -1.44269504f));
+        break;
+    default: break;
     }
 }
 
-__device__ inline float act_slope(float z, int act)
+template <int W>
+__device__ inline void act_slopes(float (&z)[W], int act)
 {
     switch (act) {
-    case 1: return z > 0.0f ? 1.0f : z == z ? 0.0f : z;
-    case 2: {
-        const float e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-        const float tail = e * gauss_tail(__builtin_fabsf(z));
-        return __builtin_fmaf(z, e * 0.39894228f, z < 0.0f ? tail : 1.0f - tail);
-    }
-    case 3: {
-        const float s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
-        return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
-    }
-    default: return 1.0f;
+    case 1:
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            z[e] = z[e] > 0.0f ? 1.0f : z[e] == z[e] ? 0.0f : z[e];
+        break;
+    case 2:
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float x = __builtin_amdgcn_exp2f(z[e] * z[e] * -0.72134752f);
+            const float tail = x * gauss_tail(__builtin_fabsf(z[e]));
+            z[e] = __builtin_fmaf(z[e], x * 0.39894228f, z[e] < 0.0f ? tail : 1.0f - tail);
+        }
+        break;
+    case 3:
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z[e] * -1.44269504f));
+            z[e] = sig * __builtin_fmaf(z[e], 1.0f - sig, 1.0f);
+        }
+        break;
+    default:
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            z[e] = 1.0f;
     }
 }
 
@@ -200,8 +277,9 @@ struct FusedArgs {
     int n_out, n_in, steps;
     const void* x;
     int64_t ld_x;
+    int64_t plane;       // elements between the planes of cut activations
     int B;
-    const float* scale;  // [n_out rounded up to 16], NULL: one
+    const float* scale;  // NULL: one
     const float* bias;
     int act;
     const void* residual;
@@ -211,72 +289,104 @@ struct FusedArgs {
     int64_t ld_y;
     void* pre;
     int64_t ld_pre;
-    int vec_out;         // rows of y, residual and pre go four elements at a time
+    int vec_out;         // rows of y, residual and pre go in vectors of 8 (16 bytes at most)
     int out_tiles, row_tiles;
+    int splits, split_steps;  // the steps go to `splits` workgroups, each writing its sums as FP32 rows at y
+    int64_t split_stride;     // elements between their outputs
 };
 
-template <typename T>
-__device__ inline f32x4 read4(const T* p, bool vec, int n)
+// W elements at p: at once where `vec`, else the first n one by one.
+template <typename T, int W>
+__device__ inline void read_w(const T* p, float (&v)[W], bool vec, int n)
 {
-    f32x4 v = {};
+    typedef T tw __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
     if (vec) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        v = __builtin_convertvector(*reinterpret_cast<const t4*>(p), f32x4);
+        const tw r = *reinterpret_cast<const tw*>(p);
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            v[e] = (float)r[e];
     } else {
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                v[e] = (float)p[e];
-    }
-    return v;
-}
-
-template <typename T>
-__device__ inline void write4(T* p, f32x4 v, bool vec, int n)
-{
-    for (int e = 0; e < 4; ++e)
-        v[e] = in_fp32<T>(v[e]);
-    if (vec) {
-        typedef T t4 __attribute__((ext_vector_type(4)));
-        *reinterpret_cast<t4*>(p) = __builtin_convertvector(v, t4);
-    } else {
-        for (int e = 0; e < 4; ++e)
-            if (e < n)
-                p[e] = (T)v[e];
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            v[e] = e < n ? (float)p[e] : 0.0f;
     }
 }
 
-template <typename T>
-__device__ inline void put_outputs(const FusedArgs& a, int m, int64_t b, f32x4 z, bool vec, int n)
+template <typename T, int W>
+__device__ inline void write_w(T* p, const float (&v)[W], bool vec, int n)
+{
+    typedef T tw __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
+    if (vec) {
+        tw r;
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            r[e] = (T)in_fp32<T>(v[e]);
+        *reinterpret_cast<tw*>(p) = r;
+    } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            if (e < n)
+                p[e] = (T)in_fp32<T>(v[e]);
+    }
+}
+
+template <typename T, int W>
+__device__ inline void put_outputs(const FusedArgs& a, int m, int64_t b, float (&z)[W], bool vec, int n, int64_t y_at)
 {
     if (a.pre)
-        write4(static_cast<T*>(a.pre) + b * a.ld_pre + m, z, vec, n);
-    if (a.act)
-        for (int e = 0; e < 4; ++e)
-            z[e] = act_value(z[e], a.act);
-    if (a.residual)
-        z += read4(static_cast<const T*>(a.residual) + b * a.ld_residual + m, vec, n);
-    write4(static_cast<T*>(a.y) + b * a.ld_y + m, z, vec, n);
+        write_w<T, W>(static_cast<T*>(a.pre) + b * a.ld_pre + m, z, vec, n);
+    act_values<W>(z, a.act);
+    if (a.residual) {
+        float r[W];
+        read_w<T, W>(static_cast<const T*>(a.residual) + b * a.ld_residual + m, r, vec, n);
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+            z[e] += r[e];
+    }
+    write_w<T, W>(static_cast<T*>(a.y) + y_at + b * a.ld_y + m, z, vec, n);
 }
 
-// Outputs m .. m + 3 of row b from their sums; m is a multiple of 4.
-__device__ inline void fused_store(const FusedArgs& a, int m, int b, f32x4 sum)
-{
-    if (b >= a.B || m >= a.n_out)
-        return;
-    const int n = min(4, a.n_out - m);
-    const bool vec = a.vec_out && n == 4;
-    f32x4 z = sum;
-    if (a.scale)
-        z *= *reinterpret_cast<const f32x4*>(a.scale + m);
-    if (a.bias)
-        for (int e = 0; e < 4; ++e)
-            z[e] += e < n ? a.bias[m + e] : 0.0f;
-    switch (a.y_type) {
-    case SPIKE_TYPE_F32: return put_outputs<float>(a, m, b, z, vec, n);
-    case SPIKE_TYPE_BF16: return put_outputs<bf16>(a, m, b, z, vec, n);
-    default: return put_outputs<f16>(a, m, b, z, vec, n);
+// Outputs m .. m + W - 1, a multiple of W: their scales and biases, read once
+// for all rows that a lane stores.
+template <int W>
+struct OutputColumns {
+    int m, n;      // n of them exist
+    bool vec;
+    float scale[W], bias[W];
+
+    __device__ inline void load(const FusedArgs& a, int m_)
+    {
+        m = m_, n = min(W, a.n_out - m_), vec = a.vec_out && n == W;
+        const int last = a.n_out - 1;
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            scale[e] = a.scale ? a.scale[min(m + e, last)] : 1.0f;
+            bias[e] = a.bias ? a.bias[min(m + e, last)] : 0.0f;
+        }
     }
-}
+
+    // y_at: elements from y's start to the rows
+    __device__ inline void store(const FusedArgs& a, int64_t b, float (&z)[W], int64_t y_at = 0) const
+    {
+        if (b >= a.B || n <= 0)
+            return;
+        if (a.scale) {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                z[e] *= scale[e];
+        }
+        if (a.bias) {
+#pragma unroll
+            for (int e = 0; e < W; ++e)
+                z[e] += bias[e];
+        }
+        switch (a.y_type) {
+        case SPIKE_TYPE_F32: return put_outputs<float, W>(a, m, b, z, vec, n, y_at);
+        case SPIKE_TYPE_BF16: return put_outputs<bf16, W>(a, m, b, z, vec, n, y_at);
+        default: return put_outputs<f16, W>(a, m, b, z, vec, n, y_at);
+        }
+    }
+};
 
 // --- few rows --------------------------------------------------------------
 
@@ -291,201 +401,387 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     constexpr int U = MT * NB >= 4 ? 1 : MT * NB >= 2 ? 2 : 4;  // steps in flight
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, c = lane % 16;
-    const int tile0 = blockIdx.x * MT, b0 = blockIdx.y * 16 * NB;
+    const int tile0 = blockIdx.x * MT;
+    const int64_t b0 = (int64_t)blockIdx.y * 16 * NB;
     const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
-    f32x4 acc[MT][NB] = {};
+    const XT* const x0 = static_cast<const XT*>(a.x) + b0 * a.ld_x;
+    const __amdgpu_buffer_rsrc_t xr = rows_resource(x0), wr = weight_resource(a.P, kBufMaxBytes);
+    static_assert(MT * NB <= WK, "a wave joins one tile's sums");
+    // the waves that join sums ask for their columns first: these are back when the sums are
+    OutputColumns<4> columns;
+    if (w < MT * NB)
+        columns.load(a, (tile0 + w / NB) * 16 + 4 * g);
+    f32x4 acc[MT][NB];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+            acc[t][n] = f32x4{};
     for (int s0 = w; s0 < a.steps; s0 += WK * U) {
         u32x4 wt[U][MT];
         Raw<XT> x[U][NB][2];
+#pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + u * WK;
-            const bool live = s < a.steps;
+#pragma unroll
             for (int t = 0; t < MT; ++t) {
-                wt[u][t] = u32x4{};
-                if (live && tile0 + t < tiles)
-                    wt[u][t] = *reinterpret_cast<const u32x4*>(a.P + (((int64_t)(tile0 + t) * a.steps + s) * 64 + lane) * 16);
+                // (the vector offset is the one that the range check sees first)
+                const bool live = s < a.steps && tile0 + t < tiles;
+                const uint32_t piece = live ? ((uint32_t)(tile0 + t) * a.steps + s) * 1024u : 0u;
+                wt[u][t] = __builtin_bit_cast(
+                    u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, piece, 0));
             }
-            for (int t = 0; t < NB; ++t)
-                for (int h = 0; h < 2; ++h) {
-                    x[u][t][h] = Raw<XT>{};
-                    const int b = b0 + 16 * t + c;
-                    if (live && b < a.B)
-                        x[u][t][h] = load_raw<XT, VECX>(static_cast<const XT*>(a.x) + b * a.ld_x, s * kFusedStep + 32 * h + 8 * g,
-                                                        a.n_in);
-                }
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                const int b = 16 * n + c;
+                const bool live = b0 + b < a.B && s < a.steps;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    x[u][n][h] = load_raw<XT, VECX>(x0, xr, min((int64_t)b, a.B - 1 - b0) * a.ld_x,
+                                                    live ? s * kFusedStep + 32 * h + 8 * g : a.n_in, a.n_in);
+            }
         }
-        for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (s0 + u * WK >= a.steps)
+                break;
+#pragma unroll
             for (int h = 0; h < 2; ++h) {
                 u32x4 wo[MT];
+#pragma unroll
                 for (int t = 0; t < MT; ++t)
                     wo[t] = widen_codes<OT>(wt[u][t][2 * h], wt[u][t][2 * h + 1]);
+#pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     u32x4 part[NS];
                     split_raw<XT, NS>(x[u][n][h], part);
+#pragma unroll
                     for (int p = 0; p < NS; ++p)
+#pragma unroll
                         for (int t = 0; t < MT; ++t)
                             acc[t][n] = mfma16<OT>(wo[t], part[p], acc[t][n]);
                 }
             }
+        }
     }
-    __shared__ f32x4 s_sum[WK > 1 ? WK : 1][MT * NB][64];
+    __shared__ f32x4 s_sum[WK][MT * NB][64];
+#pragma unroll
     for (int t = 0; t < MT; ++t)
+#pragma unroll
         for (int n = 0; n < NB; ++n)
             s_sum[w][t * NB + n][lane] = acc[t][n];
     __syncthreads();
-    for (int q = w; q < MT * NB; q += WK) {
-        f32x4 sum = s_sum[0][q][lane];
-        for (int v = 1; v < WK; ++v)
-            sum += s_sum[v][q][lane];
-        fused_store(a, (tile0 + q / NB) * 16 + 4 * g, b0 + q % NB * 16 + c, sum);
-    }
+    if (w >= MT * NB)
+        return;
+    f32x4 sum = s_sum[0][w][lane];
+#pragma unroll
+    for (int v = 1; v < WK; ++v)
+        sum += s_sum[v][w][lane];
+    float z[4] = {sum[0], sum[1], sum[2], sum[3]};
+    columns.store(a, b0 + w % NB * 16 + c, z);
 }
 
 // --- many rows -------------------------------------------------------------
 
-// 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  Each step
-// of 64 inputs: weights straight from their layout to registers, one step
-// ahead; activations through registers to LDS, two steps ahead, their parts
-// made on the way.  A row of the LDS tile is 8 chunks of 16 bytes; chunk c of
-// row r lies at c ^ (r % 8), so that the 16 rows of an operand read fall into
-// different banks.
-template <typename XT, int NS, int MT, int NT, int WM, int WN, bool VECX>
-__global__ __launch_bounds__(64 * WM * WN) void k_fused_tile(FusedArgs a)
+// 16 bytes per lane from `off` of the resource (plus `at`) to LDS at `to` + 16 lane,
+// without a register in between; past the resource: zeros.  The compiler does not
+// see the write: the caller waits.
+__device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint32_t at, uint32_t to)
 {
-    typedef typename Operand<XT>::type OT;
+    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, %3 offen lds" ::"v"(off), "s"(rsrc),
+                 "s"(__builtin_amdgcn_readfirstlane(to)), "s"(__builtin_amdgcn_readfirstlane(at))
+                 : "memory");
+}
+
+// All but the wave's N newest loads have landed.
+template <int N>
+__device__ inline void wait_loads()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ inline uint32_t lds_address(const void* p)
+{
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
+template <int NS, int MT, int NT, int WM, int WN>
+constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * MT * 1024; }
+
+template <int NS, int MT, int NT, int WM, int WN, int D>
+constexpr int fused_tile_lds()
+{
+    constexpr int ring = D * fused_stage_bytes<NS, MT, NT, WM, WN>(), turning = WM * WN * 2 * 16 * 16 * MT * 4;
+    return ring > turning ? ring : turning;
+}
+
+// 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
+// activations are NS planes of 16-bit parts (BF16 or F16 rows as they are, or
+// FP32 ones cut in three), rows of ld_x elements at 16-byte boundaries, n_in a
+// multiple of 8.  A ring of D stages in LDS holds 64 inputs of the rows and, for
+// each wave, of its weights; a stage is fetched D - 1 steps ahead by loads that
+// need no registers.  A row of a stage is 8 chunks of 16 bytes; chunk c of row r
+// lies at c ^ (r % 8) (the lanes' global chunks are exchanged), so that an
+// operand read's rows fall into different banks.  At the end each wave turns its
+// sums around in LDS, 32 rows at a time, so that they leave as whole vectors of
+// neighbouring outputs.
+template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
+{
     constexpr int kThreads = 64 * WM * WN, kRows = 16 * NT * WN;
-    constexpr int kChunks = kRows * 8 / kThreads;
-    static_assert(kChunks >= 1 && kRows * 8 % kThreads == 0, "every thread stages whole chunks");
-    __shared__ u32x4 s_x[2][NS][kRows * 8];
+    constexpr int kChunks = kRows * 8 / kThreads;  // 16-byte chunks of a plane that a thread fetches per step
+    constexpr int kStage = fused_stage_bytes<NS, MT, NT, WM, WN>();
+    constexpr int kLoads = NS * kChunks + MT;      // of a wave and step
+    static_assert(kChunks >= 1 && kRows * 8 % kThreads == 0, "every thread fetches whole chunks");
+    static_assert(NT % 2 == 0, "sums are turned around in pairs of row tiles");
+    static_assert((D - 2) * kLoads < 64, "the load counter holds what is in flight");
+    extern __shared__ u32x4 s_fused[];
     // Neighbouring workgroups of one XCD (every eighth) take tiles of a group
     // of 8 output tiles, so that they share both operands in its L2.
-    const int total = a.out_tiles * a.row_tiles, per_xcd = (total + 7) / 8;
-    const int id = (int)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-    if ((int)(blockIdx.x / 8) >= per_xcd || id >= total)
+    const int plane_tiles = a.out_tiles * a.row_tiles, total = plane_tiles * a.splits, per_xcd = (total + 7) / 8;
+    const int place = (int)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if ((int)(blockIdx.x / 8) >= per_xcd || place >= total)
         return;
+    const int split = place / plane_tiles, id = place % plane_tiles;
     const int group = id / (8 * a.row_tiles), in_group = min(8, a.out_tiles - group * 8);
     const int out_tile = group * 8 + id % (8 * a.row_tiles) % in_group;
     const int row_tile = id % (8 * a.row_tiles) / in_group;
+    const int first = split * a.split_steps, steps = min(a.split_steps, a.steps - first);
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, c = lane % 16;
     const int wm = w % WM, wn = w / WM;
     const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
-    const int tile0 = (out_tile * WM + wm) * MT, b0 = row_tile * kRows;
+    const int tile0 = (out_tile * WM + wm) * MT;
+    const int64_t b0 = (int64_t)row_tile * kRows;
 
-    const u32x4* wp[MT];
+    const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes);
+    uint32_t w_at[MT];
+#pragma unroll
     for (int t = 0; t < MT; ++t)  // tiles past the outputs repeat the last one; their results are not stored
-        wp[t] = reinterpret_cast<const u32x4*>(a.P) + (int64_t)min(tile0 + t, tiles - 1) * a.steps * 64 + lane;
-    const XT* xp[kChunks];
+        w_at[t] = ((uint32_t)min(tile0 + t, tiles - 1) * a.steps + first) * 1024u;
+    __amdgpu_buffer_rsrc_t xr[NS];
+#pragma unroll
+    for (int p = 0; p < NS; ++p)
+        xr[p] = rows_resource(static_cast<const uint16_t*>(a.x) + p * a.plane + b0 * a.ld_x);
+    const int chunk = threadIdx.x % 8 ^ threadIdx.x / 8 % 8;
+    uint32_t x_off[kChunks];  // bytes, of this thread's chunk of step 0
+#pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const int r = i * (kThreads / 8) + threadIdx.x / 8;
-        xp[i] = static_cast<const XT*>(a.x) + (int64_t)min(b0 + r, a.B - 1) * a.ld_x;
+        const int64_t r = min((int64_t)(i * (kThreads / 8) + threadIdx.x / 8), a.B - 1 - b0);
+        x_off[i] = (uint32_t)(r * a.ld_x + first * kFusedStep + 8 * chunk) * 2u;
     }
-    const int chunk = threadIdx.x % 8;
-    u32x4 wt[MT];
-    Raw<XT> raw[kChunks];
-    auto load_w = [&](int s) {
+    const uint32_t lds = lds_address(s_fused);
+    constexpr int kWeights = NS * kRows * 128;  // of a stage: where the waves' weights begin
+    // Step s of this workgroup's to stage `buf`; past the last, and past a row's end, zeros.
+    auto fetch = [&](int buf, int s) __attribute__((always_inline)) {
+        const bool live = s < steps && (first + s) * kFusedStep + 8 * chunk < a.n_in;
+        const uint32_t at = s < steps ? s : 0, to = lds + buf * kStage;
+#pragma unroll
+        for (int p = 0; p < NS; ++p)
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i)
+                load_to_lds(xr[p], live ? x_off[i] : kOutOfRange, at * 128u,
+                            to + (p * kRows + i * (kThreads / 8) + w * 8) * 128);
+#pragma unroll
         for (int t = 0; t < MT; ++t)
-            wt[t] = wp[t][s * 64];
+            load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + at * 1024u,
+                        to + kWeights + (w * MT + t) * 1024);
     };
-    auto load_x = [&](int s) {
-        for (int i = 0; i < kChunks; ++i)
-            raw[i] = load_raw<XT, VECX>(xp[i], s * kFusedStep + 8 * chunk, a.n_in);
-    };
-    auto stage = [&](int buf) {
-        for (int i = 0; i < kChunks; ++i) {
-            const int r = i * (kThreads / 8) + threadIdx.x / 8;
-            u32x4 part[NS];
-            split_raw<XT, NS>(raw[i], part);
-            for (int p = 0; p < NS; ++p)
-                s_x[buf][p][r * 8 + (chunk ^ (r % 8))] = part[p];
-        }
-    };
-    f32x4 acc[MT][NT] = {};
-    load_x(0);
-    load_w(0);
-    stage(0);
-    if (a.steps > 1)
-        load_x(1);
+    f32x4 acc[MT][NT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            acc[t][n] = f32x4{};
+    u32x4 wt[MT], wo[2][MT];  // a step's codes; the operands of its two halves
+    const u32x4* const s_w = s_fused + kWeights / 16 + w * MT * 64 + lane;
+#pragma unroll
+    for (int s = 0; s < D - 1; ++s)
+        fetch(s, s);
+    wait_loads<(D - 2) * kLoads>();
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        wt[t] = s_w[t * 64];
+        wo[0][t] = widen_codes<OT>(wt[t][0], wt[t][1]);
+    }
     __syncthreads();
-    for (int s = 0; s < a.steps; ++s) {
-        u32x4 wo[2][MT];
-        for (int h = 0; h < 2; ++h)
-            for (int t = 0; t < MT; ++t)
-                wo[h][t] = widen_codes<OT>(wt[t][2 * h], wt[t][2 * h + 1]);
-        if (s + 1 < a.steps)
-            load_w(s + 1);
-        for (int h = 0; h < 2; ++h)
-            for (int n = 0; n < NT; ++n)
-                for (int p = 0; p < NS; ++p) {
-                    const int r = (wn * NT + n) * 16 + c;
-                    const u32x4 xo = s_x[s % 2][p][r * 8 + ((4 * h + g) ^ (r % 8))];
-                    for (int t = 0; t < MT; ++t)
-                        acc[t][n] = mfma16<OT>(wo[h][t], xo, acc[t][n]);
+    // One step, in items of one operand of activations times MT of weights.  While an
+    // item's products run, part of the next half's weights is widened and the
+    // operand two items ahead is read.  A wave issues in order, so only work between
+    // two products runs beside them: the order is pinned.
+    constexpr int kHalf = NT * NS, kItems = 2 * kHalf;
+    int cur = 0;
+    for (int s = 0; s < steps; ++s) {
+        const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
+        const u32x4* const s_x = s_fused + cur * (kStage / 16) + (wn * NT * 16 + c) * 8;
+        const int c0 = g ^ (c % 8), c1 = (4 + g) ^ (c % 8);
+        u32x4 xo[3];
+        auto read = [&](int item) __attribute__((always_inline)) {
+            const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
+            return s_x[p * kRows * 8 + n * 128 + (h == 0 ? c0 : c1)];
+        };
+        xo[0] = read(0);
+        xo[1] = read(1);
+        fetch(last, s + D - 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int item = 0; item < kItems; ++item) {
+            const int h = item / kHalf, in_half = item % kHalf;
+            if (item + 2 < kItems)
+                xo[(item + 2) % 3] = read(item + 2);
+            if (item == kHalf) {
+                // this wave's part of the next stage is there: its weights are its own
+                wait_loads<(D - 2) * kLoads>();
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    wt[t] = s_w[next * (kStage / 16) + t * 64];
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                acc[t][in_half / NS] = mfma16<OT>(wo[h][t], xo[item % 3], acc[t][in_half / NS]);
+                // a share of the 4 MT registers of the next half (of the next step, one item late: its codes are on their way)
+#pragma unroll
+                for (int v = 0; v < 4 * MT; ++v) {
+                    const int slot = h == 0 ? v * kHalf / 4 : MT + v * (kHalf - 1) / 4;
+                    if (slot == in_half * MT + t)
+                        wo[1 - h][v / 4][v % 4] = widen_pair<OT>(wt[v / 4][(h == 0 ? 2 : 0) + v % 4 / 2], v % 2);
                 }
-        if (s + 1 < a.steps)
-            stage((s + 1) % 2);
-        if (s + 2 < a.steps)
-            load_x(s + 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        cur = next;
         __syncthreads();
     }
-    for (int n = 0; n < NT; ++n)
-        for (int t = 0; t < MT; ++t)
-            fused_store(a, (tile0 + t) * 16 + 4 * g, b0 + (wn * NT + n) * 16 + c, acc[t][n]);
+    // the zeros fetched past the last step have landed everywhere before LDS is used anew
+    wait_loads<0>();
+    __syncthreads();
+    // 32 rows x 16 MT outputs at a time, in this wave's own part of LDS; the
+    // 16-byte chunk q of row r lies at q ^ (r % (4 MT))
+    f32x4* const s_out = reinterpret_cast<f32x4*>(s_fused) + w * 2 * 16 * 4 * MT;
+    constexpr int kVecs = 2 * MT;  // of 8 outputs, in a row
+    static_assert(64 % kVecs == 0, "a lane keeps its outputs");
+    const int q = lane % kVecs * 2;
+    OutputColumns<8> columns;
+    columns.load(a, tile0 * 16 + 4 * q);
+    const int64_t y_at = split * a.split_stride;
+#pragma unroll
+    for (int n0 = 0; n0 < NT; n0 += 2) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] = acc[t][n0 + n];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
+            const f32x4 lo = s_out[r * 4 * MT + (q ^ (r % 16 % (4 * MT)))];
+            const f32x4 hi = s_out[r * 4 * MT + ((q + 1) ^ (r % 16 % (4 * MT)))];
+            float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            columns.store(a, b0 + (wn * NT + n0) * 16 + r, z, y_at);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Joins the sums of a product whose steps were split: 8 outputs per thread, the
+// parts in ascending order, then the epilogue.  part: [splits][B] rows of ld elements.
+__global__ __launch_bounds__(256) void k_fused_join(FusedArgs a, const float* __restrict__ part, int64_t ld)
+{
+    const int64_t groups = ld / 8, stride = ld * a.B;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups * a.B; i += (int64_t)gridDim.x * 256) {
+        const int64_t b = i / groups;
+        const int m = (int)(i % groups) * 8;
+        f32x8 sum = load8(part + b * ld + m);
+        for (int p = 1; p < a.splits; ++p)
+            sum += load8(part + p * stride + b * ld + m);
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            z[e] = sum[e];
+        OutputColumns<8> columns;
+        columns.load(a, m);
+        columns.store(a, b, z);
+    }
+}
+
+// Cuts rows of n elements of any type and alignment into NS planes for the
+// product: rows of `ld` (n rounded up to 8) elements, zeros past n.
+template <typename XT, int NS>
+__global__ __launch_bounds__(256) void k_fused_cut(const XT* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
+                                                   int64_t plane, uint16_t* __restrict__ out, int vec)
+{
+    const int64_t groups = ld / 8;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups * B; i += (int64_t)gridDim.x * 256) {
+        const int64_t b = i / groups;
+        const int k = (int)(i % groups) * 8;
+        const XT* p = x + b * ld_x + k;
+        if constexpr (NS == 1) {  // 16-bit rows as they are
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+            uint32_t r[4];
+            for (int e = 0; e < 4; ++e)
+                r[e] = (k + 2 * e < n ? h[2 * e] : 0u) | (k + 2 * e + 1 < n ? (uint32_t)h[2 * e + 1] << 16 : 0u);
+            *reinterpret_cast<u32x4*>(out + b * ld + k) = u32x4{r[0], r[1], r[2], r[3]};
+        } else {
+            float v[8];
+            read_w<XT, 8>(p, v, vec && k + 8 <= n, n - k);
+            put_planes<NS>(out + b * ld + k, plane, v);
+        }
+    }
 }
 
 // --- gradient --------------------------------------------------------------
 
 // g = dy act'(z): per workgroup 256 outputs and `rows` rows.  g * scale goes to
-// gs (rows of ld_gs elements) for the product, and the column sums of g over
-// these rows to partial[row block].  Bound by memory.
+// gs for the product, in NS planes of rows of ld_gs elements (NS = 0: FP32 rows),
+// and the column sums of g over these rows to partial[row block].  Bound by memory.
 constexpr int kGateCols = 256;
 
-template <typename T, typename TG, bool VEC>
+template <typename T, int NS, bool VEC>
 __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ pre,
                                                     int64_t ld_pre, int act, int B, int M, int rows,
-                                                    const float* __restrict__ scale, TG* __restrict__ gs, int64_t ld_gs,
-                                                    float* __restrict__ partial)
+                                                    const float* __restrict__ scale, uint16_t* __restrict__ gs,
+                                                    int64_t ld_gs, int64_t plane, float* __restrict__ partial)
 {
     const int m = blockIdx.x * kGateCols + threadIdx.x % 32 * 8;
     const int64_t b0 = (int64_t)blockIdx.y * rows, b1 = min((int64_t)B, b0 + rows);
-    const bool full = VEC && m + 8 <= M;
+    const int n = M - m;
+    const bool full = VEC && n >= 8;
     float sc[8], sum[8] = {};
+#pragma unroll
     for (int e = 0; e < 8; ++e)
-        sc[e] = m + e < M ? scale[m + e] : 0.0f;
-    if (m < M)
+        sc[e] = e < n ? scale[m + e] : 0.0f;
+    if (n > 0)
         for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
-            f32x8 g = {}, z = {};
-            if (full) {
-                g = load8(dy + b * ld_dy + m);
-                if (act)
-                    z = load8(pre + b * ld_pre + m);
-            } else {
-                for (int e = 0; e < 8; ++e)
-                    if (m + e < M) {
-                        g[e] = (float)dy[b * ld_dy + m + e];
-                        if (act)
-                            z[e] = (float)pre[b * ld_pre + m + e];
-                    }
-            }
-            f32x8 out;
+            float g[8], slope[8] = {};
+            read_w<T, 8>(dy + b * ld_dy + m, g, full, n);
+            if (act)
+                read_w<T, 8>(pre + b * ld_pre + m, slope, full, n);
+            act_slopes<8>(slope, act);
+#pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (act)
-                    g[e] *= act_slope(z[e], act);
+                g[e] *= slope[e];
                 sum[e] += g[e];
-                out[e] = g[e] * sc[e];
+                g[e] *= sc[e];
             }
-            if (gs)
-                store8(gs + b * ld_gs + m, out);  // rows of gs are padded to whole vectors
+            // rows are padded to whole vectors, with zeros
+            if constexpr (NS == 0) {
+                if (gs)
+                    write_w<float, 8>(reinterpret_cast<float*>(gs) + b * ld_gs + m, g, true, 8);
+            } else if (gs) {
+                put_planes<NS>(gs + b * ld_gs + m, plane, g);
+            }
         }
     if (!partial)
         return;
     __shared__ float s_sum[8][kGateCols];
+#pragma unroll
     for (int e = 0; e < 8; ++e)
         s_sum[threadIdx.x / 32][threadIdx.x % 32 * 8 + e] = sum[e];
     __syncthreads();
     const int col = blockIdx.x * kGateCols + threadIdx.x;
     if (col < M) {
         float v = s_sum[0][threadIdx.x];
+#pragma unroll
         for (int r = 1; r < 8; ++r)
             v += s_sum[r][threadIdx.x];
         partial[(int64_t)blockIdx.y * M + col] = v;

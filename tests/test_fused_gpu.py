@@ -20,6 +20,7 @@ import pytest
 import torch
 
 from oracle import step_oracle as so
+from tests.launches import kernels
 
 pytestmark = pytest.mark.gpu
 
@@ -346,4 +347,44 @@ def test_refusals(sp):
     with pytest.raises(sp.SpikeError, match="workspace"):
         sp.dense_fused_backward(h, y, dbias=torch.empty(24, device="cuda"),
                                 workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    h.close()
+
+
+@pytest.mark.parametrize("xk", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("K,B", [(72, 40), (72, 600), (8, 70), (136, 300), (1000, 513)])
+def test_nothing_is_left_from_the_call_before(sp, xk, K, B):
+    """A call whose inputs are all NaN, then one of integers whose last step is short: nothing of the first is in the second."""
+    p = problem(K, 520, B, integer=True)
+    h = handle(sp, p)
+    y = torch.empty((B, 520), device="cuda")
+    x = dev(p["x"], xk)
+    for n in (B, 2048):
+        sp.dense_fused_forward(h, torch.full((n, K), float("nan"), device="cuda", dtype=TYPES[xk]), torch.empty((n, 520), device="cuda"))
+    sp.dense_fused_forward(h, x, y)
+    torch.cuda.synchronize()
+    assert torch.equal(y.cpu(), torch.from_numpy(so.fused_pre(p["Q"], p["scale"], p["x"]).astype(np.float32)))
+    h.close()
+
+
+# one shape per kernel form: few rows with 1, 2 and 4 tiles of outputs (and two of
+# rows), every tile shape, products split over workgroups, cut activations or not
+FORMS = [("k_fused_rows", 100, 4000, 9), ("k_fused_rows", 72, 33000, 16), ("k_fused_rows", 72, 33000, 20),
+         ("k_fused_tile", 1000, 520, 40), ("k_fused_tile", 328, 1000, 700), ("k_fused_tile", 264, 2100, 1300),
+         ("k_fused_tile", 136, 4100, 2600), ("k_fused_join", 6000, 130, 50), ("k_fused_join", 4104, 520, 200)]
+
+
+@pytest.mark.parametrize("kernel,K,M,B", FORMS)
+@pytest.mark.parametrize("xk,yk", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+def test_every_form(sp, kernel, K, M, B, xk, yk):
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p)
+    x, y = dev(p["x"], xk), torch.empty((B, M), device="cuda")
+    ws = torch.empty(max(1, sp.dense_fused_forward_workspace_bytes(h, x)), dtype=torch.uint8, device="cuda")
+    used = kernels(lambda st: sp.dense_fused_forward(h, x, y, workspace=ws, stream=st))
+    assert any(k.startswith(kernel) for k in used), used
+    assert ("k_fused_cut" in [k.split("<")[0] for k in used]) == (B > 32 and (xk == "f32" or K % 8 != 0))
+    for pad, offset in ((0, 0), (1, 1)):
+        (x, y, z), want, want_z = forward(sp, h, p, xk, yk, act="relu", pre=True, pad=pad, offset=offset)
+        assert torch.equal(y.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[yk])), used
+        assert torch.equal(z.cpu(), torch.from_numpy(want_z.astype(np.float32)).to(TYPES[yk])), used
     h.close()

@@ -23,7 +23,7 @@ def test_fused(sp):
         assert out.value is None and sp.spike_proj_last_error()
     assert create(K=1 << 16, M=1 << 15) == sp.SPIKE_EUNSUPPORTED
     assert lib.dense_fused_destroy(None) == sp.SPIKE_OK
-    assert lib.dense_fused_forward(None, D, 0, 64, 1, None, 0, None, 0, D, 0, 32, None, 0, None) == sp.SPIKE_EINVAL
+    assert lib.dense_fused_forward(None, D, 0, 64, 1, None, 0, None, 0, D, 0, 32, None, 0, None, 0, None) == sp.SPIKE_EINVAL
     assert "handle" in sp.spike_proj_last_error()
     assert lib.dense_fused_backward(None, D, 0, 32, None, 0, 0, 1, D, 0, 64, D, D, 1 << 20, None) == sp.SPIKE_EINVAL
     assert lib.dense_fused_workspace_bytes(None, 4, 0) == -1
