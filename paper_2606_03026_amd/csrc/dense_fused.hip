@@ -242,8 +242,8 @@ void cut_rows(FusedArgs& a, void* workspace, hipStream_t st)
     a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld;
 }
 
-// Rows of a workgroup of the gate, and the parts the bias gradient comes in: at most 32.
-int gate_rows(int32_t B) { return (int)std::max<int64_t>(16, ((int64_t)B + 31) / 32); }
+// Rows of a workgroup of the gate, and the parts the bias gradient comes in.
+int gate_rows(int32_t B) { return (int)std::max<int64_t>(16, ((int64_t)B + spk::kGateParts - 1) / spk::kGateParts); }
 int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 
 // What g * scale is kept in between the gate and the product: planes, or FP32

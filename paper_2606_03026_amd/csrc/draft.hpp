@@ -1,7 +1,9 @@
 // Verification of drafted tokens (C ABI in include/head_draft.h): a pass over
 // every row of logits for its largest value and the sum of its exponentials,
 // in parts of a row, then one workgroup per part of a sequence's decisive row
-// decides on the drafts and races the residual.
+// decides on the drafts and races the residual.  The first is bound by memory
+// where rows are many, by latency where they are few; the second by a chain of
+// dependent loads, which it keeps short.
 #pragma once
 
 #include <math.h>
@@ -22,12 +24,12 @@ struct DraftPart {
     float sum;
 };
 
-// Per sequence, for the race: the best r(v) / noise(v) and p(v) / noise(v) as
-// (value bits << 32 | ~v), so that the largest code is the largest value at
-// the lowest index; 0: none.  `done` counts the workgroups that have added theirs.
+// Per sequence, for the race: the best r(v) / noise(v), or where there is none the
+// best p(v) / noise(v), as a code that is larger the better the value and, of equal
+// values, the lower v; 0: none.  `done` counts the workgroups that have added theirs.
 struct DraftBest {
-    unsigned long long r, p;
-    unsigned int done, pad[3];
+    unsigned long long code;
+    unsigned int done, pad;
 };
 
 struct DraftArgs {
@@ -47,17 +49,18 @@ struct DraftArgs {
     DraftBest* best;  // [S]
 };
 
-__device__ inline float draft_nan_low(float x) { return x == x ? x : -INFINITY; }
+__device__ inline float draft_nan_low(float x) { return fmaxf(x, -INFINITY); }  // (the maximum leaves a NaN out)
 
-// Whether the temperature takes the largest logit alone, and 1 / T: at least
+// Whether the temperature takes the largest logit alone, and log2(e) / T: at least
 // the smallest normal number, so that an infinite difference stays infinite.
 __device__ inline bool draft_greedy(float t) { return !(t > 0.0f); }
-__device__ inline float draft_inverse(float t) { return draft_greedy(t) ? 1.0f : fmaxf(1.0f / t, 1.17549435e-38f); }
+__device__ inline float draft_rate(float t) { return draft_greedy(t) ? 1.0f : fmaxf(1.44269504f / t, 1.17549435e-38f); }
 
-// exp((x - top) / T): exactly 1 at the top (an infinite one too), 0 for -inf.
-__device__ inline float draft_term(float x, float top, float inv_t)
+// exp((x - top) / T): exactly 1 at the top (an infinite one too: the minimum leaves
+// the difference's NaN out), 0 for -inf.
+__device__ inline float draft_term(float x, float top, float rate)
 {
-    return x == top ? 1.0f : expf((x - top) * inv_t);
+    return __builtin_amdgcn_exp2f(fminf((x - top) * rate, 0.0f));
 }
 
 __device__ inline int draft_count(const DraftArgs& a, int s)
@@ -73,14 +76,40 @@ __device__ inline const T* draft_row(const DraftArgs& a, int s, int row)
                       : static_cast<const T*>(a.draft) + ((int64_t)s * a.G + row - a.G - 1) * a.ld_draft;
 }
 
-__device__ inline void draft_join(DraftPart& a, const DraftPart& b, float inv_t)
+// The largest value over a wave, and the sum over it.
+__device__ inline float draft_wave_max(float v)
 {
-    const bool b_wins = b.top > a.top || (b.top == a.top && b.at < a.at);
-    const float top = b_wins ? b.top : a.top;
-    const float sum = top == -INFINITY ? 0.0f
-                                       : a.sum * (a.top == -INFINITY ? 0.0f : draft_term(a.top, top, inv_t)) +
-                                             b.sum * (b.top == -INFINITY ? 0.0f : draft_term(b.top, top, inv_t));
-    a = DraftPart{top, b_wins ? b.at : a.at, sum};
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2)
+        v = fmaxf(v, __shfl_xor(v, m));
+    return v;
+}
+
+__device__ inline float draft_wave_sum(float v)
+{
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2)
+        v += __shfl_xor(v, m);
+    return v;
+}
+
+// Joins one part per lane: every lane gets the whole.  Only a greedy row needs `at`,
+// only the others their sum.
+__device__ inline DraftPart draft_join(const DraftPart& mine, bool greedy, float rate)
+{
+    DraftPart all;
+    all.top = draft_wave_max(mine.top);
+    all.at = 0x7fffffff;
+    all.sum = 0.0f;
+    if (greedy) {
+        all.at = mine.top == all.top ? mine.at : 0x7fffffff;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2)
+            all.at = min(all.at, __shfl_xor(all.at, m));
+    } else {
+        all.sum = draft_wave_sum(mine.top == -INFINITY ? 0.0f : mine.sum * draft_term(mine.top, all.top, rate));
+    }
+    return all;
 }
 
 template <typename T, int VEC>
@@ -88,16 +117,20 @@ __device__ inline void draft_load(const T* row, int i, int end, float (&x)[8])
 {
     if (VEC == 8 && i + 8 <= end) {
         const f32x8 v = load8(row + i);
+#pragma unroll
         for (int e = 0; e < 8; ++e)
             x[e] = draft_nan_low(v[e]);
     } else {
+#pragma unroll
         for (int e = 0; e < 8; ++e)
             x[e] = i + e < end ? draft_nan_low((float)row[i + e]) : -INFINITY;
     }
 }
 
-// One workgroup per (part, row, sequence).
-template <typename T, int VEC>
+// One workgroup per (part, row, sequence).  A thread takes 8 logits of each of
+// ROUNDS stretches of 2,048 at a time, all loads in flight, then the largest of
+// them, then their exponentials: one exponential per logit.
+template <typename T, int VEC, int ROUNDS>
 __global__ __launch_bounds__(kDraftBlock) void k_draft_stats(DraftArgs a)
 {
     const int part = blockIdx.x % a.parts, row = blockIdx.x / a.parts % a.rows, s = blockIdx.x / a.parts / a.rows;
@@ -109,35 +142,52 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_stats(DraftArgs a)
     const T* x = draft_row<T>(a, s, row);
     const float temp = a.temperature ? a.temperature[s] : 1.0f;
     const bool greedy = draft_greedy(temp);
-    const float inv_t = draft_inverse(temp);
-    const int i0 = part * a.part_len, i1 = min(a.V, i0 + a.part_len);
-    DraftPart me{-INFINITY, a.V, 0.0f};
-    for (int i = i0 + (int)threadIdx.x * 8; i < i1; i += kDraftBlock * 8) {
-        float v[8];
-        draft_load<T, VEC>(x, i, i1, v);
-        float top = v[0];
-        int at = 0;
-        for (int e = 1; e < 8; ++e)
-            if (v[e] > top)
-                top = v[e], at = e;
+    const float rate = draft_rate(temp);
+    const int i1 = min(a.V, (part + 1) * a.part_len);
+    DraftPart me{-INFINITY, 0x7fffffff, 0.0f};
+    for (int i = part * a.part_len + (int)threadIdx.x * 8; i < i1; i += ROUNDS * kDraftBlock * 8) {
+        float v[ROUNDS][8];
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+            draft_load<T, VEC>(x, i + r * kDraftBlock * 8, i1, v[r]);
+        float top = me.top;
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                top = fmaxf(top, v[r][e]);
         if (top == -INFINITY)
             continue;
-        float sum = 0.0f;
-        if (!greedy)
+        if (greedy) {
+            if (top > me.top) {
+                int at = 0x7fffffff;
+#pragma unroll
+                for (int r = ROUNDS - 1; r >= 0; --r)
+#pragma unroll
+                    for (int e = 7; e >= 0; --e)
+                        at = v[r][e] == top ? i + r * kDraftBlock * 8 + e : at;
+                me.top = top, me.at = at;
+            }
+            continue;
+        }
+        float sum = me.top == -INFINITY ? 0.0f : me.sum * draft_term(me.top, top, rate);
+#pragma unroll
+        for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
             for (int e = 0; e < 8; ++e)
-                sum += draft_term(v[e], top, inv_t);
-        draft_join(me, DraftPart{top, i + at, sum}, inv_t);
+                sum += draft_term(v[r][e], top, rate);
+        me.top = top, me.sum = sum;
     }
     __shared__ DraftPart s_part[kDraftBlock / 64];
-    for (int m = 1; m < 64; m *= 2)
-        draft_join(me, DraftPart{__shfl_xor(me.top, m), __shfl_xor(me.at, m), __shfl_xor(me.sum, m)}, inv_t);
+    me = draft_join(me, greedy, rate);
     if (threadIdx.x % 64 == 0)
         s_part[threadIdx.x / 64] = me;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kDraftBlock / 64; ++w)
-            draft_join(me, s_part[w], inv_t);
-        a.part[((int64_t)s * a.rows + row) * a.parts + part] = me;
+    if (threadIdx.x < 64) {
+        me = threadIdx.x < kDraftBlock / 64 ? s_part[threadIdx.x] : DraftPart{-INFINITY, 0x7fffffff, 0.0f};
+        me = draft_join(me, greedy, rate);
+        if (threadIdx.x == 0)
+            a.part[((int64_t)s * a.rows + row) * a.parts + part] = me;
     }
 }
 
@@ -147,16 +197,19 @@ struct DraftDist {
     int at;
 };
 
-__device__ inline float draft_prob(const DraftDist& d, float x, int v, bool hot, float inv_t)
+__device__ inline float draft_prob(const DraftDist& d, float x, int v, bool hot, float rate)
 {
     if (hot)
         return v == d.at ? 1.0f : 0.0f;
-    return x == -INFINITY || d.top == -INFINITY ? 0.0f : draft_term(x, d.top, inv_t) / d.sum;
+    return x == -INFINITY ? 0.0f : draft_term(x, d.top, rate) / d.sum;
 }
 
-__device__ inline unsigned long long draft_code(float score, int v)
+// r / noise wins over every p / noise; both are positive, so their bits are ordered as they are.
+__device__ inline unsigned long long draft_code(float score, int v, bool residual)
 {
-    return score > 0.0f ? (unsigned long long)__float_as_uint(score) << 32 | (uint32_t)~v : 0ull;
+    if (!(score > 0.0f))
+        return 0ull;
+    return (unsigned long long)(__float_as_uint(score) | (residual ? 0x80000000u : 0u)) << 32 | (uint32_t)~v;
 }
 
 // One workgroup per (part, sequence): each decides on the drafts, then races its part.
@@ -165,45 +218,62 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
 {
     const int part = blockIdx.x % a.race_parts, s = blockIdx.x / a.race_parts;
     const int n = draft_count(a, s);
+    const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
     const float temp = a.temperature ? a.temperature[s] : 1.0f;
     const bool greedy = draft_greedy(temp);
-    const float inv_t = draft_inverse(temp);
+    const float rate = draft_rate(temp);
     __shared__ DraftDist s_dist[kDraftMaxRows];
     __shared__ float s_p[kDraftMaxRows], s_q[kDraftMaxRows];
+    __shared__ int s_draft[kDraftMaxRows];
     __shared__ int s_taken;
-    // the rows' distributions, one wave per row, its parts along the lanes
-    for (int row = threadIdx.x / 64; row < a.rows; row += kDraftBlock / 64) {
-        if (row <= a.G ? row > n : row - a.G - 1 >= n)
-            continue;
-        const int lane = threadIdx.x % 64;
-        DraftPart me{-INFINITY, a.V, 0.0f};
-        if (lane < a.parts)
-            me = a.part[((int64_t)s * a.rows + row) * a.parts + lane];
-        for (int m = 1; m < 64; m *= 2)
-            draft_join(me, DraftPart{__shfl_xor(me.top, m), __shfl_xor(me.at, m), __shfl_xor(me.sum, m)}, inv_t);
-        if (lane == 0)
-            s_dist[row] = DraftDist{me.top, me.sum, me.top == -INFINITY ? -1 : me.at};
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < n) {
-        const int i = threadIdx.x;
-        const int d = a.drafts[(int64_t)s * a.G + i];
-        float p = 0.0f, q = 0.0f;
+    // draft i is thread i's: its logits are asked for before the rows' sums are joined
+    const int mine = threadIdx.x;
+    int d = -1;
+    float u = 0.0f, xt = -INFINITY, xd = -INFINITY;
+    if (mine < n) {
+        d = a.drafts[(int64_t)s * a.G + mine];
+        u = a.uniform[(int64_t)s * a.G + mine];
+        s_draft[mine] = d;
         if (d >= 0 && d < a.V) {
-            p = draft_prob(s_dist[i], draft_nan_low((float)draft_row<T>(a, s, i)[d]), d, greedy, inv_t);
-            q = a.draft ? draft_prob(s_dist[a.G + 1 + i], draft_nan_low((float)draft_row<T>(a, s, a.G + 1 + i)[d]), d,
-                                     greedy, inv_t)
-                        : 1.0f;
+            xt = (float)draft_row<T>(a, s, mine)[d];
+            if (a.draft)
+                xd = (float)draft_row<T>(a, s, a.G + 1 + mine)[d];
         }
-        s_p[i] = p;
-        s_q[i] = q;
+    }
+    // the rows' distributions: one wave per row, its parts along the lanes, four rows' loads at a time
+    for (int r0 = w; r0 < a.rows; r0 += 4 * (kDraftBlock / 64)) {
+        DraftPart me[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = r0 + k * (kDraftBlock / 64);
+            me[k] = DraftPart{-INFINITY, 0x7fffffff, 0.0f};
+            if (row < a.rows && (row <= a.G ? row <= n : row - a.G - 1 < n) && lane < a.parts)
+                me[k] = a.part[((int64_t)s * a.rows + row) * a.parts + lane];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = r0 + k * (kDraftBlock / 64);
+            if (row >= a.rows)
+                break;
+            const DraftPart all = draft_join(me[k], greedy, rate);
+            if (lane == 0)
+                s_dist[row] = DraftDist{all.top, all.sum, all.top == -INFINITY ? -1 : all.at};
+        }
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        int j = 0;
-        while (j < n && a.uniform[(int64_t)s * a.G + j] * s_q[j] < s_p[j])
-            ++j;
-        s_taken = j;
+    if (w == 0) {
+        float p = 0.0f, q = 0.0f;
+        if (mine < n && d >= 0 && d < a.V) {
+            p = draft_prob(s_dist[mine], draft_nan_low(xt), d, greedy, rate);
+            q = a.draft ? draft_prob(s_dist[a.G + 1 + mine], draft_nan_low(xd), d, greedy, rate) : 1.0f;
+        }
+        if (mine < n) {
+            s_p[mine] = p;
+            s_q[mine] = q;
+        }
+        const unsigned long long refused = __ballot(mine < n && !(u * q < p));
+        if (lane == 0)
+            s_taken = refused ? __builtin_ctzll(refused) : n;
     }
     __syncthreads();
     const int j = s_taken;
@@ -211,66 +281,75 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
     const bool minus = j < n;  // a draft was refused: its distribution is taken off
     const T* draft = minus && a.draft ? draft_row<T>(a, s, a.G + 1 + j) : nullptr;
     const DraftDist dp = s_dist[j];
-    const DraftDist dq = !minus ? DraftDist{} : draft ? s_dist[a.G + 1 + j] : DraftDist{0.0f, 0.0f, a.drafts[(int64_t)s * a.G + j]};
+    const DraftDist dq = !minus ? DraftDist{0.0f, 1.0f, -1} : draft ? s_dist[a.G + 1 + j] : DraftDist{0.0f, 1.0f, s_draft[j]};
     const bool hot_q = greedy || !draft;
     const float* noise = a.noise + (int64_t)s * a.ld_noise;
-    unsigned long long best_r = 0, best_p = 0;
-    const int i0 = part * a.race_len, i1 = min(a.V, i0 + a.race_len);
-    for (int i = i0 + (int)threadIdx.x * 8; i < i1; i += kDraftBlock * 8) {
+    unsigned long long best = 0;
+    const int i1 = min(a.V, (part + 1) * a.race_len);
+    for (int i = part * a.race_len + (int)threadIdx.x * 8; i < i1; i += kDraftBlock * 8) {
         float x[8], y[8], e[8];
         draft_load<T, VEC>(target, i, i1, x);
-        if (draft)
+        if (draft) {
             draft_load<T, VEC>(draft, i, i1, y);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                y[k] = -INFINITY;
+        }
         draft_load<float, VEC>(noise, i, i1, e);  // past the end: -inf, which never wins
+#pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (!(e[k] > 0.0f))
                 continue;
             const int v = i + k;
-            const float p = draft_prob(dp, x[k], v, greedy, inv_t);
-            const float q = minus ? draft_prob(dq, draft ? y[k] : 0.0f, v, hot_q, inv_t) : 0.0f;
-            best_p = max(best_p, draft_code(p / e[k], v));
-            best_r = max(best_r, draft_code((p - q) / e[k], v));
+            const float p = draft_prob(dp, x[k], v, greedy, rate);
+            const float r = p - draft_prob(dq, y[k], v, hot_q, rate);
+            best = max(best, draft_code((r > 0.0f ? r : p) / e[k], v, r > 0.0f));
         }
     }
-    for (int m = 1; m < 64; m *= 2) {
-        best_r = max(best_r, (unsigned long long)__shfl_xor(best_r, m));
-        best_p = max(best_p, (unsigned long long)__shfl_xor(best_p, m));
-    }
-    __shared__ unsigned long long s_best[2][kDraftBlock / 64];
-    if (threadIdx.x % 64 == 0) {
-        s_best[0][threadIdx.x / 64] = best_r;
-        s_best[1][threadIdx.x / 64] = best_p;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2)
+        best = max(best, (unsigned long long)__shfl_xor(best, m));
+    __shared__ unsigned long long s_best[kDraftBlock / 64];
+    __shared__ int s_last;
+    if (lane == 0)
+        s_best[w] = best;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int k = 1; k < kDraftBlock / 64; ++k)
+            best = max(best, s_best[k]);
+        DraftBest* b = a.best + s;
+        int last = 1;
+        if (a.race_parts > 1) {
+            atomicMax(&b->code, best);
+            // the maximum is at the device's point of coherence before the count is
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0);
+            asm volatile("" ::: "memory");
+            last = atomicAdd(&b->done, 1u) == (unsigned)a.race_parts - 1;
+            if (last)
+                best = atomicMax(&b->code, 0ull);
+        }
+        s_last = last;
+        s_best[0] = best;
     }
     __syncthreads();
-    if (threadIdx.x != 0)
+    if (!s_last || mine > a.G)
         return;
-    for (int w = 1; w < kDraftBlock / 64; ++w) {
-        best_r = max(best_r, s_best[0][w]);
-        best_p = max(best_p, s_best[1][w]);
-    }
-    DraftBest* b = a.best + s;
-    atomicMax(&b->r, best_r);
-    atomicMax(&b->p, best_p);
-    // the maxima are at the device's point of coherence before the count is
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0);
-    asm volatile("" ::: "memory");
-    if (atomicAdd(&b->done, 1u) != (unsigned)a.race_parts - 1)
-        return;
-    best_r = atomicMax(&b->r, 0ull);
-    best_p = atomicMax(&b->p, 0ull);
-    const unsigned long long win = best_r ? best_r : best_p;
-    const int token = win ? (int)~(uint32_t)win : -1;
-    a.n_accepted[s] = j;
-    for (int i = 0; i <= a.G; ++i) {
-        const int64_t o = (int64_t)s * (a.G + 1) + i;
-        a.tokens[o] = i < j ? a.drafts[(int64_t)s * a.G + i] : i == j ? token : -1;
-        if (a.prob)
-            a.prob[o] = i < j ? s_p[i]
-                        : i == j && token >= 0 ? draft_prob(dp, draft_nan_low((float)target[token]), token, greedy, inv_t)
-                                               : 0.0f;
-        if (a.accept && i < a.G)
-            a.accept[(int64_t)s * a.G + i] = i >= n ? 0.0f : s_q[i] > 0.0f ? fminf(s_p[i] / s_q[i], 1.0f) : s_p[i] > 0.0f ? 1.0f : 0.0f;
+    best = s_best[0];
+    const int token = best ? (int)~(uint32_t)best : -1;
+    const int64_t o = (int64_t)s * (a.G + 1) + mine;
+    if (mine == 0)
+        a.n_accepted[s] = j;
+    a.tokens[o] = mine < j ? d : mine == j ? token : -1;
+    if (a.prob)
+        a.prob[o] = mine < j ? s_p[mine]
+                    : mine == j && token >= 0 ? draft_prob(dp, draft_nan_low((float)target[token]), token, greedy, rate)
+                                              : 0.0f;
+    if (a.accept && mine < a.G) {
+        const float p = mine < n ? s_p[mine] : 0.0f, q = mine < n ? s_q[mine] : 0.0f;
+        a.accept[(int64_t)s * a.G + mine] = q > 0.0f ? fminf(p / q, 1.0f) : p > 0.0f ? 1.0f : 0.0f;
     }
 }
 

@@ -84,19 +84,30 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sort(const ID* __restrict
     const int t0 = blockIdx.x * kSortTokens;
     const int c0 = t0 / kSortChunk * kSortChunk;
     const int n = min(kSortChunk, T - c0);
-    for (int i = threadIdx.x; i < kSortChunk; i += kEmbedBlock)
-        s[i / kSortPartKeys * kSortPartStride + i % kSortPartKeys] = i < n ? token_key(ids, c0 + i, V) : kNoToken;
+    uint32_t mine[kSortChunk / kEmbedBlock];
+#pragma unroll
+    for (int k = 0; k < kSortChunk / kEmbedBlock; ++k)
+        mine[k] = token_key(ids, c0 + min(k * kEmbedBlock + (int)threadIdx.x, n - 1), V);
+#pragma unroll
+    for (int k = 0; k < kSortChunk / kEmbedBlock; ++k) {
+        const int i = k * kEmbedBlock + threadIdx.x;
+        s[i / kSortPartKeys * kSortPartStride + i % kSortPartKeys] = i < n ? mine[k] : kNoToken;
+    }
     __syncthreads();
     const int part = threadIdx.x % kSortParts;
     const int i = t0 - c0 + threadIdx.x / kSortParts;  // this token's place in the chunk
     const uint32_t key = s[i / kSortPartKeys * kSortPartStride + i % kSortPartKeys];
     const uint32_t* p = s + part * kSortPartStride;
     const int j0 = part * kSortPartKeys;
+    // of the equal keys, those at earlier places: `key + 1` bounds them up to place i, `key` from there on
     int before = 0;
+    const int upto = i - j0;
+#pragma unroll 8
     for (int j = 0; j < kSortPartKeys; j += 4) {
         const u32x4 k = *reinterpret_cast<const u32x4*>(p + j);
+#pragma unroll
         for (int e = 0; e < 4; ++e)
-            before += k[e] < key || (k[e] == key && j0 + j + e < i);
+            before += j + e < upto ? k[e] <= key : k[e] < key;
     }
     for (int m = 1; m < kSortParts; m *= 2)
         before += __shfl_xor(before, m);
@@ -196,19 +207,27 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
     if ((int)blockIdx.x >= sum_wgs) {
         __shared__ int named[kFillRows];
         const int v0 = ((int)blockIdx.x - sum_wgs) * kFillRows;
-        if (threadIdx.x < kFillRows) {
-            const uint32_t key = (uint32_t)v0 + threadIdx.x;
-            int lo = 0, hi = T;
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (keys[mid] < key)
-                    lo = mid + 1;
-                else
-                    hi = mid;
-            }
-            named[threadIdx.x] = lo < T && keys[lo] == key;
+        if (threadIdx.x < kFillRows)
+            named[threadIdx.x] = 0;
+        // the first of the sorted keys that is not below v0: 256 probes at a time
+        int lo = 0, hi = T;  // keys before lo are below v0, keys from hi on are not
+        while (hi > lo) {
+            const int each = (hi - lo + kEmbedBlock - 1) / kEmbedBlock;
+            const int at = lo + (int)threadIdx.x * each;
+            const int below = __syncthreads_count(at < hi && keys[at] < (uint32_t)v0);
+            // probes 0 .. below - 1 are below v0
+            hi = below == 0 ? lo : min(hi, lo + below * each);
+            lo = below == 0 ? lo : lo + (below - 1) * each + 1;
         }
-        __syncthreads();
+        // mark the rows that come from there on
+        for (int i = lo;; i += kEmbedBlock) {
+            const int at = i + (int)threadIdx.x;
+            const uint32_t row = at < T ? keys[at] - (uint32_t)v0 : kFillRows;
+            if (row < kFillRows)
+                named[row] = 1;
+            if (__syncthreads_or(row >= kFillRows))
+                break;
+        }
         const float zero[VEC] = {};
         for (int r = threadIdx.x / 64; r < kFillRows && r < V - v0; r += kEmbedBlock / 64) {
             if (named[r])
@@ -232,15 +251,19 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
     for (int i = i0; i < i1; i += U) {
         float g[U][VEC] = {};
         uint32_t key[U + 1];
+#pragma unroll
         for (int u = 0; u <= U; ++u)
             key[u] = i + u < T ? keys[i + u] : kNoToken;
         if (d < D)
+#pragma unroll
             for (int u = 0; u < U; ++u)
                 if (i + u < i1 && key[u] != kNoToken)
                     load_cols<TG, VEC>(grad + (int64_t)order[i + u] * ld_grad + d, g[u]);
+#pragma unroll
         for (int u = 0; u < U; ++u) {
             if (i + u >= i1 || key[u] == kNoToken)
                 continue;
+#pragma unroll
             for (int e = 0; e < VEC; ++e)
                 sum[e] += g[u][e];
             const bool ends = i + u + 1 >= T || key[u + 1] != key[u];
@@ -282,11 +305,26 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __re
         return;
     float sum[VEC];
     load_cols<float, VEC>(partial + (int64_t)(2 * r + 1) * D + d, sum);
-    for (int64_t i = i1, q = r + 1; i < T && keys[i] == key; i += run, ++q) {
-        float p[VEC];
-        load_cols<float, VEC>(partial + (2 * q) * D + d, p);
-        for (int e = 0; e < VEC; ++e)
-            sum[e] += p[e];
+    // eight following runs at a time: their loads are in flight together
+    constexpr int U = 8;
+    for (int64_t i = i1, q = r + 1;; i += U * run, q += U) {
+        bool more[U];
+        float p[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            more[u] = i + u * run < T && keys[i + u * run] == key;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (more[u])
+                load_cols<float, VEC>(partial + 2 * (q + u) * D + d, p[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (more[u])
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    sum[e] += p[u][e];
+        if (!more[U - 1])
+            break;
     }
     put_row<TD, VEC>(dtable + (int64_t)key * ld_table + d, sum, scale, accumulate);
 }

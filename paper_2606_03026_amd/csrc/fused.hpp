@@ -735,6 +735,8 @@ __global__ __launch_bounds__(256) void k_fused_cut(const XT* __restrict__ x, int
 // gs for the product, in NS planes of rows of ld_gs elements (NS = 0: FP32 rows),
 // and the column sums of g over these rows to partial[row block].  Bound by memory.
 constexpr int kGateCols = 256;
+constexpr int kGateAhead = 4;  // rows of a thread in flight
+constexpr int kGateParts = 32;  // the most parts that the bias gradient comes in
 
 template <typename T, int NS, bool VEC>
 __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ pre,
@@ -751,24 +753,34 @@ __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, in
     for (int e = 0; e < 8; ++e)
         sc[e] = e < n ? scale[m + e] : 0.0f;
     if (n > 0)
-        for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
-            float g[8], slope[8] = {};
-            read_w<T, 8>(dy + b * ld_dy + m, g, full, n);
-            if (act)
-                read_w<T, 8>(pre + b * ld_pre + m, slope, full, n);
-            act_slopes<8>(slope, act);
+        for (int64_t r0 = b0 + threadIdx.x / 32; r0 < b1; r0 += 8 * kGateAhead) {
+            float g[kGateAhead][8], slope[kGateAhead][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                g[e] *= slope[e];
-                sum[e] += g[e];
-                g[e] *= sc[e];
+            for (int u = 0; u < kGateAhead; ++u) {
+                const int64_t b = min(r0 + 8 * u, b1 - 1);
+                read_w<T, 8>(dy + b * ld_dy + m, g[u], full, n);
+                if (act)
+                    read_w<T, 8>(pre + b * ld_pre + m, slope[u], full, n);
             }
-            // rows are padded to whole vectors, with zeros
-            if constexpr (NS == 0) {
-                if (gs)
-                    write_w<float, 8>(reinterpret_cast<float*>(gs) + b * ld_gs + m, g, true, 8);
-            } else if (gs) {
-                put_planes<NS>(gs + b * ld_gs + m, plane, g);
+#pragma unroll
+            for (int u = 0; u < kGateAhead; ++u) {
+                const int64_t b = r0 + 8 * u;
+                if (b >= b1)
+                    break;
+                act_slopes<8>(slope[u], act);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    g[u][e] *= slope[u][e];
+                    sum[e] += g[u][e];
+                    g[u][e] *= sc[e];
+                }
+                // rows are padded to whole vectors, with zeros
+                if constexpr (NS == 0) {
+                    if (gs)
+                        write_w<float, 8>(reinterpret_cast<float*>(gs) + b * ld_gs + m, g[u], true, 8);
+                } else if (gs) {
+                    put_planes<NS>(gs + b * ld_gs + m, plane, g[u]);
+                }
             }
         }
     if (!partial)
@@ -794,9 +806,14 @@ __global__ __launch_bounds__(64) void k_fused_bias(const float* __restrict__ par
     const int m = blockIdx.x * 64 + threadIdx.x;
     if (m >= M)
         return;
+    float p[kGateParts];
+#pragma unroll
+    for (int i = 0; i < kGateParts; ++i)
+        p[i] = i < parts ? partial[(int64_t)i * M + m] : 0.0f;
     float v = 0.0f;
-    for (int p = 0; p < parts; ++p)
-        v += partial[(int64_t)p * M + m];
+#pragma unroll
+    for (int i = 0; i < kGateParts; ++i)
+        v += p[i];
     dbias[m] = v;
 }
 

@@ -18,17 +18,18 @@ using spk::aligned_to;
 using spk::fail;
 using spk::hip_fail;
 
-constexpr int kWaveOf8 = spk::kDraftBlock * 8;  // logits a workgroup takes at a time
+constexpr int kWaveOf8 = spk::kDraftBlock * 8;  // logits of a stretch: 8 a thread
+constexpr int64_t kStatsWgs = 4096, kRaceWgs = 1024;
 
-// Parts a row of V logits is cut into when `rows` rows are worked on at once:
-// about four workgroups per compute unit, whole rounds of 2,048 logits each.
-void split(int64_t rows, int32_t V, int* parts, int* len)
+// Parts a row of V logits is cut into, where `rows` rows are worked on at once
+// and `want` workgroups are to share them; whole stretches of 2,048 logits each.
+void split(int64_t rows, int64_t want, int32_t V, int* parts, int* len)
 {
-    const int64_t rounds = ((int64_t)V + kWaveOf8 - 1) / kWaveOf8;
-    const int64_t want = std::min<int64_t>({std::max<int64_t>(1, 1024 / std::max<int64_t>(rows, 1)), rounds,
-                                            (int64_t)spk::kDraftMaxParts});
-    const int64_t per = (rounds + want - 1) / want;
-    *parts = (int)((rounds + per - 1) / per);
+    const int64_t stretches = ((int64_t)V + kWaveOf8 - 1) / kWaveOf8;
+    const int64_t most = std::min<int64_t>(
+        {std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)), stretches, (int64_t)spk::kDraftMaxParts});
+    const int64_t per = (stretches + most - 1) / most;
+    *parts = (int)((stretches + per - 1) / per);
     *len = (int)std::min<int64_t>(per * kWaveOf8, (int64_t)1 << 30);
 }
 
@@ -46,25 +47,23 @@ Plan make_plan(int32_t S, int32_t G, int32_t V, bool dist)
 {
     Plan p{};
     p.rows = G + 1 + (dist ? G : 0);
-    split((int64_t)S * p.rows, V, &p.parts, &p.part_len);
-    split(S, V, &p.race_parts, &p.race_len);
+    split((int64_t)S * p.rows, kStatsWgs, V, &p.parts, &p.part_len);
+    split(S, kRaceWgs, V, &p.race_parts, &p.race_len);
     p.best_bytes = (int64_t)sizeof(spk::DraftBest) * S;
     p.bytes = p.best_bytes + (int64_t)sizeof(spk::DraftPart) * S * p.rows * p.parts;
     return p;
 }
 
-template <typename T>
-void launch(const spk::DraftArgs& a, bool vec, hipStream_t st)
+template <typename T, int VEC>
+void launch(const spk::DraftArgs& a, hipStream_t st)
 {
     const dim3 block(spk::kDraftBlock), stats((unsigned)((int64_t)a.S * a.rows * a.parts)),
         race((unsigned)((int64_t)a.S * a.race_parts));
-    if (vec) {
-        hipLaunchKernelGGL((spk::k_draft_stats<T, 8>), stats, block, 0, st, a);
-        hipLaunchKernelGGL((spk::k_draft_race<T, 8>), race, block, 0, st, a);
-    } else {
-        hipLaunchKernelGGL((spk::k_draft_stats<T, 1>), stats, block, 0, st, a);
-        hipLaunchKernelGGL((spk::k_draft_race<T, 1>), race, block, 0, st, a);
-    }
+    if (a.part_len <= kWaveOf8)
+        hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 1>), stats, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 4>), stats, block, 0, st, a);
+    hipLaunchKernelGGL((spk::k_draft_race<T, VEC>), race, block, 0, st, a);
 }
 
 bool rows_vectorize(const void* p, int type, int64_t ld) { return aligned_to(p, 16) && ld * spk::type_bytes(type) % 16 == 0; }
@@ -124,9 +123,9 @@ int head_draft_verify(const void* target, int64_t ld_target, const void* draft, 
                      rows_vectorize(noise, SPIKE_TYPE_F32, ld_noise);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     switch (logits_type) {
-    case SPIKE_TYPE_F32: launch<float>(a, vec, st); break;
-    case SPIKE_TYPE_BF16: launch<spk::bf16>(a, vec, st); break;
-    default: launch<spk::f16>(a, vec, st); break;
+    case SPIKE_TYPE_F32: vec ? launch<float, 8>(a, st) : launch<float, 1>(a, st); break;
+    case SPIKE_TYPE_BF16: vec ? launch<spk::bf16, 8>(a, st) : launch<spk::bf16, 1>(a, st); break;
+    default: vec ? launch<spk::f16, 8>(a, st) : launch<spk::f16, 1>(a, st); break;
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "draft verification launch");
