@@ -459,7 +459,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         }
     }
     if (dbias)
-        hipLaunchKernelGGL(spk::k_fused_bias, dim3((unsigned)((h->M + 63) / 64)), dim3(64), 0, st, partial, parts, h->M,
+        hipLaunchKernelGGL(spk::k_fused_bias, dim3((unsigned)((h->M + 63) / 64)), dim3(256), 0, st, partial, parts, h->M,
                            dbias);
     if (dx && B > 0) {
         FusedArgs a{};

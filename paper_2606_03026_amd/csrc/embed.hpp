@@ -10,6 +10,9 @@
 // row whenever the id changes.  A row whose tokens lie in one run is written
 // at once; the others leave one partial sum per run, joined afterwards in
 // ascending order.  No atomics: the order of every sum is fixed by the ids.
+// The rows that no token names are most of a table's bytes: they are zeroed by
+// workgroups beside those of all three steps, since sorting and adding are
+// bound by latency and zeroing by the memory's writes.
 #pragma once
 
 #include "types.hpp"
@@ -73,13 +76,77 @@ constexpr int kSortTokens = kEmbedBlock / kSortParts;
 constexpr int kSortPartKeys = kSortChunk / kSortParts;
 constexpr int kSortPartStride = kSortPartKeys + 4;  // the parts' reads fall into different LDS banks
 
+// Rows [first, first + count) of a table whose rows of `bytes` bytes lie `step`
+// bytes apart, to be zeroed by workgroups of kFillRows rows each.
+struct FillArgs {
+    char* table;
+    int64_t step, bytes;
+    int first, count;
+    int wide;  // rows in 16-byte pieces, else in 2-byte ones
+};
+
+constexpr int kFillRows = 8;
+inline int64_t fill_wgs(const FillArgs& f) { return ((int64_t)f.count + kFillRows - 1) / kFillRows; }
+
+__device__ inline void zero_row(const FillArgs& f, int row)
+{
+    char* p = f.table + row * f.step;
+    if (f.wide)
+        for (int64_t i = threadIdx.x % 64 * 16; i < f.bytes; i += 64 * 16)
+            __builtin_nontemporal_store(u32x4{}, reinterpret_cast<u32x4*>(p + i));
+    else
+        for (int64_t i = threadIdx.x % 64 * 2; i < f.bytes; i += 64 * 2)
+            *reinterpret_cast<uint16_t*>(p + i) = 0;
+}
+
+// All of this workgroup's rows.
+__device__ inline void zero_rows(const FillArgs& f, int wg)
+{
+    for (int r = threadIdx.x / 64; r < kFillRows && wg * kFillRows + r < f.count; r += kEmbedBlock / 64)
+        zero_row(f, f.first + wg * kFillRows + r);
+}
+
+// Those of its rows that none of the T sorted keys names.
+__device__ inline void zero_unnamed_rows(const FillArgs& f, int wg, const uint32_t* __restrict__ keys, int T)
+{
+    __shared__ int named[kFillRows];
+    const int v0 = f.first + wg * kFillRows;
+    if (threadIdx.x < kFillRows)
+        named[threadIdx.x] = 0;
+    // the first of the sorted keys that is not below v0: 256 probes at a time
+    int lo = 0, hi = T;  // keys before lo are below v0, keys from hi on are not
+    while (hi > lo) {
+        const int each = (hi - lo + kEmbedBlock - 1) / kEmbedBlock;
+        const int at = lo + (int)threadIdx.x * each;
+        const int below = __syncthreads_count(at < hi && keys[at] < (uint32_t)v0);
+        // probes 0 .. below - 1 are below v0
+        hi = below == 0 ? lo : min(hi, lo + below * each);
+        lo = below == 0 ? lo : lo + (below - 1) * each + 1;
+    }
+    // mark the rows that come from there on
+    for (int i = lo;; i += kEmbedBlock) {
+        const int at = i + (int)threadIdx.x;
+        const uint32_t row = at < T ? keys[at] - (uint32_t)v0 : kFillRows;
+        if (row < kFillRows)
+            named[row] = 1;
+        if (__syncthreads_or(row >= kFillRows))
+            break;
+    }
+    for (int r = threadIdx.x / 64; r < kFillRows && wg * kFillRows + r < f.count; r += kEmbedBlock / 64)
+        if (!named[r])
+            zero_row(f, v0 + r);
+}
+
 // Sorts each chunk of kSortChunk tokens by (key, position): a token's place
 // is the number of tokens of its chunk that come before it.  2,048
-// comparisons a token, shared by 8 lanes.
+// comparisons a token, shared by 8 lanes.  Workgroups from sort_wgs on zero rows.
 template <typename ID>
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_sort(const ID* __restrict__ ids, int T, int V,
-                                                            uint32_t* __restrict__ keys, int* __restrict__ order)
+                                                            uint32_t* __restrict__ keys, int* __restrict__ order,
+                                                            int sort_wgs, FillArgs fill)
 {
+    if ((int)blockIdx.x >= sort_wgs)
+        return zero_rows(fill, blockIdx.x - sort_wgs);
     __shared__ uint32_t s[kSortParts * kSortPartStride];
     const int t0 = blockIdx.x * kSortTokens;
     const int c0 = t0 / kSortChunk * kSortChunk;
@@ -123,8 +190,10 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sort(const ID* __restrict
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_merge(const uint32_t* __restrict__ keys,
                                                              const int* __restrict__ order, int T,
                                                              uint32_t* __restrict__ out_keys,
-                                                             int* __restrict__ out_order)
+                                                             int* __restrict__ out_order, int merge_wgs, FillArgs fill)
 {
+    if ((int)blockIdx.x >= merge_wgs)
+        return zero_rows(fill, blockIdx.x - merge_wgs);
     const int i = blockIdx.x * kSortTokens + threadIdx.x / kSortParts;
     const int part = threadIdx.x % kSortParts;
     const bool live = i < T;
@@ -161,120 +230,104 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_merge(const uint32_t* __r
 
 // --- sums ------------------------------------------------------------------
 
-template <typename TG, int VEC>
-__device__ inline void load_cols(const TG* p, float (&v)[VEC])
+template <typename T, int VEC>
+__device__ inline void load_cols(const T* p, float (&v)[VEC])
 {
-    if constexpr (VEC == 8) {
-        const f32x8 x = load8(p);
-        for (int e = 0; e < 8; ++e)
-            v[e] = x[e];
-    } else {
+    typedef T tv __attribute__((ext_vector_type(VEC), aligned(VEC * sizeof(T) < 16 ? VEC * sizeof(T) : 16)));
+    if constexpr (VEC > 1) {
+        const tv x = *reinterpret_cast<const tv*>(p);
+#pragma unroll
         for (int e = 0; e < VEC; ++e)
-            v[e] = (float)p[e];
+            v[e] = (float)x[e];
+    } else {
+        v[0] = (float)p[0];
     }
 }
 
-template <typename TD, int VEC>
-__device__ inline void put_row(TD* p, const float (&v)[VEC], float scale, bool accumulate)
+template <typename T, int VEC>
+__device__ inline void put_row(T* p, const float (&v)[VEC], float scale, bool accumulate)
 {
-    if constexpr (VEC == 8) {
-        f32x8 x;
-        for (int e = 0; e < 8; ++e)
-            x[e] = v[e] * scale;
-        if (accumulate)
-            x += load8(p);
-        store8(p, x);
-    } else {
+    typedef T tv __attribute__((ext_vector_type(VEC), aligned(VEC * sizeof(T) < 16 ? VEC * sizeof(T) : 16)));
+    float x[VEC] = {};
+    if (accumulate)
+        load_cols<T, VEC>(p, x);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        x[e] = in_fp32<T>(v[e] * scale + x[e]);
+    if constexpr (VEC > 1) {
+        tv y;
+#pragma unroll
         for (int e = 0; e < VEC; ++e)
-            p[e] = (TD)in_fp32<TD>(v[e] * scale + (accumulate ? (float)p[e] : 0.0f));
+            y[e] = (T)x[e];
+        *reinterpret_cast<tv*>(p) = y;
+    } else {
+        p[0] = (T)x[0];
     }
 }
 
-constexpr int kFillRows = 32;  // rows of the table that a filling workgroup looks at
+constexpr int kMaxRun = 32;  // tokens of a run: its keys, and the next one, along the lanes of a wave
 
 // Workgroups below sum_wgs: each wave adds up one run (`run` tokens of the
 // sorted list) for 64 VEC columns.  partial[2 r] holds run r's sum of a row that began in an
 // earlier run, partial[2 r + 1] that of a row that begins in run r and goes
-// on.  The other workgroups write zeros to the rows that no token names.
+// on.  The other workgroups zero the rows that no token names.
 template <typename TG, typename TD, int VEC>
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict__ grad, int64_t ld_grad,
                                                            const uint32_t* __restrict__ keys,
-                                                           const int* __restrict__ order, int T, int V, int D, int run,
+                                                           const int* __restrict__ order, int T, int D, int run,
                                                            int sum_wgs, float scale, int accumulate,
                                                            TD* __restrict__ dtable, int64_t ld_table,
-                                                           float* __restrict__ partial)
+                                                           float* __restrict__ partial, FillArgs fill)
 {
-    if ((int)blockIdx.x >= sum_wgs) {
-        __shared__ int named[kFillRows];
-        const int v0 = ((int)blockIdx.x - sum_wgs) * kFillRows;
-        if (threadIdx.x < kFillRows)
-            named[threadIdx.x] = 0;
-        // the first of the sorted keys that is not below v0: 256 probes at a time
-        int lo = 0, hi = T;  // keys before lo are below v0, keys from hi on are not
-        while (hi > lo) {
-            const int each = (hi - lo + kEmbedBlock - 1) / kEmbedBlock;
-            const int at = lo + (int)threadIdx.x * each;
-            const int below = __syncthreads_count(at < hi && keys[at] < (uint32_t)v0);
-            // probes 0 .. below - 1 are below v0
-            hi = below == 0 ? lo : min(hi, lo + below * each);
-            lo = below == 0 ? lo : lo + (below - 1) * each + 1;
-        }
-        // mark the rows that come from there on
-        for (int i = lo;; i += kEmbedBlock) {
-            const int at = i + (int)threadIdx.x;
-            const uint32_t row = at < T ? keys[at] - (uint32_t)v0 : kFillRows;
-            if (row < kFillRows)
-                named[row] = 1;
-            if (__syncthreads_or(row >= kFillRows))
-                break;
-        }
-        const float zero[VEC] = {};
-        for (int r = threadIdx.x / 64; r < kFillRows && r < V - v0; r += kEmbedBlock / 64) {
-            if (named[r])
-                continue;
-            TD* p = dtable + (int64_t)(v0 + r) * ld_table;
-            for (int d = threadIdx.x % 64 * VEC; d < D; d += 64 * VEC)
-                put_row<TD, VEC>(p + d, zero, 0.0f, false);
-        }
-        return;
-    }
-    const int blocks = (D + 64 * VEC - 1) / (64 * VEC);
+    if ((int)blockIdx.x >= sum_wgs)
+        return zero_unnamed_rows(fill, blockIdx.x - sum_wgs, keys, T);
+    const int blocks = (D + 64 * VEC - 1) / (64 * VEC), lane = threadIdx.x % 64;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
     const int r = unit / blocks;
-    const int d = (unit % blocks * 64 + threadIdx.x % 64) * VEC;
-    const int i0 = r * run, i1 = min(T, i0 + run);
+    const int i0 = r * run;
     if (i0 >= T)
         return;
+    const int n = min(run, T - i0);
+    // column offset; lanes past the row repeat its last columns and store nothing
+    const int col = (unit % blocks * 64 + lane) * VEC;
+    const bool inside = col < D;
+    const int d = inside ? col : D - VEC;
+    // lane l holds the key before the run (l = 0) and those of its tokens (l = 1 .. n), then the one behind it
+    const int at = i0 + lane - 1;
+    const uint32_t key_l = lane <= n + 1 && at >= 0 && at < T ? keys[at] : kNoToken;
+    const int order_l = lane >= 1 && lane <= n && key_l != kNoToken ? order[at] : 0;
+    auto key_of = [&](int i) { return (uint32_t)__builtin_amdgcn_readlane(key_l, i + 1); };  // token i of the run; -1, n: its neighbours
     float sum[VEC] = {};
-    bool from_before = i0 > 0 && keys[i0 - 1] == keys[i0];
+    bool from_before = i0 > 0 && key_of(-1) == key_of(0);
     constexpr int U = 8;  // rows in flight
-    for (int i = i0; i < i1; i += U) {
-        float g[U][VEC] = {};
-        uint32_t key[U + 1];
-#pragma unroll
-        for (int u = 0; u <= U; ++u)
-            key[u] = i + u < T ? keys[i + u] : kNoToken;
-        if (d < D)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (i + u < i1 && key[u] != kNoToken)
-                    load_cols<TG, VEC>(grad + (int64_t)order[i + u] * ld_grad + d, g[u]);
+    for (int i = 0; i < n; i += U) {
+        float g[U][VEC];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (i + u >= i1 || key[u] == kNoToken)
-                continue;
+            // (a padding token's gradient is not read: row 0 in its place; past the run, the last token's)
+            const int t = __builtin_amdgcn_readlane(order_l, min(i + u, n - 1) + 1);
+            load_cols<TG, VEC>(grad + (int64_t)t * ld_grad + d, g[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i + u >= n)
+                break;
+            const uint32_t key = key_of(i + u);
+            if (key == kNoToken)
+                break;  // nor do any after it name a row
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
                 sum[e] += g[u][e];
-            const bool ends = i + u + 1 >= T || key[u + 1] != key[u];
-            if (!ends && i + u + 1 < i1)
+            const bool ends = i0 + i + u + 1 >= T || key_of(i + u + 1) != key;
+            if (!ends && i + u + 1 < n)
                 continue;
-            if (d < D) {
+            if (inside) {
                 if (ends && !from_before)
-                    put_row<TD, VEC>(dtable + (int64_t)key[u] * ld_table + d, sum, scale, accumulate);
+                    put_row<TD, VEC>(dtable + (int64_t)key * ld_table + d, sum, scale, accumulate);
                 else
                     put_row<float, VEC>(partial + (int64_t)(2 * r + (from_before ? 0 : 1)) * D + d, sum, 1.0f, false);
             }
+#pragma unroll
             for (int e = 0; e < VEC; ++e)
                 sum[e] = 0.0f;
             from_before = false;
@@ -289,44 +342,51 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __re
                                                             float scale, int accumulate, TD* __restrict__ dtable,
                                                             int64_t ld_table, const float* __restrict__ partial)
 {
-    const int blocks = (D + 64 * VEC - 1) / (64 * VEC);
+    const int blocks = (D + 64 * VEC - 1) / (64 * VEC), lane = threadIdx.x % 64;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
     const int r = unit / blocks;
-    const int d = (unit % blocks * 64 + threadIdx.x % 64) * VEC;
+    const int col = (unit % blocks * 64 + lane) * VEC;
+    const bool inside = col < D;
+    const int d = inside ? col : D - VEC;
     const int64_t i0 = (int64_t)r * run, i1 = i0 + run;
     if (i1 >= T)
         return;
-    const uint32_t key = keys[i1 - 1];
-    if (key == kNoToken || keys[i1] != key)
-        return;  // no row goes on
-    if (i0 > 0 && keys[i0 - 1] == key)
-        return;  // it began earlier
-    if (d >= D)
-        return;
+    // lane 0: the key before this run; lane 1: its last; lane 2 + l: the first of the l-th run after it
+    const int64_t at = lane == 0 ? i0 - 1 : lane == 1 ? i1 - 1 : i1 + (int64_t)(lane - 2) * run;
+    uint32_t key_l = at >= 0 && at < T ? keys[at] : kNoToken;
     float sum[VEC];
-    load_cols<float, VEC>(partial + (int64_t)(2 * r + 1) * D + d, sum);
-    // eight following runs at a time: their loads are in flight together
-    constexpr int U = 8;
-    for (int64_t i = i1, q = r + 1;; i += U * run, q += U) {
-        bool more[U];
-        float p[U][VEC];
+    load_cols<float, VEC>(partial + (int64_t)(2 * r + 1) * D + d, sum);  // (asked for with the keys; there if a row goes on)
+    const uint32_t key = __builtin_amdgcn_readlane(key_l, 1);
+    if (key == kNoToken || (uint32_t)__builtin_amdgcn_readlane(key_l, 2) != key)
+        return;  // no row goes on
+    if (i0 > 0 && (uint32_t)__builtin_amdgcn_readlane(key_l, 0) == key)
+        return;  // it began earlier
+    constexpr int U = 8;  // partial sums in flight
+    int64_t q = r + 1;    // the run whose key lane 2 holds
+    for (;;) {
+        // runs q .. q + more - 1 belong to the row
+        const uint64_t differ = __ballot(lane >= 2 && key_l != key) >> 2;
+        const int more = differ ? __builtin_ctzll(differ) : 62;
+        for (int k = 0; k < more; k += U) {
+            float p[U][VEC];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            more[u] = i + u * run < T && keys[i + u * run] == key;
+            for (int u = 0; u < U; ++u)
+                load_cols<float, VEC>(partial + 2 * (q + min(k + u, more - 1)) * D + d, p[u]);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (more[u])
-                load_cols<float, VEC>(partial + 2 * (q + u) * D + d, p[u]);
+            for (int u = 0; u < U; ++u)
+                if (k + u < more)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (more[u])
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    sum[e] += p[u][e];
-        if (!more[U - 1])
+                    for (int e = 0; e < VEC; ++e)
+                        sum[e] += p[u][e];
+        }
+        if (more < 62)
             break;
+        q += 62;
+        const int64_t next = q * run + (int64_t)(lane - 2) * run;
+        key_l = lane >= 2 && next < T ? keys[next] : kNoToken;
     }
-    put_row<TD, VEC>(dtable + (int64_t)key * ld_table + d, sum, scale, accumulate);
+    if (inside)
+        put_row<TD, VEC>(dtable + (int64_t)key * ld_table + d, sum, scale, accumulate);
 }
 
 }  // namespace spk

@@ -20,7 +20,11 @@ using spk::is_float_type;
 using spk::type_bytes;
 
 // Tokens a run holds: short ones where there are few tokens to spread over the chip.
-int run_length(int32_t T) { return T <= 4096 ? 8 : 32; }
+int run_length(int32_t T) { return T <= 4096 ? 8 : 16; }
+
+static_assert(32 <= spk::kMaxRun, "a run's keys lie along a wave");
+
+constexpr int64_t kFillBesideSort = 128ll << 20, kFillBesideMerge = 48ll << 20;
 
 bool rows_vectorize(const void* p, int type, int64_t ld, int32_t D)
 {
@@ -120,18 +124,23 @@ struct Grad {
     hipStream_t st;
 };
 
+// Columns a lane takes: 16 bytes of the gradients.
+template <typename TG>
+constexpr int vector_of() { return sizeof(TG) == 4 ? 4 : 8; }
+
 template <typename TG, typename TD, int VEC>
-void launch_grad(const Grad& a)
+void launch_grad(const Grad& a, const spk::FillArgs& fill)
 {
     constexpr int waves = spk::kEmbedBlock / 64;
     const int run = run_length(a.T);
     const int64_t blocks = (a.D + 64 * VEC - 1) / (64 * VEC);
     const int64_t runs = ((int64_t)a.T + run - 1) / run;
     const int64_t sum_wgs = (runs * blocks + waves - 1) / waves;
-    const int64_t fill_wgs = a.accumulate ? 0 : ((int64_t)a.V + spk::kFillRows - 1) / spk::kFillRows;
-    hipLaunchKernelGGL((spk::k_embed_sum<TG, TD, VEC>), dim3((unsigned)(sum_wgs + fill_wgs)), dim3(spk::kEmbedBlock), 0,
-                       a.st, static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.V, a.D, run,
-                       (int)sum_wgs, a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial);
+    const int64_t wgs = sum_wgs + spk::fill_wgs(fill);
+    if (wgs > 0)
+        hipLaunchKernelGGL((spk::k_embed_sum<TG, TD, VEC>), dim3((unsigned)wgs), dim3(spk::kEmbedBlock), 0, a.st,
+                           static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.D, run, (int)sum_wgs,
+                           a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, fill);
     if (runs > 1)
         hipLaunchKernelGGL((spk::k_embed_join<TD, VEC>), dim3((unsigned)sum_wgs), dim3(spk::kEmbedBlock), 0, a.st,
                            a.ws.keys, a.T, a.D, run, a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table,
@@ -139,13 +148,25 @@ void launch_grad(const Grad& a)
 }
 
 template <typename TG>
-void grad_table(const Grad& a, int table_type, bool vec)
+void grad_table(const Grad& a, int table_type, bool vec, const spk::FillArgs& fill)
 {
+    constexpr int V = vector_of<TG>();
     switch (table_type) {
-    case SPIKE_TYPE_F32: return vec ? launch_grad<TG, float, 8>(a) : launch_grad<TG, float, 1>(a);
-    case SPIKE_TYPE_BF16: return vec ? launch_grad<TG, spk::bf16, 8>(a) : launch_grad<TG, spk::bf16, 1>(a);
-    default: return vec ? launch_grad<TG, spk::f16, 8>(a) : launch_grad<TG, spk::f16, 1>(a);
+    case SPIKE_TYPE_F32: return vec ? launch_grad<TG, float, V>(a, fill) : launch_grad<TG, float, 1>(a, fill);
+    case SPIKE_TYPE_BF16: return vec ? launch_grad<TG, spk::bf16, V>(a, fill) : launch_grad<TG, spk::bf16, 1>(a, fill);
+    default: return vec ? launch_grad<TG, spk::f16, V>(a, fill) : launch_grad<TG, spk::f16, 1>(a, fill);
     }
+}
+
+// Cuts the next `bytes` bytes' worth of rows (whole workgroups' rows) off what is left to zero.
+spk::FillArgs take_rows(spk::FillArgs* left, int64_t bytes)
+{
+    spk::FillArgs f = *left;
+    const int64_t rows = bytes / std::max<int64_t>(f.bytes, 1) / spk::kFillRows * spk::kFillRows;
+    f.count = (int)std::min<int64_t>(rows, left->count);
+    left->first += f.count;
+    left->count -= f.count;
+    return f;
 }
 
 }  // namespace
@@ -225,26 +246,36 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
         return fail(SPIKE_EINVAL, "workspace of %lld bytes, needs %lld", (long long)workspace_bytes,
                     (long long)spike_embed_workspace_bytes(T, D));
     Grad a{grad, ld_grad, ids, T, V, D, scale, accumulate, dtable, ld_table, {}, static_cast<hipStream_t>(stream)};
+    const bool vec = rows_vectorize(grad, grad_type, ld_grad, D) && rows_vectorize(dtable, table_type, ld_table, D);
+    const int64_t elem = type_bytes(table_type);
+    spk::FillArgs fill{static_cast<char*>(dtable), ld_table * elem, D * elem, 0, accumulate ? 0 : V,
+                       (int)rows_vectorize(dtable, table_type, ld_table, D)};
     if (T > 0) {
         grad_space(T, D, workspace, &a.ws);
         const bool one = T <= spk::kSortChunk;
-        const dim3 grid((unsigned)((T + spk::kSortTokens - 1) / spk::kSortTokens)), block(spk::kEmbedBlock);
+        const int wgs = (T + spk::kSortTokens - 1) / spk::kSortTokens;
         uint32_t* k = one ? a.ws.keys : a.ws.chunk_keys;
         int* o = one ? a.ws.order : a.ws.chunk_order;
+        // Rows zeroed beside the sorting, before it is known which are named (those are
+        // then written again); the others wait for the sums.
+        const spk::FillArgs with_sort = take_rows(&fill, kFillBesideSort);
+        const dim3 block(spk::kEmbedBlock), grid((unsigned)(wgs + spk::fill_wgs(with_sort)));
         if (id_type == SPIKE_TYPE_I64)
             hipLaunchKernelGGL(spk::k_embed_sort<int64_t>, grid, block, 0, a.st, static_cast<const int64_t*>(ids), T, V,
-                               k, o);
+                               k, o, wgs, with_sort);
         else
             hipLaunchKernelGGL(spk::k_embed_sort<int32_t>, grid, block, 0, a.st, static_cast<const int32_t*>(ids), T, V,
-                               k, o);
-        if (!one)
-            hipLaunchKernelGGL(spk::k_embed_merge, grid, block, 0, a.st, k, o, T, a.ws.keys, a.ws.order);
+                               k, o, wgs, with_sort);
+        if (!one) {
+            const spk::FillArgs with_merge = take_rows(&fill, kFillBesideMerge);
+            hipLaunchKernelGGL(spk::k_embed_merge, dim3((unsigned)(wgs + spk::fill_wgs(with_merge))), block, 0, a.st, k, o,
+                               T, a.ws.keys, a.ws.order, wgs, with_merge);
+        }
     }
-    const bool vec = rows_vectorize(grad, grad_type, ld_grad, D) && rows_vectorize(dtable, table_type, ld_table, D);
     switch (grad_type) {
-    case SPIKE_TYPE_F32: grad_table<float>(a, table_type, vec); break;
-    case SPIKE_TYPE_BF16: grad_table<spk::bf16>(a, table_type, vec); break;
-    default: grad_table<spk::f16>(a, table_type, vec); break;
+    case SPIKE_TYPE_F32: grad_table<float>(a, table_type, vec, fill); break;
+    case SPIKE_TYPE_BF16: grad_table<spk::bf16>(a, table_type, vec, fill); break;
+    default: grad_table<spk::f16>(a, table_type, vec, fill); break;
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "embedding gradient launch");
