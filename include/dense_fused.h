@@ -75,6 +75,7 @@ extern "C" {
 
 #define FUSED_MAX_DIM (1 << 20)
 #define FUSED_MAX_B (1 << 22)
+#define FUSED_FEW_ROWS 32 /* up to here forward needs no workspace */
 
 typedef struct dense_fused *dense_fused_t;
 
@@ -92,7 +93,7 @@ int dense_fused_forward(dense_fused_t handle, const void *x, int32_t x_type, int
                         int64_t workspace_bytes, void *stream);
 
 /* Workspace of dense_fused_forward for these rows: 0 (it may then be NULL)
- * for few rows, and for 16-bit ones that start on 16-byte boundaries with K a
+ * for up to FUSED_FEW_ROWS rows, and for 16-bit ones that start on 16-byte boundaries with K a
  * multiple of 8; -1 for a null handle or a size or type it refuses. */
 int64_t dense_fused_forward_workspace_bytes(dense_fused_t handle, const void *x, int32_t x_type, int64_t ld_x,
                                             int32_t B);

@@ -31,7 +31,7 @@ SPIKE_LAYOUT_ROW_MAJOR, SPIKE_LAYOUT_COL_MAJOR = 0, 1
 SPIKE_TYPE_F32, SPIKE_TYPE_BF16, SPIKE_TYPE_F16, SPIKE_TYPE_I8, SPIKE_TYPE_I32, SPIKE_TYPE_I64 = 0, 1, 2, 3, 4, 5
 DENSE_ACT_NONE, DENSE_ACT_RELU, DENSE_ACT_GELU, DENSE_ACT_SILU = 0, 1, 2, 3
 DENSE_FUSED_BACKWARD = 1
-FUSED_MAX_DIM, FUSED_MAX_B = 1 << 20, 1 << 22
+FUSED_MAX_DIM, FUSED_MAX_B, FUSED_FEW_ROWS = 1 << 20, 1 << 22, 32
 EMBED_MAX_V, EMBED_MAX_D, EMBED_MAX_T = 1 << 28, 65536, 1 << 22
 DRAFT_MAX_S, DRAFT_MAX_G, DRAFT_MAX_V = 4096, 31, 1 << 30
 
@@ -148,6 +148,15 @@ def _type_of(t: torch.Tensor, name: str) -> int:
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int):
     """(address, elements between rows) of a device tensor [rows, cols] whose rows are contiguous."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.shape == (rows, cols):
+        step, one = t.stride()
+        if one == 1 and step >= cols:
+            return t.data_ptr(), step
+    return _other_rows(t, name, rows, cols)
+
+
+def _other_rows(t, name: str, rows: int, cols: int):
+    """_rows of a tensor with one column or one row of any stride; what else there is, is refused."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
@@ -162,9 +171,9 @@ def _vector(t: torch.Tensor | None, name: str, n: int, dtype=torch.float32):
     """Address of a contiguous device tensor of n elements; None stays None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n:
+    if t.dtype is not dtype or t.numel() != n:
         raise TypeError(f"{name} must be {dtype} with {n} entries")
-    return _dev_ptr(t, name)
+    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _dev_ptr(t, name)
 
 
 def _workspace(given: torch.Tensor | None, nbytes: int, device, stream) -> torch.Tensor:
@@ -527,7 +536,9 @@ def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: t
     if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
         raise TypeError("residual and pre must have y's type")
     x_type = _type_of(x, "x")
-    wp, n_ws = None, int(_lib.dense_fused_forward_workspace_bytes(h.ptr, xp, x_type, ldx, B))
+    wp, n_ws = None, 0
+    if B > FUSED_FEW_ROWS:
+        n_ws = _lib.dense_fused_forward_workspace_bytes(h.ptr, xp, x_type, ldx, B)
     if n_ws > 0:
         workspace = _workspace(workspace, n_ws, x.device, stream)
         wp, n_ws = _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()

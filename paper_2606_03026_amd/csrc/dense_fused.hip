@@ -14,8 +14,8 @@
 struct dense_fused {
     int32_t K = 0, M = 0;
     int device = 0;
-    int8_t* P = nullptr;   // rows of Q as outputs
-    int8_t* Pt = nullptr;  // columns of Q as outputs (DENSE_FUSED_BACKWARD)
+    int8_t* P = nullptr;     // rows of Q as outputs; the one allocation, which holds the others too
+    int8_t* Pt = nullptr;    // columns of Q as outputs (DENSE_FUSED_BACKWARD)
     float* scale = nullptr;  // [M rounded up to 16], zeros past M
 };
 
@@ -38,29 +38,28 @@ __global__ __launch_bounds__(256) void k_copy_scale(const float* __restrict__ fr
 void release(dense_fused* h)
 {
     (void)hipFree(h->P);
-    (void)hipFree(h->Pt);
-    (void)hipFree(h->scale);
     delete h;
 }
+
+int in_eights(const int8_t* Q, int32_t K) { return aligned_to(Q, 8) && K % 8 == 0; }
 
 hipError_t lay_out(const int8_t* Q, const float* scale, bool backward, dense_fused* h)
 {
     const int64_t bytes = spk::fused_packed_bytes(h->M, h->K), bytes_t = spk::fused_packed_bytes(h->K, h->M);
     const int padded = (int)spk::fused_pad(h->M, spk::kFusedTile);
-    hipError_t e = hipMalloc(&h->P, (size_t)bytes);
-    if (e == hipSuccess && backward)
-        e = hipMalloc(&h->Pt, (size_t)bytes_t);
-    if (e == hipSuccess)
-        e = hipMalloc(&h->scale, padded * sizeof(float));
+    hipError_t e = hipMalloc(&h->P, (size_t)(bytes + (backward ? bytes_t : 0) + padded * (int64_t)sizeof(float)));
     if (e == hipSuccess)
         e = hipDeviceSynchronize();  // Q may still be in flight on any stream
     if (e != hipSuccess)
         return e;
+    h->Pt = backward ? h->P + bytes : nullptr;
+    h->scale = reinterpret_cast<float*>(h->P + bytes + (backward ? bytes_t : 0));
+    const int eights = in_eights(Q, h->K);
     hipLaunchKernelGGL(spk::k_fused_pack<false>, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, nullptr, Q,
-                       h->K, h->M, h->P, bytes / 16);
+                       h->K, h->M, h->P, bytes / 16, eights);
     if (backward)
         hipLaunchKernelGGL(spk::k_fused_pack<true>, dim3((unsigned)((bytes_t / 16 + 255) / 256)), dim3(256), 0, nullptr,
-                           Q, h->K, h->M, h->Pt, bytes_t / 16);
+                           Q, h->K, h->M, h->Pt, bytes_t / 16, eights);
     hipLaunchKernelGGL(k_copy_scale, dim3((unsigned)((padded + 255) / 256)), dim3(256), 0, nullptr, scale, h->M,
                        h->scale, padded);
     if ((e = hipGetLastError()) != hipSuccess)
@@ -80,8 +79,8 @@ int check_device(int want)
 
 constexpr int kCUs = 256;
 
-// Rows up to which a call reads the activations straight from memory.
-constexpr int kFewRows = 32;
+// Up to here a call reads the activations straight from memory.
+constexpr int kFewRows = FUSED_FEW_ROWS;
 
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
 void launch_tile(FusedArgs a, hipStream_t st)
@@ -90,7 +89,9 @@ void launch_tile(FusedArgs a, hipStream_t st)
     a.row_tiles = (a.B + 16 * NT * WN - 1) / (16 * NT * WN);
     const int64_t total = (int64_t)a.out_tiles * a.row_tiles * a.splits;
     constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D>();
-    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D>), dim3((unsigned)((total + 7) / 8 * 8)),
+    static_assert(64 * WM * WN == 256, "the workgroups that sum a bias gradient are of this size too");
+    const int64_t sums = a.bias_sums.dbias ? (a.bias_sums.M + 63) / 64 : 0;
+    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D>), dim3((unsigned)((total + 7) / 8 * 8 + sums)),
                        dim3(64 * WM * WN), lds, st, a);
 }
 
@@ -458,9 +459,11 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
                 : launch_gate<spk::f16, 2>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
         }
     }
-    if (dbias)
-        hipLaunchKernelGGL(spk::k_fused_bias, dim3((unsigned)((h->M + 63) / 64)), dim3(256), 0, st, partial, parts, h->M,
-                           dbias);
+    // the bias gradient's parts are summed beside the product of many rows, else by themselves
+    const spk::BiasArgs sums{partial, parts, h->M, dbias};
+    const bool beside = dx && B > kFewRows;
+    if (dbias && !beside)
+        hipLaunchKernelGGL(spk::k_fused_bias, dim3((unsigned)((h->M + 63) / 64)), dim3(256), 0, st, sums);
     if (dx && B > 0) {
         FusedArgs a{};
         // the rows of g * scale are padded with zeros, as the weights are
@@ -468,6 +471,8 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         a.x = workspace, a.ld_x = plane_stride(h->M), a.plane = plane_stride(h->M) * B, a.B = B;
         a.y = dx, a.y_type = x_type, a.ld_y = ld_dx;
         a.vec_out = whole(dx, x_type, ld_dx);
+        if (beside)
+            a.bias_sums = sums;
         // the workspace: g * scale, the parts of the bias gradient, the sums of a split product
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M) +
                                                spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));

@@ -25,10 +25,12 @@ inline int64_t fused_packed_bytes(int64_t n_out, int64_t n_in)
     return fused_pad(n_out, kFusedTile) * fused_pad(n_in, kFusedStep);
 }
 
-// Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns.
+// Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns.  `eights`:
+// rows start on 8-byte boundaries and K is a multiple of 8 (1536 -> 6144: 20 us byte
+// by byte, 5 in eights).
 template <bool TRANSPOSE>
 __global__ __launch_bounds__(256) void k_fused_pack(const int8_t* __restrict__ Q, int K, int M, int8_t* __restrict__ P,
-                                                    int64_t chunks)
+                                                    int64_t chunks, int eights)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= chunks)
@@ -43,6 +45,16 @@ __global__ __launch_bounds__(256) void k_fused_pack(const int8_t* __restrict__ Q
         int8_t b[16];
         u32x4 v;
     } w;
+    if (!TRANSPOSE && eights) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t k = k0 + 32 * h;
+            const u32x2 v = o < n_out && k < n_in ? *reinterpret_cast<const u32x2*>(Q + o * K + k) : u32x2{};
+            w.v[2 * h] = v[0], w.v[2 * h + 1] = v[1];
+        }
+        reinterpret_cast<u32x4*>(P)[i] = w.v;
+        return;
+    }
     for (int j = 0; j < 16; ++j) {
         const int64_t k = k0 + j % 8 + j / 8 * 32;
         w.b[j] = o < n_out && k < n_in ? (TRANSPOSE ? Q[k * K + o] : Q[o * K + k]) : 0;
@@ -272,6 +284,12 @@ __device__ inline void act_slopes(float (&z)[W], int act)
 
 // --- epilogue --------------------------------------------------------------
 
+struct BiasArgs {
+    const float* partial;
+    int parts, M;
+    float* dbias;  // NULL: none
+};
+
 struct FusedArgs {
     const int8_t* P;     // weights, laid out
     int n_out, n_in, steps;
@@ -293,6 +311,7 @@ struct FusedArgs {
     int out_tiles, row_tiles;
     int splits, split_steps;  // the steps go to `splits` workgroups, each writing its sums as FP32 rows at y
     int64_t split_stride;     // elements between their outputs
+    BiasArgs bias_sums;       // workgroups behind the tiles' sum the parts of a bias gradient
 };
 
 // W elements at p: at once where `vec`, else the first n one by one.
@@ -481,6 +500,33 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     columns.store(a, b0 + w % NB * 16 + c, z);
 }
 
+// dbias from its parts (a workgroup of 256 threads: 64 outputs, a quarter of the parts
+// per wave; s_sum: 256 floats of LDS).
+__device__ inline void bias_sums(const BiasArgs& a, int wg, float* s_sum)
+{
+    const int m = min(wg * 64 + (int)threadIdx.x % 64, a.M - 1), w = threadIdx.x / 64;
+    float v = 0.0f;
+    for (int p0 = w; p0 < a.parts; p0 += 4 * 16) {
+        float p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            p[i] = p0 + 4 * i < a.parts ? a.partial[(int64_t)(p0 + 4 * i) * a.M + m] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            v += p[i];
+    }
+    s_sum[threadIdx.x] = v;
+    __syncthreads();
+    if (w == 0 && wg * 64 + (int)threadIdx.x < a.M)
+        a.dbias[m] = (s_sum[threadIdx.x] + s_sum[64 + threadIdx.x]) + (s_sum[128 + threadIdx.x] + s_sum[192 + threadIdx.x]);
+}
+
+__global__ __launch_bounds__(256) void k_fused_bias(BiasArgs a)
+{
+    __shared__ float s_sum[256];
+    bias_sums(a, blockIdx.x, s_sum);
+}
+
 // --- many rows -------------------------------------------------------------
 
 // 16 bytes per lane from `off` of the resource (plus `at`) to LDS at `to` + 16 lane,
@@ -539,6 +585,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     // Neighbouring workgroups of one XCD (every eighth) take tiles of a group
     // of 8 output tiles, so that they share both operands in its L2.
     const int plane_tiles = a.out_tiles * a.row_tiles, total = plane_tiles * a.splits, per_xcd = (total + 7) / 8;
+    if constexpr (kThreads == 256)
+        if (a.bias_sums.dbias && (int)blockIdx.x >= 8 * per_xcd)
+            return bias_sums(a.bias_sums, blockIdx.x - 8 * per_xcd, reinterpret_cast<float*>(s_fused));
     const int place = (int)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if ((int)(blockIdx.x / 8) >= per_xcd || place >= total)
         return;
@@ -790,28 +839,6 @@ __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, in
             v += s_sum[r][threadIdx.x];
         partial[(int64_t)blockIdx.y * M + col] = v;
     }
-}
-
-// dbias from its parts: 64 outputs per workgroup, a quarter of the parts per wave.
-__global__ __launch_bounds__(256) void k_fused_bias(const float* __restrict__ partial, int parts, int M,
-                                                    float* __restrict__ dbias)
-{
-    const int m = min((int)(blockIdx.x * 64 + threadIdx.x % 64), M - 1), w = threadIdx.x / 64;
-    float v = 0.0f;
-    for (int p0 = w; p0 < parts; p0 += 4 * 16) {
-        float p[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            p[i] = p0 + 4 * i < parts ? partial[(int64_t)(p0 + 4 * i) * M + m] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            v += p[i];
-    }
-    __shared__ float s_sum[4][64];
-    s_sum[w][threadIdx.x % 64] = v;
-    __syncthreads();
-    if (w == 0 && (int)(blockIdx.x * 64 + threadIdx.x) < M)
-        dbias[m] = (s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x]) + (s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x]);
 }
 
 }  // namespace spk
