@@ -76,21 +76,65 @@ __device__ inline const T* draft_row(const DraftArgs& a, int s, int row)
                       : static_cast<const T*>(a.draft) + ((int64_t)s * a.G + row - a.G - 1) * a.ld_draft;
 }
 
-// The largest value over a wave, and the sum over it.
+// Reductions over a full wave, every lane getting the result: within quads and rows
+// of 16 by DPP moves, then the four rows' through scalar registers (a chain of
+// shuffles through LDS takes several times as long).
+template <int CTRL>
+__device__ inline int draft_dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
+constexpr int kQuadXor1 = 0xb1, kQuadXor2 = 0x4e, kRowRor4 = 0x124, kRowRor8 = 0x128;
+
+template <int CTRL>
+__device__ inline float draft_dpp(float v) { return __int_as_float(draft_dpp<CTRL>(__float_as_int(v))); }
+
+__device__ inline float draft_row_of(float v, int row) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * row)); }
+
 __device__ inline float draft_wave_max(float v)
 {
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2)
-        v = fmaxf(v, __shfl_xor(v, m));
-    return v;
+    v = fmaxf(v, draft_dpp<kQuadXor1>(v));
+    v = fmaxf(v, draft_dpp<kQuadXor2>(v));
+    v = fmaxf(v, draft_dpp<kRowRor4>(v));
+    v = fmaxf(v, draft_dpp<kRowRor8>(v));
+    return fmaxf(fmaxf(draft_row_of(v, 0), draft_row_of(v, 1)), fmaxf(draft_row_of(v, 2), draft_row_of(v, 3)));
 }
 
 __device__ inline float draft_wave_sum(float v)
 {
+    v += draft_dpp<kQuadXor1>(v);
+    v += draft_dpp<kQuadXor2>(v);
+    v += draft_dpp<kRowRor4>(v);
+    v += draft_dpp<kRowRor8>(v);
+    return (draft_row_of(v, 0) + draft_row_of(v, 1)) + (draft_row_of(v, 2) + draft_row_of(v, 3));
+}
+
+__device__ inline int draft_wave_min(int v)
+{
+    v = min(v, draft_dpp<kQuadXor1>(v));
+    v = min(v, draft_dpp<kQuadXor2>(v));
+    v = min(v, draft_dpp<kRowRor4>(v));
+    v = min(v, draft_dpp<kRowRor8>(v));
+    return min(min(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16)),
+               min(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48)));
+}
+
+template <int CTRL>
+__device__ inline unsigned long long draft_dpp_max(unsigned long long v)
+{
+    const unsigned long long o = (unsigned long long)(uint32_t)draft_dpp<CTRL>((int)(v >> 32)) << 32 | (uint32_t)draft_dpp<CTRL>((int)v);
+    return max(v, o);
+}
+
+__device__ inline unsigned long long draft_wave_max(unsigned long long v)
+{
+    v = draft_dpp_max<kQuadXor1>(v);
+    v = draft_dpp_max<kQuadXor2>(v);
+    v = draft_dpp_max<kRowRor4>(v);
+    v = draft_dpp_max<kRowRor8>(v);
+    unsigned long long r[4];
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2)
-        v += __shfl_xor(v, m);
-    return v;
+    for (int i = 0; i < 4; ++i)
+        r[i] = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 16 * i) << 32 |
+               (uint32_t)__builtin_amdgcn_readlane((int)v, 16 * i);
+    return max(max(r[0], r[1]), max(r[2], r[3]));
 }
 
 // Joins one part per lane: every lane gets the whole.  Only a greedy row needs `at`,
@@ -102,10 +146,7 @@ __device__ inline DraftPart draft_join(const DraftPart& mine, bool greedy, float
     all.at = 0x7fffffff;
     all.sum = 0.0f;
     if (greedy) {
-        all.at = mine.top == all.top ? mine.at : 0x7fffffff;
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2)
-            all.at = min(all.at, __shfl_xor(all.at, m));
+        all.at = draft_wave_min(mine.top == all.top ? mine.at : 0x7fffffff);
     } else {
         all.sum = draft_wave_sum(mine.top == -INFINITY ? 0.0f : mine.sum * draft_term(mine.top, all.top, rate));
     }
@@ -191,9 +232,9 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_stats(DraftArgs a)
     }
 }
 
-// A row's distribution: p(v) = term / sum, or one at `at` (T = 0 and given drafts).
+// A row's distribution: p(v) = term * scale (scale = 1 / sum), or one at `at` (T = 0 and given drafts).
 struct DraftDist {
-    float top, sum;
+    float top, scale;
     int at;
 };
 
@@ -201,7 +242,7 @@ __device__ inline float draft_prob(const DraftDist& d, float x, int v, bool hot,
 {
     if (hot)
         return v == d.at ? 1.0f : 0.0f;
-    return x == -INFINITY ? 0.0f : draft_term(x, d.top, rate) / d.sum;
+    return x == -INFINITY ? 0.0f : draft_term(x, d.top, rate) * d.scale;
 }
 
 // r / noise wins over every p / noise; both are positive, so their bits are ordered as they are.
@@ -217,22 +258,27 @@ template <typename T, int VEC>
 __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
 {
     const int part = blockIdx.x % a.race_parts, s = blockIdx.x / a.race_parts;
-    const int n = draft_count(a, s);
     const int lane = threadIdx.x % 64, w = threadIdx.x / 64;
-    const float temp = a.temperature ? a.temperature[s] : 1.0f;
-    const bool greedy = draft_greedy(temp);
-    const float rate = draft_rate(temp);
     __shared__ DraftDist s_dist[kDraftMaxRows];
     __shared__ float s_p[kDraftMaxRows], s_q[kDraftMaxRows];
     __shared__ int s_draft[kDraftMaxRows];
     __shared__ int s_taken;
-    // draft i is thread i's: its logits are asked for before the rows' sums are joined
+    // Draft i is thread i's.  What does not depend on the decision is asked for at
+    // once: the drafts, their random numbers, and the first stretch of the noise.
     const int mine = threadIdx.x;
-    int d = -1;
-    float u = 0.0f, xt = -INFINITY, xd = -INFINITY;
+    const int d_any = mine < a.G ? a.drafts[(int64_t)s * a.G + mine] : -1;
+    const float u = mine < a.G ? a.uniform[(int64_t)s * a.G + mine] : 0.0f;
+    const float* noise = a.noise + (int64_t)s * a.ld_noise;
+    const int i0 = part * a.race_len + (int)threadIdx.x * 8, i1 = min(a.V, (part + 1) * a.race_len);
+    float ahead[8];
+    draft_load<float, VEC>(noise, i0, i1, ahead);  // past the end: -inf, which never wins
+    const int n = draft_count(a, s);
+    const float temp = a.temperature ? a.temperature[s] : 1.0f;
+    const bool greedy = draft_greedy(temp);
+    const float rate = draft_rate(temp);
+    const int d = mine < n ? d_any : -1;
+    float xt = -INFINITY, xd = -INFINITY;
     if (mine < n) {
-        d = a.drafts[(int64_t)s * a.G + mine];
-        u = a.uniform[(int64_t)s * a.G + mine];
         s_draft[mine] = d;
         if (d >= 0 && d < a.V) {
             xt = (float)draft_row<T>(a, s, mine)[d];
@@ -257,7 +303,7 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
                 break;
             const DraftPart all = draft_join(me[k], greedy, rate);
             if (lane == 0)
-                s_dist[row] = DraftDist{all.top, all.sum, all.top == -INFINITY ? -1 : all.at};
+                s_dist[row] = DraftDist{all.top, 1.0f / all.sum, all.top == -INFINITY ? -1 : all.at};
         }
     }
     __syncthreads();
@@ -283,11 +329,13 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
     const DraftDist dp = s_dist[j];
     const DraftDist dq = !minus ? DraftDist{0.0f, 1.0f, -1} : draft ? s_dist[a.G + 1 + j] : DraftDist{0.0f, 1.0f, s_draft[j]};
     const bool hot_q = greedy || !draft;
-    const float* noise = a.noise + (int64_t)s * a.ld_noise;
     unsigned long long best = 0;
-    const int i1 = min(a.V, (part + 1) * a.race_len);
-    for (int i = part * a.race_len + (int)threadIdx.x * 8; i < i1; i += kDraftBlock * 8) {
+    for (int i = i0; i < i1; i += kDraftBlock * 8) {
         float x[8], y[8], e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            e[k] = ahead[k];
+        draft_load<float, VEC>(noise, i + kDraftBlock * 8, i1, ahead);
         draft_load<T, VEC>(target, i, i1, x);
         if (draft) {
             draft_load<T, VEC>(draft, i, i1, y);
@@ -296,20 +344,16 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
             for (int k = 0; k < 8; ++k)
                 y[k] = -INFINITY;
         }
-        draft_load<float, VEC>(noise, i, i1, e);  // past the end: -inf, which never wins
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            if (!(e[k] > 0.0f))
-                continue;
             const int v = i + k;
             const float p = draft_prob(dp, x[k], v, greedy, rate);
             const float r = p - draft_prob(dq, y[k], v, hot_q, rate);
-            best = max(best, draft_code((r > 0.0f ? r : p) / e[k], v, r > 0.0f));
+            const float score = (r > 0.0f ? r : p) * __builtin_amdgcn_rcpf(e[k]);
+            best = max(best, e[k] > 0.0f ? draft_code(score, v, r > 0.0f) : 0ull);
         }
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2)
-        best = max(best, (unsigned long long)__shfl_xor(best, m));
+    best = draft_wave_max(best);
     __shared__ unsigned long long s_best[kDraftBlock / 64];
     __shared__ int s_last;
     if (lane == 0)
