@@ -331,7 +331,8 @@ __device__ inline void read_w(const T* p, float (&v)[W], bool vec, int n)
     }
 }
 
-template <typename T, int W>
+// (STREAM: past the caches)
+template <typename T, int W, bool STREAM = false>
 __device__ inline void write_w(T* p, const float (&v)[W], bool vec, int n)
 {
     typedef T tw __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
@@ -340,7 +341,10 @@ __device__ inline void write_w(T* p, const float (&v)[W], bool vec, int n)
 #pragma unroll
         for (int e = 0; e < W; ++e)
             r[e] = (T)in_fp32<T>(v[e]);
-        *reinterpret_cast<tw*>(p) = r;
+        if constexpr (STREAM)
+            __builtin_nontemporal_store(r, reinterpret_cast<tw*>(p));
+        else
+            *reinterpret_cast<tw*>(p) = r;
     } else {
 #pragma unroll
         for (int e = 0; e < W; ++e)
@@ -349,11 +353,11 @@ __device__ inline void write_w(T* p, const float (&v)[W], bool vec, int n)
     }
 }
 
-template <typename T, int W>
+template <typename T, int W, bool STREAM>
 __device__ inline void put_outputs(const FusedArgs& a, int m, int64_t b, float (&z)[W], bool vec, int n, int64_t y_at)
 {
     if (a.pre)
-        write_w<T, W>(static_cast<T*>(a.pre) + b * a.ld_pre + m, z, vec, n);
+        write_w<T, W, STREAM>(static_cast<T*>(a.pre) + b * a.ld_pre + m, z, vec, n);
     act_values<W>(z, a.act);
     if (a.residual) {
         float r[W];
@@ -362,7 +366,7 @@ __device__ inline void put_outputs(const FusedArgs& a, int m, int64_t b, float (
         for (int e = 0; e < W; ++e)
             z[e] += r[e];
     }
-    write_w<T, W>(static_cast<T*>(a.y) + y_at + b * a.ld_y + m, z, vec, n);
+    write_w<T, W, STREAM>(static_cast<T*>(a.y) + y_at + b * a.ld_y + m, z, vec, n);
 }
 
 // Outputs m .. m + W - 1, a multiple of W: their scales and biases, read once
@@ -385,6 +389,7 @@ struct OutputColumns {
     }
 
     // y_at: elements from y's start to the rows
+    template <bool STREAM = false>
     __device__ inline void store(const FusedArgs& a, int64_t b, float (&z)[W], int64_t y_at = 0) const
     {
         if (b >= a.B || n <= 0)
@@ -400,9 +405,9 @@ struct OutputColumns {
                 z[e] += bias[e];
         }
         switch (a.y_type) {
-        case SPIKE_TYPE_F32: return put_outputs<float, W>(a, m, b, z, vec, n, y_at);
-        case SPIKE_TYPE_BF16: return put_outputs<bf16, W>(a, m, b, z, vec, n, y_at);
-        default: return put_outputs<f16, W>(a, m, b, z, vec, n, y_at);
+        case SPIKE_TYPE_F32: return put_outputs<float, W, STREAM>(a, m, b, z, vec, n, y_at);
+        case SPIKE_TYPE_BF16: return put_outputs<bf16, W, STREAM>(a, m, b, z, vec, n, y_at);
+        default: return put_outputs<f16, W, STREAM>(a, m, b, z, vec, n, y_at);
         }
     }
 };
@@ -570,7 +575,9 @@ constexpr int fused_tile_lds()
 // lies at c ^ (r % 8) (the lanes' global chunks are exchanged), so that an
 // operand read's rows fall into different banks.  At the end each wave turns its
 // sums around in LDS, 32 rows at a time, so that they leave as whole vectors of
-// neighbouring outputs.
+// neighbouring outputs, past the caches, where they would only push the operands out
+// (16,384 rows of 6144, BF16, and the values before the activation: 341 us through the
+// caches, 321 past them; 2500 rows 52.7 and 51.4).
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
 {
@@ -580,7 +587,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     constexpr int kLoads = NS * kChunks + MT;      // of a wave and step
     static_assert(kChunks >= 1 && kRows * 8 % kThreads == 0, "every thread fetches whole chunks");
     static_assert(NT % 2 == 0, "sums are turned around in pairs of row tiles");
-    static_assert((D - 2) * kLoads < 64, "the load counter holds what is in flight");
+    // From three stages on, the next step's is there one step early, and is read into
+    // registers while this step's is multiplied.
+    constexpr bool kEarly = D >= 3;
+    constexpr int kBehind = kEarly ? (D - 3) * kLoads : 0;  // loads that may be on their way at a wait
+    static_assert(kBehind < 64, "the load counter holds what is in flight");
     extern __shared__ u32x4 s_fused[];
     // Neighbouring workgroups of one XCD (every eighth) take tiles of a group
     // of 8 output tiles, so that they share both operands in its L2.
@@ -647,7 +658,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
 #pragma unroll
     for (int s = 0; s < D - 1; ++s)
         fetch(s, s);
-    wait_loads<(D - 2) * kLoads>();
+    wait_loads<kBehind>();
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         wt[t] = s_w[t * 64];
@@ -659,48 +670,93 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     // operand two items ahead is read.  A wave issues in order, so only work between
     // two products runs beside them: the order is pinned.
     constexpr int kHalf = NT * NS, kItems = 2 * kHalf;
+    // (waves that multiply go before the waves of another workgroup that store)
+    __builtin_amdgcn_s_setprio(1);
     int cur = 0;
-    for (int s = 0; s < steps; ++s) {
-        const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
-        const u32x4* const s_x = s_fused + cur * (kStage / 16) + (wn * NT * 16 + c) * 8;
-        const int c0 = g ^ (c % 8), c1 = (4 + g) ^ (c % 8);
-        u32x4 xo[3];
-        auto read = [&](int item) __attribute__((always_inline)) {
-            const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
-            return s_x[p * kRows * 8 + n * 128 + (h == 0 ? c0 : c1)];
-        };
-        xo[0] = read(0);
-        xo[1] = read(1);
-        fetch(last, s + D - 1);
-        __builtin_amdgcn_sched_barrier(0);
+    const int c0 = g ^ (c % 8), c1 = (4 + g) ^ (c % 8);
+    auto read = [&](int stage, int item) __attribute__((always_inline)) {
+        const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
+        return s_fused[stage * (kStage / 16) + ((p * kRows + (wn * NT + n) * 16 + c) * 8 + (h == 0 ? c0 : c1))];
+    };
+    if constexpr (kEarly) {
+        // all of the next step's operands and codes are read while this step's are multiplied
+        u32x4 xs[2][kItems], ws[2][MT];
 #pragma unroll
-        for (int item = 0; item < kItems; ++item) {
-            const int h = item / kHalf, in_half = item % kHalf;
-            if (item + 2 < kItems)
-                xo[(item + 2) % 3] = read(item + 2);
-            if (item == kHalf) {
-                // this wave's part of the next stage is there: its weights are its own
-                wait_loads<(D - 2) * kLoads>();
+        for (int item = 0; item < kItems; ++item)
+            xs[0][item] = read(0, item);
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-                    wt[t] = s_w[next * (kStage / 16) + t * 64];
-            }
+        for (int t = 0; t < MT; ++t)
+            ws[0][t] = wt[t];
+        auto step = [&](auto parity, int s) __attribute__((always_inline)) {
+            constexpr int q = decltype(parity)::value;
+            const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-                acc[t][in_half / NS] = mfma16<OT>(wo[h][t], xo[item % 3], acc[t][in_half / NS]);
-                // a share of the 4 MT registers of the next half (of the next step, one item late: its codes are on their way)
+            for (int t = 0; t < MT; ++t)
+                ws[1 - q][t] = s_w[next * (kStage / 16) + t * 64];
 #pragma unroll
-                for (int v = 0; v < 4 * MT; ++v) {
-                    const int slot = h == 0 ? v * kHalf / 4 : MT + v * (kHalf - 1) / 4;
-                    if (slot == in_half * MT + t)
-                        wo[1 - h][v / 4][v % 4] = widen_pair<OT>(wt[v / 4][(h == 0 ? 2 : 0) + v % 4 / 2], v % 2);
+            for (int item = 0; item < kItems; ++item)
+                xs[1 - q][item] = read(next, item);
+            fetch(last, s + D - 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int item = 0; item < kItems; ++item) {
+                const int h = item / kHalf, in_half = item % kHalf;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    acc[t][in_half / NS] = mfma16<OT>(wo[h][t], xs[q][item], acc[t][in_half / NS]);
+#pragma unroll
+                    for (int v = 0; v < 4 * MT; ++v)
+                        if (v * kHalf / 4 == in_half * MT + t)
+                            wo[1 - h][v / 4][v % 4] = widen_pair<OT>(h == 0 ? ws[q][v / 4][2 + v % 4 / 2] : ws[1 - q][v / 4][v % 4 / 2], v % 2);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
+            cur = next;
+            wait_loads<kBehind>();
+            __syncthreads();
+        };
+        for (int s = 0; s < steps; s += 2) {  // (a step past the last multiplies zeros)
+            step(std::integral_constant<int, 0>{}, s);
+            step(std::integral_constant<int, 1>{}, s + 1);
         }
-        cur = next;
-        __syncthreads();
+    } else {
+        for (int s = 0; s < steps; ++s) {
+            const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
+            u32x4 xo[3];
+            xo[0] = read(cur, 0);
+            xo[1] = read(cur, 1);
+            fetch(last, s + D - 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int item = 0; item < kItems; ++item) {
+                const int h = item / kHalf, in_half = item % kHalf;
+                if (item + 2 < kItems)
+                    xo[(item + 2) % 3] = read(cur, item + 2);
+                if (item == kHalf) {
+                    // this wave's part of the next stage is there: its weights are its own
+                    wait_loads<0>();
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+                        wt[t] = s_w[next * (kStage / 16) + t * 64];
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    acc[t][in_half / NS] = mfma16<OT>(wo[h][t], xo[item % 3], acc[t][in_half / NS]);
+                    // a share of the 4 MT registers of the next half (of the next step, one item late: its codes are on their way)
+#pragma unroll
+                    for (int v = 0; v < 4 * MT; ++v) {
+                        const int slot = h == 0 ? v * kHalf / 4 : MT + v * (kHalf - 1) / 4;
+                        if (slot == in_half * MT + t)
+                            wo[1 - h][v / 4][v % 4] = widen_pair<OT>(wt[v / 4][(h == 0 ? 2 : 0) + v % 4 / 2], v % 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            cur = next;
+            __syncthreads();
+        }
     }
+    __builtin_amdgcn_s_setprio(0);
     // the zeros fetched past the last step have landed everywhere before LDS is used anew
     wait_loads<0>();
     __syncthreads();
@@ -726,7 +782,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
             const f32x4 lo = s_out[r * 4 * MT + (q ^ (r % 16 % (4 * MT)))];
             const f32x4 hi = s_out[r * 4 * MT + ((q + 1) ^ (r % 16 % (4 * MT)))];
             float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            columns.store(a, b0 + (wn * NT + n0) * 16 + r, z, y_at);
+            columns.template store<true>(a, b0 + (wn * NT + n0) * 16 + r, z, y_at);
         }
         __builtin_amdgcn_wave_barrier();
     }
