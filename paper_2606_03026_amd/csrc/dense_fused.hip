@@ -82,57 +82,59 @@ constexpr int kCUs = 256;
 // Up to here a call reads the activations straight from memory.
 constexpr int kFewRows = FUSED_FEW_ROWS;
 
-template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
+template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
 void launch_tile(FusedArgs a, hipStream_t st)
 {
     a.out_tiles = (a.n_out + 16 * MT * WM - 1) / (16 * MT * WM);
     a.row_tiles = (a.B + 16 * NT * WN - 1) / (16 * NT * WN);
     const int64_t total = (int64_t)a.out_tiles * a.row_tiles * a.splits;
-    constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D>();
-    static_assert(64 * WM * WN == 256, "the workgroups that sum a bias gradient are of this size too");
+    constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D, KS>();
+    static_assert(64 * WM * WN >= 256, "a workgroup can sum a bias gradient too");
     const int64_t sums = a.bias_sums.dbias ? (a.bias_sums.M + 63) / 64 : 0;
-    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D>), dim3((unsigned)((total + 7) / 8 * 8 + sums)),
-                       dim3(64 * WM * WN), lds, st, a);
+    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D, KS>), dim3((unsigned)((total + 7) / 8 * 8 + sums)),
+                       dim3(64 * WM * WN * KS), lds, st, a);
 }
 
-// A tile shape of k_fused_tile, and what a step of 64 inputs of one of its
-// tiles takes: `alone` on its compute unit (latency), and `among` others that
-// keep the unit busy (throughput), in us.
+// A tile shape of k_fused_tile (its outputs and rows, the teams that share its steps)
+// and what it takes, in us: `fixed` for a call, and for a step of 64 inputs `alone` where
+// a compute unit has one tile, `among` for each where it has several.
 struct TileShape {
-    int outs, rows;
-    float alone, among;
+    int outs, rows, teams;
+    float fixed, alone, among;
 };
 
-// Measured over 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 33 to 8192 rows:
-// BF16 and F16 (one plane), FP32 (three).
-constexpr TileShape kShapes1[] = {
-    {256, 128, 0.79f, 0.95f}, {128, 128, 0.58f, 0.50f}, {128, 64, 0.35f, 0.34f}, {64, 64, 0.28f, 0.209f}, {64, 32, 0.22f, 0.131f}};
-constexpr TileShape kShapes3[] = {{256, 64, 1.03f, 1.22f}, {128, 32, 0.42f, 0.43f}, {64, 32, 0.34f, 0.285f}};
+// Measured over 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 33 to 4096 rows: BF16
+// and F16 (one plane), FP32 (three).
+constexpr TileShape kShapes1[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 128, 1, 4.2f, 0.55f, 0.50f},
+                                  {128, 64, 1, 4.5f, 0.32f, 0.34f},  {64, 64, 1, 3.8f, 0.25f, 0.206f},
+                                  {128, 64, 2, 5.5f, 0.24f, 0.44f},  {64, 32, 2, 3.9f, 0.14f, 0.156f},
+                                  {64, 32, 4, 4.7f, 0.10f, 0.24f}};
+constexpr TileShape kShapes3[] = {
+    {256, 64, 1, 8.1f, 1.09f, 1.16f}, {128, 32, 1, 6.6f, 0.40f, 0.40f}, {64, 32, 1, 5.9f, 0.31f, 0.27f}, {64, 32, 2, 6.7f, 0.21f, 0.34f}};
 
 struct TilePlan {
     int shape, splits;
 };
 
-// The shape, and the workgroups that share a tile's steps, with the least
-// estimated time: steps of the tiles that come to one compute unit, and for a
-// split the join (a launch, and the FP32 sums written and read at 3.9 MB/us).
-// What the estimate stands for, in us at 1536 inputs, BF16: 1536 outputs and 64 rows
-// 8.7 in tiles of 64 x 32, 25 in 256 x 128; 6144 outputs and 2500 rows 98 and 51. With
-// 6144 inputs, 1536 outputs and 64 rows 24.6 in one part, 14 in four; with 2500
-// rows 59 in one, 80 in two.
+// The shape, and the workgroups that share a tile's steps, with the least estimated
+// time: the steps of the tiles that come to one compute unit, and for a split the join
+// (a launch, and the FP32 sums written and read at 3.9 MB/us).  What that decides
+// between, BF16, in us: 1536 -> 1536, 64 rows: 7.1 in tiles of 64 x 32 by four teams, 8.2 by one,
+// 26 in 256 x 128; 1536 -> 6144, 2500 rows: 94 in 64 x 32, 48 in 256 x 128; 6144 -> 1536, 33
+// rows: 14.2 in one part, 13.1 in four; with 1024 rows 30.7 by two teams, 43 in four parts.
 TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
 {
     const TileShape* shapes = ns == 1 ? kShapes1 : kShapes3;
-    const int n = ns == 1 ? 5 : 3;
+    const int n = ns == 1 ? 7 : 4;
     const float parts = ns == 2 ? 2.0f / 3.0f : 1.0f;
     TilePlan best{0, 1};
     float least = 0.0f;
     for (int i = 0; i < n; ++i)
         for (int splits = 1; splits <= 8 && (splits == 1 || steps / splits >= 8); ++splits) {
-            const int64_t tiles = (((int64_t)n_out + shapes[i].outs - 1) / shapes[i].outs) *
-                                  (((int64_t)B + shapes[i].rows - 1) / shapes[i].rows) * splits;
-            const float per_unit = (float)((tiles + kCUs - 1) / kCUs) * shapes[i].among;
-            float us = (float)((steps + splits - 1) / splits) * parts * std::max(shapes[i].alone, per_unit);
+            const TileShape& t = shapes[i];
+            const int64_t tiles = (((int64_t)n_out + t.outs - 1) / t.outs) * (((int64_t)B + t.rows - 1) / t.rows) * splits;
+            const int64_t each = (tiles + kCUs - 1) / kCUs;
+            float us = t.fixed + (float)((steps + splits - 1) / splits) * parts * (each == 1 ? t.alone : (float)each * t.among);
             if (splits > 1)
                 us += 3.5f + (float)splits * (float)B * (float)n_out * (4.0f / 3.9e6f);
             if ((i == 0 && splits == 1) || us < least)
@@ -164,17 +166,20 @@ void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
     }
     if constexpr (NS == 1) {
         switch (p.shape) {
-        case 0: launch_tile<OT, NS, 4, 8, 4, 1, 2>(t, st); break;
-        case 1: launch_tile<OT, NS, 2, 8, 4, 1, 2>(t, st); break;
-        case 2: launch_tile<OT, NS, 2, 4, 4, 1, 4>(t, st); break;
-        case 3: launch_tile<OT, NS, 1, 4, 4, 1, 4>(t, st); break;
-        default: launch_tile<OT, NS, 1, 2, 4, 1, 4>(t, st); break;
+        case 0: launch_tile<OT, NS, 4, 8, 4, 1, 2, 1>(t, st); break;
+        case 1: launch_tile<OT, NS, 2, 8, 4, 1, 2, 1>(t, st); break;
+        case 2: launch_tile<OT, NS, 2, 4, 4, 1, 4, 1>(t, st); break;
+        case 3: launch_tile<OT, NS, 1, 4, 4, 1, 4, 1>(t, st); break;
+        case 4: launch_tile<OT, NS, 2, 4, 4, 1, 4, 2>(t, st); break;
+        case 5: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
+        default: launch_tile<OT, NS, 1, 2, 4, 1, 4, 4>(t, st); break;
         }
     } else {
         switch (p.shape) {
-        case 0: launch_tile<OT, NS, 4, 4, 4, 1, 2>(t, st); break;
-        case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4>(t, st); break;
-        default: launch_tile<OT, NS, 1, 2, 4, 1, 4>(t, st); break;
+        case 0: launch_tile<OT, NS, 4, 4, 4, 1, 2, 1>(t, st); break;
+        case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4, 1>(t, st); break;
+        case 2: launch_tile<OT, NS, 1, 2, 4, 1, 4, 1>(t, st); break;
+        default: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
         }
     }
     if (p.splits > 1) {
@@ -243,6 +248,8 @@ void cut_rows(FusedArgs& a, void* workspace, hipStream_t st)
     a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld;
 }
 
+constexpr int64_t kCacheBytes = 256ll << 20;  // of the chip's last cache
+
 // Rows of a workgroup of the gate, and the parts the bias gradient comes in.
 int gate_rows(int32_t B) { return (int)std::max<int64_t>(16, ((int64_t)B + spk::kGateParts - 1) / spk::kGateParts); }
 int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
@@ -265,7 +272,11 @@ void launch_gate(const dense_fused* h, const void* dy, int64_t ld_dy, const void
 {
     const dim3 grid((unsigned)((h->M + spk::kGateCols - 1) / spk::kGateCols), (unsigned)gate_parts(B));
     const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
-    hipLaunchKernelGGL(vec ? (spk::k_fused_gate<T, NS, true>) : (spk::k_fused_gate<T, NS, false>), grid, dim3(256), 0, st,
+    const int64_t moved = ((pre ? 2 : 1) * type_bytes(y_type) + 2 * NS) * (int64_t)B * h->M;
+    const auto gate = !vec                  ? spk::k_fused_gate<T, NS, false, false>
+                      : moved < kCacheBytes ? spk::k_fused_gate<T, NS, true, false>
+                                            : spk::k_fused_gate<T, NS, true, true>;
+    hipLaunchKernelGGL(gate, grid, dim3(256), 0, st,
                        static_cast<const T*>(dy), ld_dy, static_cast<const T*>(pre), ld_pre, act, B, h->M, gate_rows(B),
                        h->scale, static_cast<uint16_t*>(gs), plane_stride(h->M), plane_stride(h->M) * B, partial);
 }

@@ -314,13 +314,17 @@ struct FusedArgs {
     BiasArgs bias_sums;       // workgroups behind the tiles' sum the parts of a bias gradient
 };
 
-// W elements at p: at once where `vec`, else the first n one by one.
-template <typename T, int W>
+// W elements at p: at once where `vec`, else the first n one by one.  (STREAM: past the caches)
+template <typename T, int W, bool STREAM = false>
 __device__ inline void read_w(const T* p, float (&v)[W], bool vec, int n)
 {
     typedef T tw __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
     if (vec) {
-        const tw r = *reinterpret_cast<const tw*>(p);
+        tw r;
+        if constexpr (STREAM)
+            r = __builtin_nontemporal_load(reinterpret_cast<const tw*>(p));
+        else
+            r = *reinterpret_cast<const tw*>(p);
 #pragma unroll
         for (int e = 0; e < W; ++e)
             v[e] = (float)r[e];
@@ -505,13 +509,13 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     columns.store(a, b0 + w % NB * 16 + c, z);
 }
 
-// dbias from its parts (a workgroup of 256 threads: 64 outputs, a quarter of the parts
-// per wave; s_sum: 256 floats of LDS).
+// dbias from its parts (the first 256 threads of a workgroup: 64 outputs, a quarter of
+// the parts per wave; s_sum: 256 floats of LDS).
 __device__ inline void bias_sums(const BiasArgs& a, int wg, float* s_sum)
 {
     const int m = min(wg * 64 + (int)threadIdx.x % 64, a.M - 1), w = threadIdx.x / 64;
     float v = 0.0f;
-    for (int p0 = w; p0 < a.parts; p0 += 4 * 16) {
+    for (int p0 = w; w < 4 && p0 < a.parts; p0 += 4 * 16) {
         float p[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -520,7 +524,8 @@ __device__ inline void bias_sums(const BiasArgs& a, int wg, float* s_sum)
         for (int i = 0; i < 16; ++i)
             v += p[i];
     }
-    s_sum[threadIdx.x] = v;
+    if (w < 4)
+        s_sum[threadIdx.x] = v;
     __syncthreads();
     if (w == 0 && wg * 64 + (int)threadIdx.x < a.M)
         a.dbias[m] = (s_sum[threadIdx.x] + s_sum[64 + threadIdx.x]) + (s_sum[128 + threadIdx.x] + s_sum[192 + threadIdx.x]);
@@ -559,11 +564,12 @@ __device__ inline uint32_t lds_address(const void* p)
 template <int NS, int MT, int NT, int WM, int WN>
 constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * MT * 1024; }
 
-template <int NS, int MT, int NT, int WM, int WN, int D>
+template <int NS, int MT, int NT, int WM, int WN, int D, int KS>
 constexpr int fused_tile_lds()
 {
-    constexpr int ring = D * fused_stage_bytes<NS, MT, NT, WM, WN>(), turning = WM * WN * 2 * 16 * 16 * MT * 4;
-    return ring > turning ? ring : turning;
+    constexpr int rings = KS * D * fused_stage_bytes<NS, MT, NT, WM, WN>();
+    constexpr int joining = (KS - 1) * WM * WN * MT * NT * 1024, turning = WM * WN * 2 * 16 * 16 * MT * 4;
+    return rings > joining + turning ? rings : joining + turning;
 }
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
@@ -578,10 +584,13 @@ constexpr int fused_tile_lds()
 // neighbouring outputs, past the caches, where they would only push the operands out
 // (16,384 rows of 6144, BF16, and the values before the activation: 341 us through the
 // caches, 321 past them; 2500 rows 52.7 and 51.4).
-template <typename OT, int NS, int MT, int NT, int WM, int WN, int D>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
+// KS groups of these waves share the steps, each with a ring of its own, and the first
+// adds up their sums: where there are fewer tiles than compute units, one group leaves
+// most of its unit's issue slots empty.
+template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
 {
-    constexpr int kThreads = 64 * WM * WN, kRows = 16 * NT * WN;
+    constexpr int kThreads = 64 * WM * WN, kRows = 16 * NT * WN;  // threads of a group
     constexpr int kChunks = kRows * 8 / kThreads;  // 16-byte chunks of a plane that a thread fetches per step
     constexpr int kStage = fused_stage_bytes<NS, MT, NT, WM, WN>();
     constexpr int kLoads = NS * kChunks + MT;      // of a wave and step
@@ -596,9 +605,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     // Neighbouring workgroups of one XCD (every eighth) take tiles of a group
     // of 8 output tiles, so that they share both operands in its L2.
     const int plane_tiles = a.out_tiles * a.row_tiles, total = plane_tiles * a.splits, per_xcd = (total + 7) / 8;
-    if constexpr (kThreads == 256)
-        if (a.bias_sums.dbias && (int)blockIdx.x >= 8 * per_xcd)
-            return bias_sums(a.bias_sums, blockIdx.x - 8 * per_xcd, reinterpret_cast<float*>(s_fused));
+    if (a.bias_sums.dbias && (int)blockIdx.x >= 8 * per_xcd)
+        return bias_sums(a.bias_sums, blockIdx.x - 8 * per_xcd, reinterpret_cast<float*>(s_fused));
     const int place = (int)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if ((int)(blockIdx.x / 8) >= per_xcd || place >= total)
         return;
@@ -606,8 +614,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     const int group = id / (8 * a.row_tiles), in_group = min(8, a.out_tiles - group * 8);
     const int out_tile = group * 8 + id % (8 * a.row_tiles) % in_group;
     const int row_tile = id % (8 * a.row_tiles) / in_group;
-    const int first = split * a.split_steps, steps = min(a.split_steps, a.steps - first);
-    const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int team = KS == 1 ? 0 : wave / (WM * WN), w = KS == 1 ? wave : wave % (WM * WN);
+    const int tid = KS == 1 ? (int)threadIdx.x : (int)threadIdx.x % kThreads;
+    // every team walks `walk` steps; it has `steps` of them
+    const int mine = min(a.split_steps, a.steps - split * a.split_steps), walk = (mine + KS - 1) / KS;
+    const int first = min(split * a.split_steps + team * walk, a.steps - 1), steps = min(walk, mine - team * walk);
     const int g = lane / 16, c = lane % 16;
     const int wm = w % WM, wn = w / WM;
     const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
@@ -623,14 +635,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
 #pragma unroll
     for (int p = 0; p < NS; ++p)
         xr[p] = rows_resource(static_cast<const uint16_t*>(a.x) + p * a.plane + b0 * a.ld_x);
-    const int chunk = threadIdx.x % 8 ^ threadIdx.x / 8 % 8;
+    const int chunk = tid % 8 ^ tid / 8 % 8;
     uint32_t x_off[kChunks];  // bytes, of this thread's chunk of step 0
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const int64_t r = min((int64_t)(i * (kThreads / 8) + threadIdx.x / 8), a.B - 1 - b0);
+        const int64_t r = min((int64_t)(i * (kThreads / 8) + tid / 8), a.B - 1 - b0);
         x_off[i] = (uint32_t)(r * a.ld_x + first * kFusedStep + 8 * chunk) * 2u;
     }
-    const uint32_t lds = lds_address(s_fused);
+    u32x4* const s_ring = s_fused + team * D * (kStage / 16);
+    const uint32_t lds = lds_address(s_ring);
     constexpr int kWeights = NS * kRows * 128;  // of a stage: where the waves' weights begin
     // Step s of this workgroup's to stage `buf`; past the last, and past a row's end, zeros.
     auto fetch = [&](int buf, int s) __attribute__((always_inline)) {
@@ -654,7 +667,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
         for (int n = 0; n < NT; ++n)
             acc[t][n] = f32x4{};
     u32x4 wt[MT], wo[2][MT];  // a step's codes; the operands of its two halves
-    const u32x4* const s_w = s_fused + kWeights / 16 + w * MT * 64 + lane;
+    const u32x4* const s_w = s_ring + kWeights / 16 + w * MT * 64 + lane;
 #pragma unroll
     for (int s = 0; s < D - 1; ++s)
         fetch(s, s);
@@ -676,7 +689,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     const int c0 = g ^ (c % 8), c1 = (4 + g) ^ (c % 8);
     auto read = [&](int stage, int item) __attribute__((always_inline)) {
         const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
-        return s_fused[stage * (kStage / 16) + ((p * kRows + (wn * NT + n) * 16 + c) * 8 + (h == 0 ? c0 : c1))];
+        return s_ring[stage * (kStage / 16) + ((p * kRows + (wn * NT + n) * 16 + c) * 8 + (h == 0 ? c0 : c1))];
     };
     if constexpr (kEarly) {
         // all of the next step's operands and codes are read while this step's are multiplied
@@ -715,12 +728,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
             wait_loads<kBehind>();
             __syncthreads();
         };
-        for (int s = 0; s < steps; s += 2) {  // (a step past the last multiplies zeros)
+        for (int s = 0; s < walk; s += 2) {  // (a step past the last multiplies zeros)
             step(std::integral_constant<int, 0>{}, s);
             step(std::integral_constant<int, 1>{}, s + 1);
         }
     } else {
-        for (int s = 0; s < steps; ++s) {
+        for (int s = 0; s < walk; ++s) {
             const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
             u32x4 xo[3];
             xo[0] = read(cur, 0);
@@ -760,9 +773,31 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_fused_tile(FusedArgs a)
     // the zeros fetched past the last step have landed everywhere before LDS is used anew
     wait_loads<0>();
     __syncthreads();
+    if constexpr (KS > 1) {
+        f32x4* const s_join = reinterpret_cast<f32x4*>(s_fused) + (w * MT * NT) * 64 + lane;
+        constexpr int kTeam = WM * WN * MT * NT * 64;
+        if (team > 0) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    s_join[(team - 1) * kTeam + (t * NT + n) * 64] = acc[t][n];
+        }
+        __syncthreads();
+        if (team > 0)
+            return;
+#pragma unroll
+        for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    acc[t][n] += s_join[k * kTeam + (t * NT + n) * 64];
+    }
     // 32 rows x 16 MT outputs at a time, in this wave's own part of LDS; the
     // 16-byte chunk q of row r lies at q ^ (r % (4 MT))
-    f32x4* const s_out = reinterpret_cast<f32x4*>(s_fused) + w * 2 * 16 * 4 * MT;
+    // (behind the other teams' sums)
+    f32x4* const s_out = reinterpret_cast<f32x4*>(s_fused) + (KS - 1) * WM * WN * MT * NT * 64 + w * 2 * 16 * 4 * MT;
     constexpr int kVecs = 2 * MT;  // of 8 outputs, in a row
     static_assert(64 % kVecs == 0, "a lane keeps its outputs");
     const int q = lane % kVecs * 2;
@@ -845,7 +880,10 @@ __global__ __launch_bounds__(256) void k_fused_cut(const XT* __restrict__ x, int
 constexpr int kGateCols = 256;
 constexpr int kGateParts = 256;  // the most parts that the bias gradient comes in
 
-template <typename T, int NS, bool VEC>
+// STREAM: dy and pre are read past the caches, which then keep gs for the product
+// (8192 rows with the product behind: 201 us without, 191 with; 500 rows, whose inputs
+// the caches still hold from the forward pass, 45 and 47).
+template <typename T, int NS, bool VEC, bool STREAM>
 __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ pre,
                                                     int64_t ld_pre, int act, int B, int M, int rows,
                                                     const float* __restrict__ scale, uint16_t* __restrict__ gs,
@@ -862,9 +900,9 @@ __global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, in
     if (n > 0)
         for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
             float g[8], slope[8] = {};
-            read_w<T, 8>(dy + b * ld_dy + m, g, full, n);
+            read_w<T, 8, STREAM>(dy + b * ld_dy + m, g, full, n);
             if (act)
-                read_w<T, 8>(pre + b * ld_pre + m, slope, full, n);
+                read_w<T, 8, STREAM>(pre + b * ld_pre + m, slope, full, n);
             act_slopes<8>(slope, act);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {

@@ -20,7 +20,7 @@ import pytest
 import torch
 
 from oracle import step_oracle as so
-from tests.launches import kernels
+from tests.launches import launches
 
 pytestmark = pytest.mark.gpu
 
@@ -366,25 +366,79 @@ def test_nothing_is_left_from_the_call_before(sp, xk, K, B):
     h.close()
 
 
-# one shape per kernel form: few rows with 1, 2 and 4 tiles of outputs (and two of
-# rows), every tile shape, products split over workgroups, cut activations or not
-FORMS = [("k_fused_rows", 100, 4000, 9), ("k_fused_rows", 72, 33000, 16), ("k_fused_rows", 72, 33000, 20),
-         ("k_fused_tile", 1000, 520, 40), ("k_fused_tile", 328, 1000, 700), ("k_fused_tile", 264, 2100, 1300),
-         ("k_fused_tile", 136, 4100, 2600), ("k_fused_join", 6000, 130, 50), ("k_fused_join", 4104, 520, 200)]
+# sizes that take each kernel form: few rows by 1, 2 and 4 tiles of outputs (and two of
+# rows); every tile shape (the template's tiles per wave, waves, stages and teams), with
+# the steps in one part and in several
+FEW = [(200, 100, 9), (100, 4200, 9), (72, 33000, 16), (72, 33000, 20)]
+ONE_PLANE = [((4, 8, 4, 1, 2, 1), 1104, 4100, 3800, False), ((2, 8, 4, 1, 2, 1), 72, 4100, 1300, False),
+             ((2, 4, 4, 1, 4, 1), 456, 384, 2752, False), ((1, 4, 4, 1, 4, 1), 72, 4100, 100, False),
+             ((1, 4, 4, 1, 4, 1), 6000, 2100, 40, True), ((2, 4, 4, 1, 4, 2), 1000, 2100, 520, False),
+             ((1, 2, 4, 1, 4, 2), 72, 70, 40, False), ((1, 2, 4, 1, 4, 2), 6000, 70, 40, True),
+             ((1, 2, 4, 1, 4, 4), 2000, 70, 40, False), ((1, 2, 4, 1, 4, 4), 6000, 70, 1300, True)]
+THREE_PLANES = [((4, 4, 4, 1, 2, 1), 72, 4100, 2600, False), ((4, 4, 4, 1, 2, 1), 2000, 2100, 520, True),
+                ((2, 2, 4, 1, 4, 1), 328, 4100, 100, False), ((2, 2, 4, 1, 4, 1), 6000, 2100, 40, True),
+                ((1, 2, 4, 1, 4, 1), 72, 70, 40, False), ((1, 2, 4, 1, 4, 1), 2000, 70, 40, True),
+                ((1, 2, 4, 1, 4, 2), 1000, 70, 40, False), ((1, 2, 4, 1, 4, 2), 6000, 70, 40, True)]
 
 
-@pytest.mark.parametrize("kernel,K,M,B", FORMS)
-@pytest.mark.parametrize("xk,yk", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
-def test_every_form(sp, kernel, K, M, B, xk, yk):
-    p = problem(K, M, B, integer=True)
-    h = handle(sp, p)
-    x, y = dev(p["x"], xk), torch.empty((B, M), device="cuda")
+def kernel_names(sp, h, x, y):
     ws = torch.empty(max(1, sp.dense_fused_forward_workspace_bytes(h, x)), dtype=torch.uint8, device="cuda")
-    used = kernels(lambda st: sp.dense_fused_forward(h, x, y, workspace=ws, stream=st))
-    assert any(k.startswith(kernel) for k in used), used
-    assert ("k_fused_cut" in [k.split("<")[0] for k in used]) == (B > 32 and (xk == "f32" or K % 8 != 0))
+    return [name for name, _, _ in launches(lambda st: sp.dense_fused_forward(h, x, y, workspace=ws, stream=st))]
+
+
+def check_integers(sp, h, p, xk, yk):
     for pad, offset in ((0, 0), (1, 1)):
         (x, y, z), want, want_z = forward(sp, h, p, xk, yk, act="relu", pre=True, pad=pad, offset=offset)
-        assert torch.equal(y.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[yk])), used
-        assert torch.equal(z.cpu(), torch.from_numpy(want_z.astype(np.float32)).to(TYPES[yk])), used
+        assert torch.equal(y.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[yk]))
+        assert torch.equal(z.cpu(), torch.from_numpy(want_z.astype(np.float32)).to(TYPES[yk]))
+
+
+@pytest.mark.parametrize("K,M,B", FEW)
+@pytest.mark.parametrize("xk,yk", [("f32", "f32"), ("bf16", "bf16"), ("f16", "f32")])
+def test_few_rows(sp, K, M, B, xk, yk):
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p)
+    names = kernel_names(sp, h, dev(p["x"], xk), torch.empty((B, M), device="cuda"))
+    assert len(names) == 1 and "k_fused_rows" in names[0]
+    check_integers(sp, h, p, xk, yk)
+    h.close()
+
+
+@pytest.mark.parametrize("xk,shape,K,M,B,split", [(xk, *c) for xk in ("bf16", "f16") for c in ONE_PLANE if xk == "bf16" or c[3] < 3000]
+                         + [("f32", *c) for c in THREE_PLANES])
+def test_every_tile_shape(sp, xk, shape, K, M, B, split):
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p)
+    names = kernel_names(sp, h, dev(p["x"], xk), torch.empty((B, M), device="cuda"))
+    planes = 3 if xk == "f32" else 1
+    assert any("k_fused_tile" in n and "".join(f"Li{v}E" for v in (planes, *shape)) in n for n in names), names
+    assert any("k_fused_join" in n for n in names) == split
+    assert any("k_fused_cut" in n for n in names) == (xk == "f32")
+    check_integers(sp, h, p, xk, "f32")
+    h.close()
+
+
+def test_rows_that_fill_no_chunk_are_cut_too(sp):
+    """16-bit rows of an odd length, or off 16-byte boundaries, go through a plane."""
+    for K, pad, offset in ((101, 0, 0), (96, 1, 0), (96, 0, 1)):
+        p = problem(K, 64, 50, integer=True)
+        h = handle(sp, p)
+        x = dev(p["x"], "bf16", pad, offset)
+        y = torch.empty((50, 64), device="cuda")
+        assert any("k_fused_cut" in n for n in kernel_names(sp, h, x, y))
+        sp.dense_fused_forward(h, x, y)
+        torch.cuda.synchronize()
+        assert torch.equal(y.cpu(), torch.from_numpy(so.fused_pre(p["Q"], p["scale"], p["x"]).astype(np.float32)))
+        h.close()
+
+
+@pytest.mark.parametrize("yk", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("K,M,B", [(70, 72, 40), (2000, 300, 90), (300, 6000, 333), (520, 2100, 700)])
+def test_backward_forms(sp, yk, K, M, B):
+    """Products of one, two and three planes in several shapes, split and not, the bias gradient summed beside them."""
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p, backward=True)
+    dx, db, (want, wb, _) = backward(sp, h, p, "f32", yk, "none")
+    assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)))
+    assert (db.cpu().numpy() == wb).all()
     h.close()
