@@ -185,9 +185,8 @@ void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
     if (p.splits > 1) {
         t = a;
         t.splits = p.splits;
-        const int64_t ld = spk::fused_pad(a.n_out, 8), groups = ld / 8 * a.B;
-        hipLaunchKernelGGL(spk::k_fused_join, dim3((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16)), dim3(256), 0,
-                           st, t, part, ld);
+        const int64_t ld = spk::fused_pad(a.n_out, 8);
+        hipLaunchKernelGGL(spk::k_fused_join, spk::row_grid(a.B, ld / 8), dim3(256), 0, st, t, part, ld);
     }
 }
 
@@ -240,11 +239,10 @@ int64_t planes_bytes(int ns, int32_t B, int32_t n) { return spk::fused_pad(ns * 
 template <typename XT, int NS>
 void cut_rows(FusedArgs& a, void* workspace, hipStream_t st)
 {
-    const int64_t ld = plane_stride(a.n_in), groups = ld / 8 * a.B;
+    const int64_t ld = plane_stride(a.n_in);
     uint16_t* out = static_cast<uint16_t*>(workspace);
-    hipLaunchKernelGGL((spk::k_fused_cut<XT, NS>), dim3((unsigned)std::min<int64_t>((groups + 255) / 256, 1 << 16)), dim3(256),
-                       0, st, static_cast<const XT*>(a.x), a.ld_x, a.B, a.n_in, ld, ld * a.B, out,
-                       (int)whole(a.x, NS == 3 ? SPIKE_TYPE_F32 : SPIKE_TYPE_BF16, a.ld_x));
+    hipLaunchKernelGGL((spk::k_fused_cut<XT, NS>), spk::row_grid(a.B, ld / 8), dim3(256), 0, st,
+                       static_cast<const XT*>(a.x), a.ld_x, a.B, a.n_in, ld, ld * a.B, out, (int)whole(a.x, NS == 3 ? SPIKE_TYPE_F32 : SPIKE_TYPE_BF16, a.ld_x));
     a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld;
 }
 

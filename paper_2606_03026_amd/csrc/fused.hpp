@@ -823,23 +823,33 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     }
 }
 
-// Joins the sums of a product whose steps were split: 8 outputs per thread, the
-// parts in ascending order, then the epilogue.  part: [splits][B] rows of ld elements.
+// The two kernels below walk rows of vectors of 8: a wave along a row, the four waves
+// of a workgroup on rows of their own.
+inline dim3 row_grid(int64_t rows, int64_t vectors)
+{
+    const int64_t along = (vectors + 63) / 64, down = (rows + 3) / 4;
+    return dim3((unsigned)along, (unsigned)(down < 65535 ? down : 65535));
+}
+
+// Joins the sums of a product whose steps were split, the parts in ascending order,
+// then the epilogue.  part: [splits][B] rows of ld elements.
 __global__ __launch_bounds__(256) void k_fused_join(FusedArgs a, const float* __restrict__ part, int64_t ld)
 {
-    const int64_t groups = ld / 8, stride = ld * a.B;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups * a.B; i += (int64_t)gridDim.x * 256) {
-        const int64_t b = i / groups;
-        const int m = (int)(i % groups) * 8;
-        f32x8 sum = load8(part + b * ld + m);
-        for (int p = 1; p < a.splits; ++p)
-            sum += load8(part + p * stride + b * ld + m);
+    const int m = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
+    if (m >= ld)
+        return;
+    const int64_t stride = ld * a.B;
+    OutputColumns<8> columns;
+    columns.load(a, m);
+    for (int64_t b = blockIdx.y * 4 + threadIdx.x / 64; b < a.B; b += gridDim.y * 4) {
+        const float* p = part + b * ld + m;
+        f32x8 sum = load8(p);
+        for (int k = 1; k < a.splits; ++k)
+            sum += load8(p + k * stride);
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             z[e] = sum[e];
-        OutputColumns<8> columns;
-        columns.load(a, m);
         columns.store(a, b, z);
     }
 }
@@ -850,14 +860,15 @@ template <typename XT, int NS>
 __global__ __launch_bounds__(256) void k_fused_cut(const XT* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
                                                    int64_t plane, uint16_t* __restrict__ out, int vec)
 {
-    const int64_t groups = ld / 8;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < groups * B; i += (int64_t)gridDim.x * 256) {
-        const int64_t b = i / groups;
-        const int k = (int)(i % groups) * 8;
+    const int k = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
+    if (k >= ld)
+        return;
+    for (int64_t b = blockIdx.y * 4 + threadIdx.x / 64; b < B; b += gridDim.y * 4) {
         const XT* p = x + b * ld_x + k;
         if constexpr (NS == 1) {  // 16-bit rows as they are
             const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
             uint32_t r[4];
+#pragma unroll
             for (int e = 0; e < 4; ++e)
                 r[e] = (k + 2 * e < n ? h[2 * e] : 0u) | (k + 2 * e + 1 < n ? (uint32_t)h[2 * e + 1] << 16 : 0u);
             *reinterpret_cast<u32x4*>(out + b * ld + k) = u32x4{r[0], r[1], r[2], r[3]};
