@@ -337,11 +337,15 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
 
 // Joins the partial sums of the rows that several runs share: the wave of the
 // run in which such a row begins adds the following runs' sums to its own.
+// Workgroups from join_wgs on zero rows that no token names.
 template <typename TD, int VEC>
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __restrict__ keys, int T, int D, int run,
                                                             float scale, int accumulate, TD* __restrict__ dtable,
-                                                            int64_t ld_table, const float* __restrict__ partial)
+                                                            int64_t ld_table, const float* __restrict__ partial,
+                                                            int join_wgs, FillArgs fill)
 {
+    if ((int)blockIdx.x >= join_wgs)
+        return zero_unnamed_rows(fill, blockIdx.x - join_wgs, keys, T);
     const int blocks = (D + 64 * VEC - 1) / (64 * VEC), lane = threadIdx.x % 64;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
     const int r = unit / blocks;

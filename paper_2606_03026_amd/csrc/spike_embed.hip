@@ -24,7 +24,11 @@ int run_length(int32_t T) { return T <= 4096 ? 8 : 16; }
 
 static_assert(32 <= spk::kMaxRun, "a run's keys lie along a wave");
 
-constexpr int64_t kFillBesideSort = 128ll << 20, kFillBesideMerge = 48ll << 20;
+// Of the table's zeros, the bytes written beside the merging, the sums and their
+// joining (a smaller table's shares below); the rest goes beside the sorting.  A
+// 352 MB table's gradient, 2,500 tokens: 70 us, with nothing beside the joining and
+// 128 MB beside the sorting 71; 16,384 tokens: 82 and 85.
+constexpr int64_t kFillBesideMerge = 48ll << 20, kFillBesideSums = 160ll << 20, kFillBesideJoin = 32ll << 20;
 
 bool rows_vectorize(const void* p, int type, int64_t ld, int32_t D)
 {
@@ -129,7 +133,7 @@ template <typename TG>
 constexpr int vector_of() { return sizeof(TG) == 4 ? 4 : 8; }
 
 template <typename TG, typename TD, int VEC>
-void launch_grad(const Grad& a, const spk::FillArgs& fill)
+void launch_grad(const Grad& a, const spk::FillArgs& fill, const spk::FillArgs& with_join)
 {
     constexpr int waves = spk::kEmbedBlock / 64;
     const int run = run_length(a.T);
@@ -142,19 +146,19 @@ void launch_grad(const Grad& a, const spk::FillArgs& fill)
                            static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.D, run, (int)sum_wgs,
                            a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, fill);
     if (runs > 1)
-        hipLaunchKernelGGL((spk::k_embed_join<TD, VEC>), dim3((unsigned)sum_wgs), dim3(spk::kEmbedBlock), 0, a.st,
-                           a.ws.keys, a.T, a.D, run, a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table,
-                           a.ws.partial);
+        hipLaunchKernelGGL((spk::k_embed_join<TD, VEC>), dim3((unsigned)(sum_wgs + spk::fill_wgs(with_join))),
+                           dim3(spk::kEmbedBlock), 0, a.st, a.ws.keys, a.T, a.D, run, a.scale, a.accumulate,
+                           static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, (int)sum_wgs, with_join);
 }
 
 template <typename TG>
-void grad_table(const Grad& a, int table_type, bool vec, const spk::FillArgs& fill)
+void grad_table(const Grad& a, int table_type, bool vec, const spk::FillArgs& fill, const spk::FillArgs& with_join)
 {
     constexpr int V = vector_of<TG>();
     switch (table_type) {
-    case SPIKE_TYPE_F32: return vec ? launch_grad<TG, float, V>(a, fill) : launch_grad<TG, float, 1>(a, fill);
-    case SPIKE_TYPE_BF16: return vec ? launch_grad<TG, spk::bf16, V>(a, fill) : launch_grad<TG, spk::bf16, 1>(a, fill);
-    default: return vec ? launch_grad<TG, spk::f16, V>(a, fill) : launch_grad<TG, spk::f16, 1>(a, fill);
+    case SPIKE_TYPE_F32: return vec ? launch_grad<TG, float, V>(a, fill, with_join) : launch_grad<TG, float, 1>(a, fill, with_join);
+    case SPIKE_TYPE_BF16: return vec ? launch_grad<TG, spk::bf16, V>(a, fill, with_join) : launch_grad<TG, spk::bf16, 1>(a, fill, with_join);
+    default: return vec ? launch_grad<TG, spk::f16, V>(a, fill, with_join) : launch_grad<TG, spk::f16, 1>(a, fill, with_join);
     }
 }
 
@@ -250,6 +254,8 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
     const int64_t elem = type_bytes(table_type);
     spk::FillArgs fill{static_cast<char*>(dtable), ld_table * elem, D * elem, 0, accumulate ? 0 : V,
                        (int)rows_vectorize(dtable, table_type, ld_table, D)};
+    spk::FillArgs with_join = fill;
+    with_join.count = 0;
     if (T > 0) {
         grad_space(T, D, workspace, &a.ws);
         const bool one = T <= spk::kSortChunk;
@@ -257,8 +263,13 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
         uint32_t* k = one ? a.ws.keys : a.ws.chunk_keys;
         int* o = one ? a.ws.order : a.ws.chunk_order;
         // Rows zeroed beside the sorting, before it is known which are named (those are
-        // then written again); the others wait for the sums.
-        const spk::FillArgs with_sort = take_rows(&fill, kFillBesideSort);
+        // then written again); the others go beside the sums and their joining.
+        const int64_t all = fill.count * fill.bytes;
+        if (T > run_length(T))
+            with_join = take_rows(&fill, std::min<int64_t>(kFillBesideJoin, all / 8));
+        const int64_t beside_sums = std::min<int64_t>(kFillBesideSums, all / 2);
+        const int64_t beside_merge = one ? 0 : std::min<int64_t>(kFillBesideMerge, all / 8);
+        const spk::FillArgs with_sort = take_rows(&fill, fill.count * fill.bytes - beside_sums - beside_merge);
         const dim3 block(spk::kEmbedBlock), grid((unsigned)(wgs + spk::fill_wgs(with_sort)));
         if (id_type == SPIKE_TYPE_I64)
             hipLaunchKernelGGL(spk::k_embed_sort<int64_t>, grid, block, 0, a.st, static_cast<const int64_t*>(ids), T, V,
@@ -267,15 +278,15 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
             hipLaunchKernelGGL(spk::k_embed_sort<int32_t>, grid, block, 0, a.st, static_cast<const int32_t*>(ids), T, V,
                                k, o, wgs, with_sort);
         if (!one) {
-            const spk::FillArgs with_merge = take_rows(&fill, kFillBesideMerge);
+            const spk::FillArgs with_merge = take_rows(&fill, beside_merge);
             hipLaunchKernelGGL(spk::k_embed_merge, dim3((unsigned)(wgs + spk::fill_wgs(with_merge))), block, 0, a.st, k, o,
                                T, a.ws.keys, a.ws.order, wgs, with_merge);
         }
     }
     switch (grad_type) {
-    case SPIKE_TYPE_F32: grad_table<float>(a, table_type, vec, fill); break;
-    case SPIKE_TYPE_BF16: grad_table<spk::bf16>(a, table_type, vec, fill); break;
-    default: grad_table<spk::f16>(a, table_type, vec, fill); break;
+    case SPIKE_TYPE_F32: grad_table<float>(a, table_type, vec, fill, with_join); break;
+    case SPIKE_TYPE_BF16: grad_table<spk::bf16>(a, table_type, vec, fill, with_join); break;
+    default: grad_table<spk::f16>(a, table_type, vec, fill, with_join); break;
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "embedding gradient launch");
