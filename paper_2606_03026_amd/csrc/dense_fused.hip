@@ -104,11 +104,14 @@ struct TileShape {
 };
 
 // Measured over 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 33 to 4096 rows: BF16
-// and F16 (one plane), FP32 (three).
+// and F16 (one plane), FP32 activations (two), FP32 gradients (three).
 constexpr TileShape kShapes1[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 128, 1, 4.2f, 0.55f, 0.50f},
                                   {128, 64, 1, 4.5f, 0.32f, 0.34f},  {64, 64, 1, 3.8f, 0.25f, 0.206f},
                                   {128, 64, 2, 5.5f, 0.24f, 0.44f},  {64, 32, 2, 3.9f, 0.14f, 0.156f},
                                   {64, 32, 4, 4.7f, 0.10f, 0.24f}};
+constexpr TileShape kShapes2[] = {{256, 64, 1, 8.4f, 0.96f, 0.90f}, {128, 32, 1, 7.1f, 0.36f, 0.32f},
+                                  {64, 32, 1, 6.4f, 0.29f, 0.203f}, {64, 32, 2, 7.0f, 0.20f, 0.286f},
+                                  {128, 64, 1, 7.7f, 0.74f, 0.46f}};
 constexpr TileShape kShapes3[] = {
     {256, 64, 1, 8.1f, 1.09f, 1.16f}, {128, 32, 1, 6.6f, 0.40f, 0.40f}, {64, 32, 1, 5.9f, 0.31f, 0.27f}, {64, 32, 2, 6.7f, 0.21f, 0.34f}};
 
@@ -124,9 +127,8 @@ struct TilePlan {
 // rows: 14.2 in one part, 13.1 in four; with 1024 rows 30.7 by two teams, 43 in four parts.
 TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
 {
-    const TileShape* shapes = ns == 1 ? kShapes1 : kShapes3;
-    const int n = ns == 1 ? 7 : 4;
-    const float parts = ns == 2 ? 2.0f / 3.0f : 1.0f;
+    const TileShape* shapes = ns == 1 ? kShapes1 : ns == 2 ? kShapes2 : kShapes3;
+    const int n = ns == 1 ? 7 : ns == 2 ? 5 : 4;
     TilePlan best{0, 1};
     float least = 0.0f;
     for (int i = 0; i < n; ++i)
@@ -134,7 +136,7 @@ TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
             const TileShape& t = shapes[i];
             const int64_t tiles = (((int64_t)n_out + t.outs - 1) / t.outs) * (((int64_t)B + t.rows - 1) / t.rows) * splits;
             const int64_t each = (tiles + kCUs - 1) / kCUs;
-            float us = t.fixed + (float)((steps + splits - 1) / splits) * parts * (each == 1 ? t.alone : (float)each * t.among);
+            float us = t.fixed + (float)((steps + splits - 1) / splits) * (each == 1 ? t.alone : (float)each * t.among);
             if (splits > 1)
                 us += 3.5f + (float)splits * (float)B * (float)n_out * (4.0f / 3.9e6f);
             if ((i == 0 && splits == 1) || us < least)
@@ -162,7 +164,7 @@ void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
     t.split_steps = (a.steps + p.splits - 1) / p.splits;
     if (p.splits > 1) {
         t.y = part, t.y_type = SPIKE_TYPE_F32, t.ld_y = spk::fused_pad(a.n_out, 8), t.split_stride = t.ld_y * a.B;
-        t.scale = t.bias = nullptr, t.act = 0, t.residual = t.pre = nullptr, t.vec_out = 1;
+        t.scale = t.row_scale = t.bias = nullptr, t.act = 0, t.residual = t.pre = nullptr, t.vec_out = 1;
     }
     if constexpr (NS == 1) {
         switch (p.shape) {
@@ -179,7 +181,10 @@ void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
         case 0: launch_tile<OT, NS, 4, 4, 4, 1, 2, 1>(t, st); break;
         case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4, 1>(t, st); break;
         case 2: launch_tile<OT, NS, 1, 2, 4, 1, 4, 1>(t, st); break;
-        default: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
+        case 3: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
+        default:
+            if constexpr (NS == 2)
+                launch_tile<OT, NS, 2, 4, 4, 1, 2, 1>(t, st);
         }
     }
     if (p.splits > 1) {
@@ -236,14 +241,31 @@ void few_rows(const FusedArgs& a, bool chunks, hipStream_t st)
 int64_t plane_stride(int32_t n) { return spk::fused_pad(n, 8); }
 int64_t planes_bytes(int ns, int32_t B, int32_t n) { return spk::fused_pad(ns * plane_stride(n) * B * 2, 16); }
 
-template <typename XT, int NS>
+// What forward prepares x into: FP32 rows into two F16 planes and their scales; rows of
+// 16-bit elements that do not go in chunks into ones that do.
+int64_t prepared_bytes(int x_type, bool chunks, int32_t B, int32_t n)
+{
+    if (x_type == SPIKE_TYPE_F32)
+        return planes_bytes(2, B, n) + spk::fused_pad((int64_t)B * 4, 16);
+    return chunks ? 0 : planes_bytes(1, B, n);
+}
+
 void cut_rows(FusedArgs& a, void* workspace, hipStream_t st)
 {
     const int64_t ld = plane_stride(a.n_in);
-    uint16_t* out = static_cast<uint16_t*>(workspace);
-    hipLaunchKernelGGL((spk::k_fused_cut<XT, NS>), spk::row_grid(a.B, ld / 8), dim3(256), 0, st,
-                       static_cast<const XT*>(a.x), a.ld_x, a.B, a.n_in, ld, ld * a.B, out, (int)whole(a.x, NS == 3 ? SPIKE_TYPE_F32 : SPIKE_TYPE_BF16, a.ld_x));
-    a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld;
+    float* undo = reinterpret_cast<float*>(static_cast<char*>(workspace) + planes_bytes(2, a.B, a.n_in));
+    hipLaunchKernelGGL(spk::k_fused_cut, dim3((unsigned)std::min(a.B, 1 << 20)), dim3(256), 0, st,
+                       static_cast<const float*>(a.x), a.ld_x, a.B, a.n_in, ld, ld * a.B, static_cast<uint16_t*>(workspace),
+                       undo, (int)whole(a.x, SPIKE_TYPE_F32, a.ld_x));
+    a.x = workspace, a.ld_x = ld, a.plane = ld * a.B, a.n_in = (int)ld, a.row_scale = undo;
+}
+
+void align_rows(FusedArgs& a, void* workspace, hipStream_t st)
+{
+    const int64_t ld = plane_stride(a.n_in);
+    hipLaunchKernelGGL(spk::k_fused_align, spk::row_grid(a.B, ld / 8), dim3(256), 0, st, static_cast<const uint16_t*>(a.x),
+                       a.ld_x, a.B, a.n_in, ld, static_cast<uint16_t*>(workspace));
+    a.x = workspace, a.ld_x = ld, a.n_in = (int)ld;
 }
 
 constexpr int64_t kCacheBytes = 256ll << 20;  // of the chip's last cache
@@ -344,9 +366,9 @@ int64_t dense_fused_forward_workspace_bytes(dense_fused_t h, const void* x, int3
         return -1;
     if (B <= kFewRows)
         return 0;
-    const int ns = x_type == SPIKE_TYPE_F32 ? 3 : 1;
+    const int ns = x_type == SPIKE_TYPE_F32 ? 2 : 1;
     const int64_t sums = split_bytes(tile_plan(ns, B, h->M, (h->K + spk::kFusedStep - 1) / spk::kFusedStep), B, h->M);
-    return sums + (ns == 1 && in_chunks(x, x_type, ld_x, h->K) ? 0 : planes_bytes(ns, B, h->K));
+    return sums + prepared_bytes(x_type, in_chunks(x, x_type, ld_x, h->K), B, h->K);
 }
 
 int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t ld_x, int32_t B, const float* bias,
@@ -388,15 +410,14 @@ int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t 
         default: few_rows<spk::f16, 1>(a, chunks, st); break;
         }
     } else {
-        // first the planes where x has to be cut, then the sums of a split product
-        const int ns = x_type == SPIKE_TYPE_F32 ? 3 : 1;
-        float* part = static_cast<float*>(workspace);
-        if (ns == 3 || !chunks) {
-            part = reinterpret_cast<float*>(static_cast<char*>(workspace) + planes_bytes(ns, B, h->K));
-            ns == 3 ? cut_rows<float, 3>(a, workspace, st) : cut_rows<uint16_t, 1>(a, workspace, st);
-        }
+        // the workspace: x prepared where it has to be, then the sums of a split product
+        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + prepared_bytes(x_type, chunks, B, h->K));
+        if (x_type == SPIKE_TYPE_F32)
+            cut_rows(a, workspace, st);
+        else if (!chunks)
+            align_rows(a, workspace, st);
         switch (x_type) {
-        case SPIKE_TYPE_F32: launch_planes<spk::bf16, 3>(a, part, st); break;
+        case SPIKE_TYPE_F32: launch_planes<spk::f16, 2>(a, part, st); break;
         case SPIKE_TYPE_BF16: launch_planes<spk::bf16, 1>(a, part, st); break;
         default: launch_planes<spk::f16, 1>(a, part, st); break;
         }

@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void k_fused_pack(const int8_t* __restrict__ Q
 
 // --- values ----------------------------------------------------------------
 
-// Operand types of the matrix instructions: activations in BF16 parts, or F16 as they are.
+// Operand types of the matrix instructions where rows are few: activations in BF16 parts, or F16 as they are.
 template <typename XT> struct Operand { typedef bf16 type; };
 template <> struct Operand<f16> { typedef f16 type; };
 
@@ -298,6 +298,7 @@ struct FusedArgs {
     int64_t plane;       // elements between the planes of cut activations
     int B;
     const float* scale;  // NULL: one
+    const float* row_scale;  // of cut FP32 activations: what undoes a row's scaling
     const float* bias;
     int act;
     const void* residual;
@@ -561,6 +562,10 @@ __device__ inline uint32_t lds_address(const void* p)
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
+// Two F16 planes: FP32 activations, their rows scaled.
+template <typename OT, int NS>
+constexpr bool kScaled = __is_same(OT, f16) && NS == 2;
+
 template <int NS, int MT, int NT, int WM, int WN>
 constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * MT * 1024; }
 
@@ -573,8 +578,8 @@ constexpr int fused_tile_lds()
 }
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
-// activations are NS planes of 16-bit parts (BF16 or F16 rows as they are, or
-// FP32 ones cut in three), rows of ld_x elements at 16-byte boundaries, n_in a
+// activations are NS planes of 16-bit parts (BF16 or F16 rows as they are, FP32
+// ones cut in two scaled F16 planes, gradients in up to three BF16 ones), rows of ld_x elements at 16-byte boundaries, n_in a
 // multiple of 8.  A ring of D stages in LDS holds 64 inputs of the rows and, for
 // each wave, of its weights; a stage is fetched D - 1 steps ahead by loads that
 // need no registers.  A row of a stage is 8 chunks of 16 bytes; chunk c of row r
@@ -794,6 +799,12 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                 for (int n = 0; n < NT; ++n)
                     acc[t][n] += s_join[k * kTeam + (t * NT + n) * 64];
     }
+    float undo[NT];  // a lane's results belong to one row of each tile
+    if constexpr (kScaled<OT, NS>) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            undo[n] = a.row_scale ? a.row_scale[min(b0 + (wn * NT + n) * 16 + c, (int64_t)a.B - 1)] : 1.0f;
+    }
     // 32 rows x 16 MT outputs at a time, in this wave's own part of LDS; the
     // 16-byte chunk q of row r lies at q ^ (r % (4 MT))
     // (behind the other teams' sums)
@@ -810,7 +821,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] = acc[t][n0 + n];
+                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] =
+                    kScaled<OT, NS> ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
         for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
@@ -823,7 +835,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     }
 }
 
-// The two kernels below walk rows of vectors of 8: a wave along a row, the four waves
+// The join, and the copy below, walk rows of vectors of 8: a wave along a row, the four waves
 // of a workgroup on rows of their own.
 inline dim3 row_grid(int64_t rows, int64_t vectors)
 {
@@ -846,36 +858,95 @@ __global__ __launch_bounds__(256) void k_fused_join(FusedArgs a, const float* __
         f32x8 sum = load8(p);
         for (int k = 1; k < a.splits; ++k)
             sum += load8(p + k * stride);
+        const float undo = a.row_scale ? a.row_scale[b] : 1.0f;
         float z[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            z[e] = sum[e];
+            z[e] = sum[e] * undo;
         columns.store(a, b, z);
     }
 }
 
-// Cuts rows of n elements of any type and alignment into NS planes for the
-// product: rows of `ld` (n rounded up to 8) elements, zeros past n.
-template <typename XT, int NS>
-__global__ __launch_bounds__(256) void k_fused_cut(const XT* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
-                                                   int64_t plane, uint16_t* __restrict__ out, int vec)
+// Copies rows of n 16-bit elements at any alignment for the product: rows of `ld`
+// (n rounded up to 8) elements, zeros past n.
+__global__ __launch_bounds__(256) void k_fused_align(const uint16_t* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
+                                                     uint16_t* __restrict__ out)
 {
     const int k = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
     if (k >= ld)
         return;
     for (int64_t b = blockIdx.y * 4 + threadIdx.x / 64; b < B; b += gridDim.y * 4) {
-        const XT* p = x + b * ld_x + k;
-        if constexpr (NS == 1) {  // 16-bit rows as they are
-            const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-            uint32_t r[4];
+        const uint16_t* h = x + b * ld_x + k;
+        uint32_t r[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                r[e] = (k + 2 * e < n ? h[2 * e] : 0u) | (k + 2 * e + 1 < n ? (uint32_t)h[2 * e + 1] << 16 : 0u);
-            *reinterpret_cast<u32x4*>(out + b * ld + k) = u32x4{r[0], r[1], r[2], r[3]};
-        } else {
+        for (int e = 0; e < 4; ++e)
+            r[e] = (k + 2 * e < n ? h[2 * e] : 0u) | (k + 2 * e + 1 < n ? (uint32_t)h[2 * e + 1] << 16 : 0u);
+        *reinterpret_cast<u32x4*>(out + b * ld + k) = u32x4{r[0], r[1], r[2], r[3]};
+    }
+}
+
+// Cuts FP32 rows of n elements into two F16 planes for the product: a row is scaled
+// by the power of two that brings its largest finite size to [2^14, 2^15), then
+// rounded, and what the rounding left is rounded again.  Two roundings to 11 bits
+// keep an element to 2^-23 of itself (one bit less than FP32 holds; the sums' own
+// rounding, 2^-24 of a partial sum per step, is larger) down to 2^-17 of the row's
+// largest, and smaller ones to 2^-40 of that.  Three BF16 planes would keep every
+// bit at any range, for half as much again in the product (1536 -> 6144, 2500 rows:
+// 126 us, against 99; 500 rows 40 and 30).  The planes' rows have `ld`
+// (n rounded up to 8) elements, zeros past n; undo[b] is the power's inverse.
+// An infinite element stays one, with nothing left of it.  A workgroup walks a row,
+// whose first 2,048 elements stay in registers between the two passes.
+__device__ inline float largest_finite(const float (&v)[8], float top)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_fabsf(v[e]);
+        top = x < __builtin_inff() ? fmaxf(top, x) : top;
+    }
+    return top;
+}
+
+__global__ __launch_bounds__(256) void k_fused_cut(const float* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
+                                                   int64_t plane, uint16_t* __restrict__ out, float* __restrict__ undo, int vec)
+{
+    __shared__ float s_top[2][4];
+    int turn = 0;  // rows take turns with s_top, so that one barrier a row is enough
+    for (int64_t b = blockIdx.x; b < B; b += gridDim.x, turn ^= 1) {
+        const float* p = x + b * ld_x;
+        const int k0 = threadIdx.x * 8;
+        float held[8] = {};
+        if (k0 < n)
+            read_w<float, 8>(p + k0, held, vec && k0 + 8 <= n, n - k0);
+        float top = largest_finite(held, 0.0f);
+        for (int k = k0 + 2048; k < n; k += 2048) {
             float v[8];
-            read_w<XT, 8>(p, v, vec && k + 8 <= n, n - k);
-            put_planes<NS>(out + b * ld + k, plane, v);
+            read_w<float, 8>(p + k, v, vec && k + 8 <= n, n - k);
+            top = largest_finite(v, top);
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d /= 2)
+            top = fmaxf(top, __shfl_xor(top, d));
+        if (threadIdx.x % 64 == 0)
+            s_top[turn][threadIdx.x / 64] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(s_top[turn][0], s_top[turn][1]), fmaxf(s_top[turn][2], s_top[turn][3]));
+        // 2^(14 - exponent), at most 2^126 (subnormal rows are then exact all the same)
+        const int shift = min(14 + 127 - (int)(__float_as_uint(top) >> 23), 126);
+        const float factor = __uint_as_float((uint32_t)(127 + shift) << 23);
+        if (threadIdx.x == 0)
+            undo[b] = __uint_as_float((uint32_t)(127 - shift) << 23);
+        for (int k = k0; k < ld; k += 2048) {
+            if (k > k0)
+                read_w<float, 8>(p + k, held, vec && k + 8 <= n, n - k);
+            f16x8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float v = held[e] * factor;
+                hi[e] = (f16)v;
+                lo[e] = (f16)(__builtin_isinf(v) ? 0.0f : v - (float)hi[e]);
+            }
+            *reinterpret_cast<f16x8*>(out + b * ld + k) = hi;
+            *reinterpret_cast<f16x8*>(out + plane + b * ld + k) = lo;
         }
     }
 }

@@ -8,7 +8,7 @@ independent, stay within
 
     lim = 6 u sqrt(n) sum_k |scale Q x|,  n = parts * K + 32
 
-(parts: the BF16 parts of an FP32 activation; 32: waves, scale, bias).  The
+(parts: three BF16 parts of an FP32 activation or gradient at most; 32: waves, scale, bias).  The
 activation adds at most 1e-6 + 4e-7 |y| (its polynomial's 1.7e-7 and ten FP32
 operations), its slope is at most 1.13 in size, and storing rounds by half a
 unit of the type.  In the backward pass each g * scale enters as one BF16
@@ -375,6 +375,11 @@ ONE_PLANE = [((4, 8, 4, 1, 2, 1), 1104, 4100, 3800, False), ((2, 8, 4, 1, 2, 1),
              ((1, 4, 4, 1, 4, 1), 6000, 2100, 40, True), ((2, 4, 4, 1, 4, 2), 1000, 2100, 520, False),
              ((1, 2, 4, 1, 4, 2), 72, 70, 40, False), ((1, 2, 4, 1, 4, 2), 6000, 70, 40, True),
              ((1, 2, 4, 1, 4, 4), 2000, 70, 40, False), ((1, 2, 4, 1, 4, 4), 6000, 70, 1300, True)]
+TWO_PLANES = [((4, 4, 4, 1, 2, 1), 1000, 4100, 2600, False), ((2, 2, 4, 1, 4, 1), 136, 1000, 2600, False),
+              ((2, 2, 4, 1, 4, 1), 6000, 70, 1300, True), ((1, 2, 4, 1, 4, 1), 72, 70, 40, False),
+              ((1, 2, 4, 1, 4, 1), 6000, 2100, 40, True), ((1, 2, 4, 1, 4, 2), 1000, 70, 40, False),
+              ((1, 2, 4, 1, 4, 2), 2000, 70, 40, True), ((2, 4, 4, 1, 2, 1), 72, 4100, 1300, False),
+              ((2, 4, 4, 1, 2, 1), 2000, 2100, 520, True)]
 THREE_PLANES = [((4, 4, 4, 1, 2, 1), 72, 4100, 2600, False), ((4, 4, 4, 1, 2, 1), 2000, 2100, 520, True),
                 ((2, 2, 4, 1, 4, 1), 328, 4100, 100, False), ((2, 2, 4, 1, 4, 1), 6000, 2100, 40, True),
                 ((1, 2, 4, 1, 4, 1), 72, 70, 40, False), ((1, 2, 4, 1, 4, 1), 2000, 70, 40, True),
@@ -405,16 +410,60 @@ def test_few_rows(sp, K, M, B, xk, yk):
 
 
 @pytest.mark.parametrize("xk,shape,K,M,B,split", [(xk, *c) for xk in ("bf16", "f16") for c in ONE_PLANE if xk == "bf16" or c[3] < 3000]
-                         + [("f32", *c) for c in THREE_PLANES])
+                         + [("f32", *c) for c in TWO_PLANES])
 def test_every_tile_shape(sp, xk, shape, K, M, B, split):
     p = problem(K, M, B, integer=True)
     h = handle(sp, p)
     names = kernel_names(sp, h, dev(p["x"], xk), torch.empty((B, M), device="cuda"))
-    planes = 3 if xk == "f32" else 1
+    planes = 2 if xk == "f32" else 1
     assert any("k_fused_tile" in n and "".join(f"Li{v}E" for v in (planes, *shape)) in n for n in names), names
     assert any("k_fused_join" in n for n in names) == split
     assert any("k_fused_cut" in n for n in names) == (xk == "f32")
     check_integers(sp, h, p, xk, "f32")
+    h.close()
+
+
+@pytest.mark.parametrize("shape,K,M,B,split", THREE_PLANES)
+def test_every_tile_shape_of_the_gradient(sp, shape, K, M, B, split):
+    p = problem(M, K, B, integer=True)
+    h = handle(sp, p, backward=True)
+    dy, dx = dev(p["dy"]), torch.empty((B, M), device="cuda")
+    ws = torch.empty(sp.dense_fused_workspace_bytes(h, B, torch.float32), dtype=torch.uint8, device="cuda")
+    names = [n for n, _, _ in launches(lambda st: sp.dense_fused_backward(h, dy, dx=dx, workspace=ws, stream=st))]
+    assert any("k_fused_tile" in n and "".join(f"Li{v}E" for v in (3, *shape)) in n for n in names), names
+    assert any("k_fused_join" in n for n in names) == split
+    dx, _, (want, _, _) = backward(sp, h, p, "f32", "f32", "none", want_bias=False)
+    assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)))
+    h.close()
+
+
+@pytest.mark.parametrize("K", [300, 2060, 5000])
+def test_scaled_rows(sp, K):
+    """FP32 rows of many sizes next to each other, and elements far below their row's largest.
+
+    An element enters the product to 2^-23 of itself or to 2^-40 of its row's largest,
+    whichever is more; the sums' rounding is as above.  The largest meets the code 0
+    in every other output, so that the small ones have to carry those.
+    """
+    p = problem(K, 64, 100)
+    r = np.random.default_rng([17, K])
+    rows = 10.0 ** r.uniform(-36, 30, (100, 1))
+    rows[:6, 0] = 1e-44, 1e-40, 1e-38, 3e-38, 1e30, 0.0
+    below = 2.0 ** -r.uniform(0, 30, (100, 1))
+    at = r.integers(0, K, 100)
+    x = r.uniform(-1, 1, (100, K)) * rows * below
+    x[np.arange(100), at] = rows[:, 0]
+    p["x"] = x.astype(np.float32)
+    p["Q"][::2, :] *= (np.bincount(at, minlength=K) == 0).astype(np.int8)
+    h = handle(sp, p)
+    (xd, y, _), want, want_z = forward(sp, h, p, "f32", "f32", bias=False, residual=False)
+    w = np.abs(p["Q"].astype(np.float64)) * p["scale"].astype(np.float64)[:, None]
+    x64 = np.abs(host(xd))
+    top = x64.max(axis=1, keepdims=True)
+    lim = (6 * U * np.sqrt(2 * K + 32) * (x64 @ w.T) + 2.0 ** -23 * (x64 @ w.T) + 2.0 ** -40 * top * w.sum(axis=1)
+           + U * np.abs(want) + 2.0 ** -149 * 128)
+    got = host(y)
+    assert (np.abs(got - want) <= lim).all(), np.max(np.abs(got - want) / lim)
     h.close()
 
 
@@ -425,7 +474,7 @@ def test_rows_that_fill_no_chunk_are_cut_too(sp):
         h = handle(sp, p)
         x = dev(p["x"], "bf16", pad, offset)
         y = torch.empty((50, 64), device="cuda")
-        assert any("k_fused_cut" in n for n in kernel_names(sp, h, x, y))
+        assert any("k_fused_align" in n for n in kernel_names(sp, h, x, y))
         sp.dense_fused_forward(h, x, y)
         torch.cuda.synchronize()
         assert torch.equal(y.cpu(), torch.from_numpy(so.fused_pre(p["Q"], p["scale"], p["x"]).astype(np.float32)))
