@@ -18,19 +18,18 @@ using spk::aligned_to;
 using spk::fail;
 using spk::hip_fail;
 
-constexpr int kWaveOf8 = spk::kDraftBlock * 8;  // logits of a stretch: 8 a thread
 constexpr int64_t kStatsWgs = 4096, kRaceWgs = 1024;
 
 // Parts a row of V logits is cut into, where `rows` rows are worked on at once
 // and `want` workgroups are to share them; whole stretches of 2,048 logits each.
 void split(int64_t rows, int64_t want, int32_t V, int* parts, int* len)
 {
-    const int64_t stretches = ((int64_t)V + kWaveOf8 - 1) / kWaveOf8;
+    const int64_t stretches = ((int64_t)V + spk::kDraftStretch - 1) / spk::kDraftStretch;
     const int64_t most = std::min<int64_t>(
         {std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)), stretches, (int64_t)spk::kDraftMaxParts});
     const int64_t per = (stretches + most - 1) / most;
     *parts = (int)((stretches + per - 1) / per);
-    *len = (int)std::min<int64_t>(per * kWaveOf8, (int64_t)1 << 30);
+    *len = (int)std::min<int64_t>(per * spk::kDraftStretch, (int64_t)1 << 30);
 }
 
 struct Plan {
@@ -59,11 +58,14 @@ void launch(const spk::DraftArgs& a, hipStream_t st)
 {
     const dim3 block(spk::kDraftBlock), stats((unsigned)((int64_t)a.S * a.rows * a.parts)),
         race((unsigned)((int64_t)a.S * a.race_parts));
-    if (a.part_len <= kWaveOf8)
+    if (a.part_len <= spk::kDraftStretch)
         hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 1>), stats, block, 0, st, a);
     else
-        hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 4>), stats, block, 0, st, a);
-    hipLaunchKernelGGL((spk::k_draft_race<T, VEC>), race, block, 0, st, a);
+        hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 2>), stats, block, 0, st, a);
+    if (a.race_len <= spk::kDraftStretch)
+        hipLaunchKernelGGL((spk::k_draft_race<T, VEC, 1>), race, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((spk::k_draft_race<T, VEC, 2>), race, block, 0, st, a);
 }
 
 bool rows_vectorize(const void* p, int type, int64_t ld) { return aligned_to(p, 16) && ld * spk::type_bytes(type) % 16 == 0; }
