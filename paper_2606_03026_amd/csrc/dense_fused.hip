@@ -104,7 +104,7 @@ struct TileShape {
 };
 
 // Measured over 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 33 to 4096 rows: BF16
-// and F16 (one plane), FP32 activations (two), FP32 gradients (three).
+// and F16 (one plane), FP32 (two).
 constexpr TileShape kShapes1[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 128, 1, 4.2f, 0.55f, 0.50f},
                                   {128, 64, 1, 4.5f, 0.32f, 0.34f},  {64, 64, 1, 3.8f, 0.25f, 0.206f},
                                   {128, 64, 2, 5.5f, 0.24f, 0.44f},  {64, 32, 2, 3.9f, 0.14f, 0.156f},
@@ -112,8 +112,6 @@ constexpr TileShape kShapes1[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 128, 
 constexpr TileShape kShapes2[] = {{256, 64, 1, 8.4f, 0.96f, 0.90f}, {128, 32, 1, 7.1f, 0.36f, 0.32f},
                                   {64, 32, 1, 6.4f, 0.29f, 0.203f}, {64, 32, 2, 7.0f, 0.20f, 0.286f},
                                   {128, 64, 1, 7.7f, 0.74f, 0.46f}};
-constexpr TileShape kShapes3[] = {
-    {256, 64, 1, 8.1f, 1.09f, 1.16f}, {128, 32, 1, 6.6f, 0.40f, 0.40f}, {64, 32, 1, 5.9f, 0.31f, 0.27f}, {64, 32, 2, 6.7f, 0.21f, 0.34f}};
 
 struct TilePlan {
     int shape, splits;
@@ -127,8 +125,8 @@ struct TilePlan {
 // rows: 14.2 in one part, 13.1 in four; with 1024 rows 30.7 by two teams, 43 in four parts.
 TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
 {
-    const TileShape* shapes = ns == 1 ? kShapes1 : ns == 2 ? kShapes2 : kShapes3;
-    const int n = ns == 1 ? 7 : ns == 2 ? 5 : 4;
+    const TileShape* shapes = ns == 1 ? kShapes1 : kShapes2;
+    const int n = ns == 1 ? 7 : 5;
     TilePlan best{0, 1};
     float least = 0.0f;
     for (int i = 0; i < n; ++i)
@@ -182,9 +180,7 @@ void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
         case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4, 1>(t, st); break;
         case 2: launch_tile<OT, NS, 1, 2, 4, 1, 4, 1>(t, st); break;
         case 3: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
-        default:
-            if constexpr (NS == 2)
-                launch_tile<OT, NS, 2, 4, 4, 1, 2, 1>(t, st);
+        default: launch_tile<OT, NS, 2, 4, 4, 1, 2, 1>(t, st); break;
         }
     }
     if (p.splits > 1) {
@@ -268,37 +264,36 @@ void align_rows(FusedArgs& a, void* workspace, hipStream_t st)
     a.x = workspace, a.ld_x = ld, a.n_in = (int)ld;
 }
 
-constexpr int64_t kCacheBytes = 256ll << 20;  // of the chip's last cache
-
 // Rows of a workgroup of the gate, and the parts the bias gradient comes in.
-int gate_rows(int32_t B) { return (int)std::max<int64_t>(16, ((int64_t)B + spk::kGateParts - 1) / spk::kGateParts); }
+int gate_rows(int32_t B)
+{
+    return B <= kFewRows ? 1 : (int)std::max<int64_t>(2, ((int64_t)B + spk::kGateParts - 1) / spk::kGateParts);
+}
 int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 
-// What g * scale is kept in between the gate and the product: planes, or FP32
-// rows where the product takes few of them (BF16: one plane, also then).
-int gate_planes(int y_type, int32_t B)
-{
-    return y_type == SPIKE_TYPE_BF16 ? 1 : B <= kFewRows ? 0 : y_type == SPIKE_TYPE_F32 ? 3 : 2;
-}
-int64_t gate_bytes(int y_type, int32_t B, int32_t M)
+// What g * scale is kept in between the gate and the product: scaled F16 planes and what
+// undoes the scaling, or (0) FP32 rows where the product takes few of them, which it cuts itself.
+int gate_planes(int y_type, int32_t B) { return y_type == SPIKE_TYPE_BF16 ? 1 : B <= kFewRows ? 0 : 2; }
+int64_t gate_plane_bytes(int y_type, int32_t B, int32_t M)
 {
     const int ns = gate_planes(y_type, B);
     return ns == 0 ? spk::fused_pad(plane_stride(M) * B * 4, 16) : planes_bytes(ns, B, M);
 }
+int64_t gate_bytes(int y_type, int32_t B, int32_t M)
+{
+    return gate_plane_bytes(y_type, B, M) + spk::fused_pad((int64_t)B * 4, 16);
+}
 
 template <typename T, int NS>
-void launch_gate(const dense_fused* h, const void* dy, int64_t ld_dy, const void* pre, int64_t ld_pre, int act, int32_t B,
-                 void* gs, float* partial, int y_type, hipStream_t st)
+void launch_gate(spk::GateArgs a, bool vec, hipStream_t st)
 {
-    const dim3 grid((unsigned)((h->M + spk::kGateCols - 1) / spk::kGateCols), (unsigned)gate_parts(B));
-    const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
-    const int64_t moved = ((pre ? 2 : 1) * type_bytes(y_type) + 2 * NS) * (int64_t)B * h->M;
-    const auto gate = !vec                  ? spk::k_fused_gate<T, NS, false, false>
-                      : moved < kCacheBytes ? spk::k_fused_gate<T, NS, true, false>
-                                            : spk::k_fused_gate<T, NS, true, true>;
-    hipLaunchKernelGGL(gate, grid, dim3(256), 0, st,
-                       static_cast<const T*>(dy), ld_dy, static_cast<const T*>(pre), ld_pre, act, B, h->M, gate_rows(B),
-                       h->scale, static_cast<uint16_t*>(gs), plane_stride(h->M), plane_stride(h->M) * B, partial);
+    const bool any = !vec || a.M > 8192;  // else a row's vectors are a workgroup's threads at most
+    a.along = any ? 512 : (a.M + 511) / 512 * 64;
+    a.groups = any ? 1 : std::min(a.rows, std::max(1, 768 / a.along));
+    const auto gate = !vec ? spk::k_fused_gate<T, NS, true, false>
+                      : any ? spk::k_fused_gate<T, NS, true, true>
+                            : spk::k_fused_gate<T, NS, false, true>;
+    hipLaunchKernelGGL(gate, dim3((unsigned)gate_parts(a.B)), dim3(a.along * a.groups), (a.groups - 1) * a.along * 32, st, a);
 }
 
 int check_rows(int32_t B, int32_t act, int x_type, int y_type)
@@ -471,22 +466,20 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         pre = nullptr;
     const int parts = B > 0 ? gate_parts(B) : 0;
     float* partial = nullptr;
+    float* undo = nullptr;
     if (B > 0) {
-        void* gs = dx ? workspace : nullptr;
+        undo = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_plane_bytes(y_type, B, h->M));
         if (dbias)
             partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M));
-        const bool few = B <= kFewRows;
+        spk::GateArgs g{};
+        g.dy = dy, g.ld_dy = ld_dy, g.pre = pre, g.ld_pre = ld_pre, g.act = act, g.B = B, g.M = h->M, g.rows = gate_rows(B);
+        g.scale = h->scale, g.gs = dx ? workspace : nullptr, g.ld_gs = plane_stride(h->M), g.plane = g.ld_gs * B;
+        g.undo = undo, g.partial = partial;
+        const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
         switch (y_type) {
-        case SPIKE_TYPE_F32:
-            few ? launch_gate<float, 0>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st)
-                : launch_gate<float, 3>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
-            break;
-        case SPIKE_TYPE_BF16:
-            launch_gate<spk::bf16, 1>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
-            break;
-        default:
-            few ? launch_gate<spk::f16, 0>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st)
-                : launch_gate<spk::f16, 2>(h, dy, ld_dy, pre, ld_pre, act, B, gs, partial, y_type, st);
+        case SPIKE_TYPE_F32: B <= kFewRows ? launch_gate<float, 0>(g, vec, st) : launch_gate<float, 2>(g, vec, st); break;
+        case SPIKE_TYPE_BF16: launch_gate<spk::bf16, 1>(g, vec, st); break;
+        default: B <= kFewRows ? launch_gate<spk::f16, 0>(g, vec, st) : launch_gate<spk::f16, 2>(g, vec, st); break;
         }
     }
     // the bias gradient's parts are summed beside the product of many rows, else by themselves
@@ -503,14 +496,16 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         a.vec_out = whole(dx, x_type, ld_dx);
         if (beside)
             a.bias_sums = sums;
-        // the workspace: g * scale, the parts of the bias gradient, the sums of a split product
+        // the workspace: g * scale (and its rows' scalings), the parts of the bias gradient, the sums of a split product
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M) +
                                                spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
         const bool few = B <= kFewRows;
+        if (gate_planes(y_type, B) > 0)
+            a.row_scale = undo;
         switch (y_type) {
-        case SPIKE_TYPE_F32: few ? few_rows<float, 3>(a, true, st) : launch_planes<spk::bf16, 3>(a, part, st); break;
-        case SPIKE_TYPE_BF16: few ? few_rows<spk::bf16, 1>(a, true, st) : launch_planes<spk::bf16, 1>(a, part, st); break;
-        default: few ? few_rows<float, 2>(a, true, st) : launch_planes<spk::bf16, 2>(a, part, st); break;
+        case SPIKE_TYPE_F32: few ? few_rows<float, 3>(a, true, st) : launch_planes<spk::f16, 2>(a, part, st); break;
+        case SPIKE_TYPE_BF16: few ? few_rows<spk::f16, 1>(a, true, st) : launch_planes<spk::f16, 1>(a, part, st); break;
+        default: few ? few_rows<float, 2>(a, true, st) : launch_planes<spk::f16, 2>(a, part, st); break;
         }
     }
     const hipError_t e = hipGetLastError();

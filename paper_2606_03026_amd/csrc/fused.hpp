@@ -103,26 +103,62 @@ __device__ inline float below_bf16(float x)
     return FIRST && __builtin_isinf(x) ? 0.0f : r;
 }
 
-// v as NS BF16 parts at p, p + plane, ..: all but the last cut off, that one rounded.
-template <int NS>
-__device__ inline void put_planes(uint16_t* p, int64_t plane, float (&v)[8])
+// Rows of FP32 values enter the product of many rows as NS planes of F16 values: a row is
+// scaled by the power of two that brings its largest size to [2^14, 2^15), then
+// rounded, and what that leaves is rounded again for the second plane.
+__device__ inline float largest(const float (&v)[8], float top)
 {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        u32x4 part;
+    for (int e = 0; e < 8; ++e)
+        top = fmaxf(top, __builtin_fabsf(v[e]));  // (leaves NaN out)
+    return top;
+}
+
+// The power (2^126 at most: rows of subnormals are exact all the same; with an infinite
+// element the one for the largest exponent, so that no other overflows) and its inverse.
+struct RowPower {
+    float factor, undo;
+};
+
+__device__ inline RowPower row_power(float top)
+{
+    const int shift = min(14 + 127 - min((int)(__float_as_uint(top) >> 23), 254), 126);
+    return RowPower{__uint_as_float((uint32_t)(127 + shift) << 23), __uint_as_float((uint32_t)(127 - shift) << 23)};
+}
+
+// The largest over `waves` waves from wave `first` on, that this one is among.  s_top: one of
+// two rows of LDS, taken in turn, so that the workgroup's one barrier is enough.
+__device__ inline float largest_of_waves(float top, float (&s_top)[16], int first, int waves)
+{
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (s + 1 < NS) {
-                part[i] = high_halves(v[2 * i], v[2 * i + 1]);
-                v[2 * i] = s == 0 ? below_bf16<true>(v[2 * i]) : below_bf16<false>(v[2 * i]);
-                v[2 * i + 1] = s == 0 ? below_bf16<true>(v[2 * i + 1]) : below_bf16<false>(v[2 * i + 1]);
-            } else {
-                typedef bf16 b2 __attribute__((ext_vector_type(2)));
-                part[i] = __builtin_bit_cast(uint32_t, b2{(bf16)v[2 * i], (bf16)v[2 * i + 1]});
-            }
-        }
-        *reinterpret_cast<u32x4*>(p + s * plane) = part;
+    for (int d = 32; d > 0; d /= 2)
+        top = fmaxf(top, __shfl_xor(top, d));
+    if (threadIdx.x % 64 == 0)
+        s_top[threadIdx.x / 64] = top;
+    __syncthreads();
+    const int w = threadIdx.x % 16;
+    top = s_top[first + (w < waves ? w : 0)];
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2)
+        top = fmaxf(top, __shfl_xor(top, d));
+    return top;
+}
+
+// 8 values at p (and p + plane).  Of an infinite one nothing is left for the second.
+template <int NS>
+__device__ inline void put_planes(uint16_t* p, int64_t plane, const float (&v)[8], float factor)
+{
+    f16x8 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float x = v[e] * factor;
+        hi[e] = (f16)in_fp32<f16>(x);
+        if (NS > 1)
+            lo[e] = (f16)(__builtin_isinf(x) ? 0.0f : x - (float)hi[e]);
     }
+    *reinterpret_cast<f16x8*>(p) = hi;
+    if (NS > 1)
+        *reinterpret_cast<f16x8*>(p + plane) = lo;
 }
 
 // 8 activations as they were loaded.
@@ -298,7 +334,7 @@ struct FusedArgs {
     int64_t plane;       // elements between the planes of cut activations
     int B;
     const float* scale;  // NULL: one
-    const float* row_scale;  // of cut FP32 activations: what undoes a row's scaling
+    const float* row_scale;  // of rows that were scaled to F16 planes: what undoes that; NULL: one
     const float* bias;
     int act;
     const void* residual;
@@ -315,17 +351,13 @@ struct FusedArgs {
     BiasArgs bias_sums;       // workgroups behind the tiles' sum the parts of a bias gradient
 };
 
-// W elements at p: at once where `vec`, else the first n one by one.  (STREAM: past the caches)
-template <typename T, int W, bool STREAM = false>
+// W elements at p: at once where `vec`, else the first n one by one.
+template <typename T, int W>
 __device__ inline void read_w(const T* p, float (&v)[W], bool vec, int n)
 {
     typedef T tw __attribute__((ext_vector_type(W), aligned(W * sizeof(T) < 16 ? W * sizeof(T) : 16)));
     if (vec) {
-        tw r;
-        if constexpr (STREAM)
-            r = __builtin_nontemporal_load(reinterpret_cast<const tw*>(p));
-        else
-            r = *reinterpret_cast<const tw*>(p);
+        const tw r = *reinterpret_cast<const tw*>(p);
 #pragma unroll
         for (int e = 0; e < W; ++e)
             v[e] = (float)r[e];
@@ -506,8 +538,13 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 #pragma unroll
     for (int v = 1; v < WK; ++v)
         sum += s_sum[v][w][lane];
+    const int64_t b = b0 + w % NB * 16 + c;
+    if constexpr (__is_same(XT, f16)) {
+        if (a.row_scale)
+            sum *= a.row_scale[min(b, (int64_t)a.B - 1)];
+    }
     float z[4] = {sum[0], sum[1], sum[2], sum[3]};
-    columns.store(a, b0 + w % NB * 16 + c, z);
+    columns.store(a, b, z);
 }
 
 // dbias from its parts (the first 256 threads of a workgroup: 64 outputs, a quarter of
@@ -562,10 +599,6 @@ __device__ inline uint32_t lds_address(const void* p)
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-// Two F16 planes: FP32 activations, their rows scaled.
-template <typename OT, int NS>
-constexpr bool kScaled = __is_same(OT, f16) && NS == 2;
-
 template <int NS, int MT, int NT, int WM, int WN>
 constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * MT * 1024; }
 
@@ -579,7 +612,7 @@ constexpr int fused_tile_lds()
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
 // activations are NS planes of 16-bit parts (BF16 or F16 rows as they are, FP32
-// ones cut in two scaled F16 planes, gradients in up to three BF16 ones), rows of ld_x elements at 16-byte boundaries, n_in a
+// ones and gradients in scaled F16 planes), rows of ld_x elements at 16-byte boundaries, n_in a
 // multiple of 8.  A ring of D stages in LDS holds 64 inputs of the rows and, for
 // each wave, of its weights; a stage is fetched D - 1 steps ahead by loads that
 // need no registers.  A row of a stage is 8 chunks of 16 bytes; chunk c of row r
@@ -800,7 +833,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                     acc[t][n] += s_join[k * kTeam + (t * NT + n) * 64];
     }
     float undo[NT];  // a lane's results belong to one row of each tile
-    if constexpr (kScaled<OT, NS>) {
+    if constexpr (__is_same(OT, f16)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             undo[n] = a.row_scale ? a.row_scale[min(b0 + (wn * NT + n) * 16 + c, (int64_t)a.B - 1)] : 1.0f;
@@ -822,7 +855,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
 #pragma unroll
             for (int t = 0; t < MT; ++t)
                 s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] =
-                    kScaled<OT, NS> ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
+                    __is_same(OT, f16) ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
         for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
@@ -885,135 +918,214 @@ __global__ __launch_bounds__(256) void k_fused_align(const uint16_t* __restrict_
     }
 }
 
-// Cuts FP32 rows of n elements into two F16 planes for the product: a row is scaled
-// by the power of two that brings its largest finite size to [2^14, 2^15), then
-// rounded, and what the rounding left is rounded again.  Two roundings to 11 bits
-// keep an element to 2^-23 of itself (one bit less than FP32 holds; the sums' own
-// rounding, 2^-24 of a partial sum per step, is larger) down to 2^-17 of the row's
-// largest, and smaller ones to 2^-40 of that.  Three BF16 planes would keep every
-// bit at any range, for half as much again in the product (1536 -> 6144, 2500 rows:
-// 126 us, against 99; 500 rows 40 and 30).  The planes' rows have `ld`
-// (n rounded up to 8) elements, zeros past n; undo[b] is the power's inverse.
-// An infinite element stays one, with nothing left of it.  A workgroup walks a row,
-// whose first 2,048 elements stay in registers between the two passes.
-__device__ inline float largest_finite(const float (&v)[8], float top)
-{
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float x = __builtin_fabsf(v[e]);
-        top = x < __builtin_inff() ? fmaxf(top, x) : top;
-    }
-    return top;
-}
-
+// Cuts FP32 rows of n elements into two scaled F16 planes for the product.  Two
+// roundings to 11 bits keep an element to 2^-23 of itself (one bit less than FP32
+// holds; the sums' own rounding, 2^-24 of a partial sum per step, is larger) down to
+// 2^-17 of the row's largest, and smaller ones to 2^-40 of that.  Three BF16 planes
+// would keep every bit at any range, for half as much again in the product
+// (1536 -> 6144, 2500 rows: 126 us, against 98; 500 rows 40 and 30).  The planes' rows
+// have `ld` (n rounded up to 8) elements, zeros past n.  A workgroup walks a row, whose
+// first 2,048 elements stay in registers between the two passes; bound by memory
+// (2500 rows of 1536: 7.7 us, 4.0 TB/s read and written).
 __global__ __launch_bounds__(256) void k_fused_cut(const float* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
                                                    int64_t plane, uint16_t* __restrict__ out, float* __restrict__ undo, int vec)
 {
-    __shared__ float s_top[2][4];
-    int turn = 0;  // rows take turns with s_top, so that one barrier a row is enough
+    __shared__ float s_top[2][16];
+    int turn = 0;
     for (int64_t b = blockIdx.x; b < B; b += gridDim.x, turn ^= 1) {
         const float* p = x + b * ld_x;
         const int k0 = threadIdx.x * 8;
         float held[8] = {};
         if (k0 < n)
             read_w<float, 8>(p + k0, held, vec && k0 + 8 <= n, n - k0);
-        float top = largest_finite(held, 0.0f);
+        float top = largest(held, 0.0f);
         for (int k = k0 + 2048; k < n; k += 2048) {
             float v[8];
             read_w<float, 8>(p + k, v, vec && k + 8 <= n, n - k);
-            top = largest_finite(v, top);
+            top = largest(v, top);
         }
-#pragma unroll
-        for (int d = 32; d > 0; d /= 2)
-            top = fmaxf(top, __shfl_xor(top, d));
-        if (threadIdx.x % 64 == 0)
-            s_top[turn][threadIdx.x / 64] = top;
-        __syncthreads();
-        top = fmaxf(fmaxf(s_top[turn][0], s_top[turn][1]), fmaxf(s_top[turn][2], s_top[turn][3]));
-        // 2^(14 - exponent), at most 2^126 (subnormal rows are then exact all the same)
-        const int shift = min(14 + 127 - (int)(__float_as_uint(top) >> 23), 126);
-        const float factor = __uint_as_float((uint32_t)(127 + shift) << 23);
+        const RowPower power = row_power(largest_of_waves(top, s_top[turn], 0, blockDim.x / 64));
         if (threadIdx.x == 0)
-            undo[b] = __uint_as_float((uint32_t)(127 - shift) << 23);
+            undo[b] = power.undo;
         for (int k = k0; k < ld; k += 2048) {
             if (k > k0)
                 read_w<float, 8>(p + k, held, vec && k + 8 <= n, n - k);
-            f16x8 hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = held[e] * factor;
-                hi[e] = (f16)v;
-                lo[e] = (f16)(__builtin_isinf(v) ? 0.0f : v - (float)hi[e]);
-            }
-            *reinterpret_cast<f16x8*>(out + b * ld + k) = hi;
-            *reinterpret_cast<f16x8*>(out + plane + b * ld + k) = lo;
+            put_planes<2>(out + b * ld + k, plane, held, power.factor);
         }
     }
 }
 
 // --- gradient --------------------------------------------------------------
 
-// g = dy act'(z): per workgroup 256 outputs and `rows` rows.  g * scale goes to
-// gs for the product, in NS planes of rows of ld_gs elements (NS = 0: FP32 rows),
-// and the column sums of g over these rows to partial[row block].  Bound by memory:
-// many workgroups of few rows, one row of a thread in flight, so that 8 waves per SIMD
-// hide the loads (8192 rows of 6144, BF16, 302 MB: 65 us with 256 row blocks, 70 with
-// 128, 85 with 32 and four rows of a thread in flight).
-constexpr int kGateCols = 256;
-constexpr int kGateParts = 256;  // the most parts that the bias gradient comes in
+// g = dy act'(z) of 8 outputs, as they were loaded and then as they are.
+template <typename T>
+struct GateRaw {
+    typename Vec8<T>::type dy, z;
+};
 
-// STREAM: dy and pre are read past the caches, which then keep gs for the product
-// (8192 rows with the product behind: 201 us without, 191 with; 500 rows, whose inputs
-// the caches still hold from the forward pass, 45 and 47).
-template <typename T, int NS, bool VEC, bool STREAM>
-__global__ __launch_bounds__(256) void k_fused_gate(const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ pre,
-                                                    int64_t ld_pre, int act, int B, int M, int rows,
-                                                    const float* __restrict__ scale, uint16_t* __restrict__ gs,
-                                                    int64_t ld_gs, int64_t plane, float* __restrict__ partial)
+// (VEC: rows of whole vectors at 16-byte boundaries, up to the last one)
+template <typename T, bool VEC>
+__device__ inline typename Vec8<T>::type gate_load(const T* p, int n)
 {
-    const int m = blockIdx.x * kGateCols + threadIdx.x % 32 * 8;
-    const int64_t b0 = (int64_t)blockIdx.y * rows, b1 = min((int64_t)B, b0 + rows);
-    const int n = M - m;
-    const bool full = VEC && n >= 8;
-    float sc[8], sum[8] = {};
+    typename Vec8<T>::type v = (T)0.0f;
+    if (VEC && n >= 8) {
+        v = *reinterpret_cast<const typename Vec8<T>::type*>(p);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e < n)
+                v[e] = p[e];
+    }
+    return v;
+}
+
+template <typename T, bool VEC>
+__device__ inline GateRaw<T> gate_read(const T* dy, const T* pre, int m, int M, int act)
+{
+    GateRaw<T> r;
+    r.dy = gate_load<T, VEC>(dy + m, M - m);
+    r.z = act ? gate_load<T, VEC>(pre + m, M - m) : (typename Vec8<T>::type)(T)0.0f;
+    return r;
+}
+
+template <typename T>
+__device__ inline void gate_values(const GateRaw<T>& r, int act, float (&g)[8])
+{
+    float slope[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        sc[e] = e < n ? scale[m + e] : 0.0f;
-    if (n > 0)
-        for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
-            float g[8], slope[8] = {};
-            read_w<T, 8, STREAM>(dy + b * ld_dy + m, g, full, n);
-            if (act)
-                read_w<T, 8, STREAM>(pre + b * ld_pre + m, slope, full, n);
-            act_slopes<8>(slope, act);
+        slope[e] = (float)r.z[e];
+    act_slopes<8>(slope, act);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        g[e] = (float)r.dy[e] * slope[e];
+}
+
+struct GateArgs {
+    const void *dy, *pre;
+    int64_t ld_dy, ld_pre;
+    int act, B, M, rows;  // rows of a workgroup
+    int along, groups;    // threads of a row, and the rows that a workgroup has at a time
+    const float* scale;   // [M rounded up to 16]
+    void* gs;             // NULL: only the bias gradient
+    int64_t ld_gs, plane; // elements between rows and planes of gs
+    float* undo;          // [B] inverses of the rows' scalings
+    float* partial;       // [workgroups down][M] column sums of g, or NULL
+};
+
+// A workgroup walks `rows` whole rows, `groups` at a time, g * scale of a row staying in
+// registers until the row's largest is known, and goes to gs in NS scaled F16 planes
+// (NS = 0: as FP32 rows).  BF16 dy take one plane (11 bits: dx of 8192 rows is off by
+// 0.0017 of its size, which is the rounding of dx itself; one BF16 plane left 0.0023), F16
+// and FP32 ones two.  A thread has one vector of outputs and their sums over the rows,
+// which the groups join in LDS and leave in partial[workgroup]; the next row's loads are on
+// their way while this one's largest is found.  LONG: any number of outputs, read twice,
+// the sums in `partial` itself.  Bound by memory, and about as much by the slope's
+// arithmetic (8192 rows of 6144, BF16, 302 MB: 67 us, 4.5 TB/s; with the product behind
+// 205 us, 213 without the loads ahead, 215 in 256 workgroups, 208 in 1024).
+constexpr int kGateParts = 512;  // the most parts that the bias gradient comes in
+
+template <typename T, int NS>
+__device__ inline void gate_put(const GateArgs& a, int64_t b, int m, const float (&v)[8], float factor)
+{
+    if constexpr (NS == 0)
+        write_w<float, 8>(static_cast<float*>(a.gs) + b * a.ld_gs + m, v, true, 8);
+    else
+        put_planes<NS>(static_cast<uint16_t*>(a.gs) + b * a.ld_gs + m, a.plane, v, factor);
+}
+
+template <typename T, int NS, bool LONG, bool VEC>
+__global__ __launch_bounds__(1024) void k_fused_gate(GateArgs a)
+{
+    __shared__ float s_top[2][16];
+    extern __shared__ u32x4 s_fused[];
+    const int group = __builtin_amdgcn_readfirstlane((int)threadIdx.x / a.along), waves = a.along / 64;
+    const int m0 = ((int)threadIdx.x - group * a.along) * 8;
+    const int64_t b0 = (int64_t)blockIdx.x * a.rows, b1 = min((int64_t)a.B, b0 + a.rows);
+    const T* const dy = static_cast<const T*>(a.dy);
+    const T* const pre = static_cast<const T*>(a.pre);
+    float* const partial = a.partial ? a.partial + blockIdx.x * (int64_t)a.M : nullptr;
+    int turn = 0;
+    if constexpr (!LONG) {
+        float sc[8], sum[8] = {};
+        GateRaw<T> raw{};
+        // (rows past the last are zeros)
+        auto read = [&](int64_t b) __attribute__((always_inline)) {
+            raw = gate_read<T, VEC>(dy + b * a.ld_dy, pre + b * a.ld_pre, m0, b < b1 ? a.M : 0, a.act);
+        };
+        read(b0 + group);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            sc[e] = m0 + e < a.M ? a.scale[m0 + e] : 0.0f;
+        for (int64_t first = b0; first < b1; first += a.groups, turn ^= 1) {
+            const int64_t b = first + group;
+            const bool live = b < b1;
+            float g[8], top = 0.0f;
+            gate_values(raw, a.act, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                g[e] *= slope[e];
                 sum[e] += g[e];
                 g[e] *= sc[e];
             }
-            // rows are padded to whole vectors, with zeros
-            if constexpr (NS == 0) {
-                if (gs)
-                    write_w<float, 8>(reinterpret_cast<float*>(gs) + b * ld_gs + m, g, true, 8);
-            } else if (gs) {
-                put_planes<NS>(gs + b * ld_gs + m, plane, g);
+            if (first + a.groups < b1)
+                read(b + a.groups);
+            if (!a.gs)
+                continue;
+            RowPower power{};
+            if constexpr (NS > 0) {
+                power = row_power(largest_of_waves(largest(g, top), s_top[turn], group * waves, waves));
+                if (live && m0 == 0)
+                    a.undo[b] = power.undo;
+            }
+            if (live && m0 < a.ld_gs)
+                gate_put<T, NS>(a, b, m0, g, power.factor);
+        }
+        if (!partial)
+            return;
+        // [groups - 1][along] vectors
+        f32x4* const s_sum = reinterpret_cast<f32x4*>(s_fused) + (int)threadIdx.x - a.along;
+        const int total = (a.groups - 1) * a.along;
+        if (group > 0) {
+            s_sum[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
+            s_sum[total] = f32x4{sum[4], sum[5], sum[6], sum[7]};
+        }
+        __syncthreads();
+        if (group > 0)
+            return;
+        for (int k = 1; k < a.groups; ++k)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                sum[e] += s_sum[k * a.along + e / 4 * total][e % 4];
+        write_w<float, 8>(partial + m0, sum, a.M % 8 == 0 && m0 < a.M, a.M - m0);
+    } else {
+        for (int64_t b = b0; b < b1; ++b, turn ^= 1) {
+            float g[8], top = 0.0f;
+            for (int pass = NS == 0 ? 1 : 0; pass < 2; ++pass) {
+                RowPower power{};
+                if (NS > 0 && pass == 1) {
+                    power = row_power(largest_of_waves(top, s_top[turn], 0, waves));
+                    if (a.gs && threadIdx.x == 0)
+                        a.undo[b] = power.undo;
+                }
+                for (int m = m0; m < a.M; m += a.along * 8) {
+                    gate_values(gate_read<T, VEC>(dy + b * a.ld_dy, pre + b * a.ld_pre, m, a.M, a.act), a.act, g);
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[e] = m + e < a.M ? g[e] * a.scale[m + e] : 0.0f;
+                    if (pass == 0) {
+                        top = largest(v, top);
+                        continue;
+                    }
+                    if (a.gs)
+                        gate_put<T, NS>(a, b, m, v, power.factor);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (partial && m + e < a.M)
+                            partial[m + e] = b == b0 ? g[e] : partial[m + e] + g[e];
+                }
             }
         }
-    if (!partial)
-        return;
-    __shared__ float s_sum[8][kGateCols];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        s_sum[threadIdx.x / 32][threadIdx.x % 32 * 8 + e] = sum[e];
-    __syncthreads();
-    const int col = blockIdx.x * kGateCols + threadIdx.x;
-    if (col < M) {
-        float v = s_sum[0][threadIdx.x];
-#pragma unroll
-        for (int r = 1; r < 8; ++r)
-            v += s_sum[r][threadIdx.x];
-        partial[(int64_t)blockIdx.y * M + col] = v;
     }
 }
 

@@ -380,10 +380,6 @@ TWO_PLANES = [((4, 4, 4, 1, 2, 1), 1000, 4100, 2600, False), ((2, 2, 4, 1, 4, 1)
               ((1, 2, 4, 1, 4, 1), 6000, 2100, 40, True), ((1, 2, 4, 1, 4, 2), 1000, 70, 40, False),
               ((1, 2, 4, 1, 4, 2), 2000, 70, 40, True), ((2, 4, 4, 1, 2, 1), 72, 4100, 1300, False),
               ((2, 4, 4, 1, 2, 1), 2000, 2100, 520, True)]
-THREE_PLANES = [((4, 4, 4, 1, 2, 1), 72, 4100, 2600, False), ((4, 4, 4, 1, 2, 1), 2000, 2100, 520, True),
-                ((2, 2, 4, 1, 4, 1), 328, 4100, 100, False), ((2, 2, 4, 1, 4, 1), 6000, 2100, 40, True),
-                ((1, 2, 4, 1, 4, 1), 72, 70, 40, False), ((1, 2, 4, 1, 4, 1), 2000, 70, 40, True),
-                ((1, 2, 4, 1, 4, 2), 1000, 70, 40, False), ((1, 2, 4, 1, 4, 2), 6000, 70, 40, True)]
 
 
 def kernel_names(sp, h, x, y):
@@ -423,17 +419,59 @@ def test_every_tile_shape(sp, xk, shape, K, M, B, split):
     h.close()
 
 
-@pytest.mark.parametrize("shape,K,M,B,split", THREE_PLANES)
-def test_every_tile_shape_of_the_gradient(sp, shape, K, M, B, split):
+@pytest.mark.parametrize("yk,shape,K,M,B,split", [("f32", *c) for c in TWO_PLANES] + [("bf16", *c) for c in ONE_PLANE])
+def test_every_tile_shape_of_the_gradient(sp, yk, shape, K, M, B, split):
     p = problem(M, K, B, integer=True)
     h = handle(sp, p, backward=True)
-    dy, dx = dev(p["dy"]), torch.empty((B, M), device="cuda")
-    ws = torch.empty(sp.dense_fused_workspace_bytes(h, B, torch.float32), dtype=torch.uint8, device="cuda")
+    dy, dx = dev(p["dy"], yk), torch.empty((B, M), device="cuda")
+    ws = torch.empty(sp.dense_fused_workspace_bytes(h, B, TYPES[yk]), dtype=torch.uint8, device="cuda")
+    planes = 1 if yk == "bf16" else 2
     names = [n for n, _, _ in launches(lambda st: sp.dense_fused_backward(h, dy, dx=dx, workspace=ws, stream=st))]
-    assert any("k_fused_tile" in n and "".join(f"Li{v}E" for v in (3, *shape)) in n for n in names), names
+    assert any("k_fused_tile" in n and "".join(f"Li{v}E" for v in (planes, *shape)) in n for n in names), names
     assert any("k_fused_join" in n for n in names) == split
-    dx, _, (want, _, _) = backward(sp, h, p, "f32", "f32", "none", want_bias=False)
+    dx, _, (want, _, _) = backward(sp, h, p, "f32", yk, "none", want_bias=False)
     assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)))
+    h.close()
+
+
+# outputs on both sides of what a workgroup's threads hold, rows that the vectors do not fit
+@pytest.mark.parametrize("M", [40, 2048, 2056, 4100, 8192, 8200])
+@pytest.mark.parametrize("yk", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B", [33, 1100])
+def test_gate_forms(sp, yk, M, B):
+    """Every form of the gate: dx and dbias of integers, rows whole or at odd strides, one without the other."""
+    p = problem(64, M, B, integer=True)
+    z = np.random.default_rng([18, M, B]).integers(-3, 4, (B, M)).astype(np.float32)
+    h = handle(sp, p, backward=True)
+    for pad, offset in ((0, 0), (3, 1)):
+        dx, db, (want, wb, _) = backward(sp, h, p, "f32", yk, "relu", pad, offset, z)
+        assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32))) and (db.cpu().numpy() == wb).all()
+    dx2, _, _ = backward(sp, h, p, "f32", yk, "relu", z=z, want_bias=False)
+    _, db2, _ = backward(sp, h, p, "f32", yk, "relu", z=z, want_dx=False)
+    assert torch.equal(dx, dx2) and torch.equal(db, db2)
+    h.close()
+
+
+@pytest.mark.parametrize("yk,entry", [("f32", 2.0 ** -23), ("bf16", 2.0 ** -11)])
+@pytest.mark.parametrize("B", [50, 600])
+def test_gradients_of_any_size(sp, yk, entry, B):
+    """Rows of dy between 1e-34 and 1e30, one all zero, one infinite: each keeps its digits, none touches another."""
+    p = problem(96, 200, B)
+    r = np.random.default_rng([19, B])
+    rows = 10.0 ** r.uniform(-34, 30, (B, 1))
+    rows[0] = 0.0
+    p["dy"] = (p["dy"] * rows).astype(np.float32)
+    p["dy"][1, 7] = np.inf
+    p["Q"][7, :] = np.where(np.arange(96) % 2, 5, -5).astype(np.int8)
+    h = handle(sp, p, backward=True)
+    dx, db, (want, _, g) = backward(sp, h, p, "f32", yk, "none")
+    got = host(dx)
+    assert (got[1] == np.where(np.arange(96) % 2, np.inf, -np.inf)).all() and (got[0] == 0).all()
+    got, want, g = np.delete(got, 1, 0), np.delete(want, 1, 0), np.delete(g, 1, 0)
+    w = np.abs(p["Q"].astype(np.float64)) * p["scale"].astype(np.float64)[:, None]
+    lim = ((6 * U * np.sqrt(2 * 200 + 32) + 2 * U) * (np.abs(g) @ w) + 6 * entry * np.sqrt((g * g) @ (w * w))
+           + 2.0 ** -39 * np.abs(g * p["scale"]).max(axis=1, keepdims=True) * np.abs(p["Q"].astype(np.float64)).sum(axis=0) + 2.0 ** -140)
+    assert (np.abs(got - want) <= lim).all(), np.max(np.abs(got - want) / lim)
     h.close()
 
 
@@ -484,7 +522,7 @@ def test_rows_that_fill_no_chunk_are_cut_too(sp):
 @pytest.mark.parametrize("yk", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("K,M,B", [(70, 72, 40), (2000, 300, 90), (300, 6000, 333), (520, 2100, 700)])
 def test_backward_forms(sp, yk, K, M, B):
-    """Products of one, two and three planes in several shapes, split and not, the bias gradient summed beside them."""
+    """Products of one and two planes in several shapes, split and not, the bias gradient summed beside them."""
     p = problem(K, M, B, integer=True)
     h = handle(sp, p, backward=True)
     dx, db, (want, wb, _) = backward(sp, h, p, "f32", yk, "none")
