@@ -639,6 +639,10 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     constexpr bool kEarly = D >= 3;
     constexpr int kBehind = kEarly ? (D - 3) * kLoads : 0;  // loads that may be on their way at a wait
     static_assert(kBehind < 64, "the load counter holds what is in flight");
+    // With two stages, the next step's weights are needed half a step before its rows.  Asked
+    // for first, they leave the rows the whole step (two planes, FP32 gradient of 2500 rows:
+    // 139 us with both waited for half-way, 133 so; one plane, 16,384 rows: 334 and 341).
+    constexpr bool kWeightsFirst = !kEarly && NS == 2;
     extern __shared__ u32x4 s_fused[];
     // Neighbouring workgroups of one XCD (every eighth) take tiles of a group
     // of 8 output tiles, so that they share both operands in its L2.
@@ -687,16 +691,22 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     auto fetch = [&](int buf, int s) __attribute__((always_inline)) {
         const bool live = s < steps && (first + s) * kFusedStep + 8 * chunk < a.n_in;
         const uint32_t at = s < steps ? s : 0, to = lds + buf * kStage;
+        auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + at * 1024u,
+                            to + kWeights + (w * MT + t) * 1024);
+        };
+        if (kWeightsFirst)
+            weights();
 #pragma unroll
         for (int p = 0; p < NS; ++p)
 #pragma unroll
             for (int i = 0; i < kChunks; ++i)
                 load_to_lds(xr[p], live ? x_off[i] : kOutOfRange, at * 128u,
                             to + (p * kRows + i * (kThreads / 8) + w * 8) * 128);
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-            load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + at * 1024u,
-                        to + kWeights + (w * MT + t) * 1024);
+        if (!kWeightsFirst)
+            weights();
     };
     f32x4 acc[MT][NT];
 #pragma unroll
@@ -784,8 +794,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                 if (item + 2 < kItems)
                     xo[(item + 2) % 3] = read(cur, item + 2);
                 if (item == kHalf) {
-                    // this wave's part of the next stage is there: its weights are its own
-                    wait_loads<0>();
+                    // this wave's weights of the next step are there; they are its own
+                    wait_loads<kWeightsFirst ? NS * kChunks : 0>();
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
                         wt[t] = s_w[next * (kStage / 16) + t * 64];
@@ -804,6 +814,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                 }
             }
             cur = next;
+            if (kWeightsFirst)
+                wait_loads<0>();
             __syncthreads();
         }
     }
