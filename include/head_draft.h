@@ -26,8 +26,10 @@
  *  - A drafted token outside [0, V) has probability zero and is refused.
  *  - noise entries that are not positive never win.
  *
- * Precision: FP32; the sums of the exponentials are taken per part of a row
- * and joined in a fixed order, so equal calls give equal bits.
+ * Precision: FP32, with the hardware's base-2 exponential and reciprocal (of
+ * noise; within one unit in the last place); the sums of the exponentials are
+ * taken per part of a row and joined in a fixed order, so equal calls give equal
+ * bits.
  *
  * Data layout (DEVICE pointers):
  *   target       [S][G + 1] rows of V logits, ld_target elements apart.

@@ -284,16 +284,30 @@ int64_t gate_bytes(int y_type, int32_t B, int32_t M)
     return gate_plane_bytes(y_type, B, M) + spk::fused_pad((int64_t)B * 4, 16);
 }
 
-template <typename T, int NS>
-void launch_gate(spk::GateArgs a, bool vec, hipStream_t st)
+template <typename T, int NS, bool VEC>
+void launch_long_gate(const spk::GateArgs& a, hipStream_t st)
 {
-    const bool any = !vec || a.M > 8192;  // else a row's vectors are a workgroup's threads at most
-    a.along = any ? 512 : (a.M + 511) / 512 * 64;
-    a.groups = any ? 1 : std::min(a.rows, std::max(1, 768 / a.along));
-    const auto gate = !vec ? spk::k_fused_gate<T, NS, true, false>
-                      : any ? spk::k_fused_gate<T, NS, true, true>
-                            : spk::k_fused_gate<T, NS, false, true>;
-    hipLaunchKernelGGL(gate, dim3((unsigned)gate_parts(a.B)), dim3(a.along * a.groups), (a.groups - 1) * a.along * 32, st, a);
+    if (NS > 0 && a.gs)
+        hipLaunchKernelGGL((spk::k_fused_gate_top<T, VEC>), dim3((unsigned)a.B), dim3(512), 0, st, a);
+    const dim3 grid((unsigned)((a.M + spk::kGateCols - 1) / spk::kGateCols), (unsigned)((a.B + a.rows - 1) / a.rows));
+    hipLaunchKernelGGL((spk::k_fused_gate_columns<T, NS, VEC>), grid, dim3(256), 0, st, a);
+}
+
+// Returns the parts that the bias gradient came in: gate_parts at most.
+template <typename T, int NS>
+int launch_gate(spk::GateArgs a, bool vec, hipStream_t st)
+{
+    a.rows = gate_rows(a.B);
+    if (!vec || a.M > 8192) {
+        a.rows = std::max(a.rows, 16);
+        vec ? launch_long_gate<T, NS, true>(a, st) : launch_long_gate<T, NS, false>(a, st);
+    } else {
+        a.along = (a.M + 511) / 512 * 64;
+        a.groups = std::min(a.rows, std::max(1, 768 / a.along));
+        hipLaunchKernelGGL((spk::k_fused_gate<T, NS>), dim3((unsigned)gate_parts(a.B)), dim3(a.along * a.groups),
+                           (a.groups - 1) * a.along * 32, st, a);
+    }
+    return (a.B + a.rows - 1) / a.rows;
 }
 
 int check_rows(int32_t B, int32_t act, int x_type, int y_type)
@@ -464,7 +478,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return rc;
     if (act == DENSE_ACT_NONE)
         pre = nullptr;
-    const int parts = B > 0 ? gate_parts(B) : 0;
+    int parts = 0;
     float* partial = nullptr;
     float* undo = nullptr;
     if (B > 0) {
@@ -472,14 +486,14 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         if (dbias)
             partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M));
         spk::GateArgs g{};
-        g.dy = dy, g.ld_dy = ld_dy, g.pre = pre, g.ld_pre = ld_pre, g.act = act, g.B = B, g.M = h->M, g.rows = gate_rows(B);
+        g.dy = dy, g.ld_dy = ld_dy, g.pre = pre, g.ld_pre = ld_pre, g.act = act, g.B = B, g.M = h->M;
         g.scale = h->scale, g.gs = dx ? workspace : nullptr, g.ld_gs = plane_stride(h->M), g.plane = g.ld_gs * B;
         g.undo = undo, g.partial = partial;
         const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
         switch (y_type) {
-        case SPIKE_TYPE_F32: B <= kFewRows ? launch_gate<float, 0>(g, vec, st) : launch_gate<float, 2>(g, vec, st); break;
-        case SPIKE_TYPE_BF16: launch_gate<spk::bf16, 1>(g, vec, st); break;
-        default: B <= kFewRows ? launch_gate<spk::f16, 0>(g, vec, st) : launch_gate<spk::f16, 2>(g, vec, st); break;
+        case SPIKE_TYPE_F32: parts = B <= kFewRows ? launch_gate<float, 0>(g, vec, st) : launch_gate<float, 2>(g, vec, st); break;
+        case SPIKE_TYPE_BF16: parts = launch_gate<spk::bf16, 1>(g, vec, st); break;
+        default: parts = B <= kFewRows ? launch_gate<spk::f16, 0>(g, vec, st) : launch_gate<spk::f16, 2>(g, vec, st); break;
         }
     }
     // the bias gradient's parts are summed beside the product of many rows, else by themselves

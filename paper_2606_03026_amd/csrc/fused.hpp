@@ -25,9 +25,9 @@ inline int64_t fused_packed_bytes(int64_t n_out, int64_t n_in)
     return fused_pad(n_out, kFusedTile) * fused_pad(n_in, kFusedStep);
 }
 
-// Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns.  `eights`:
-// rows start on 8-byte boundaries and K is a multiple of 8 (1536 -> 6144: 20 us byte
-// by byte, 5 in eights).
+// Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns; once per
+// handle.  `eights`: rows start on 8-byte boundaries and K is a multiple of 8 (1536 ->
+// 6144: 20 us byte by byte, 8 in eights).
 template <bool TRANSPOSE>
 __global__ __launch_bounds__(256) void k_fused_pack(const int8_t* __restrict__ Q, int K, int M, int8_t* __restrict__ P,
                                                     int64_t chunks, int eights)
@@ -453,8 +453,9 @@ struct OutputColumns {
 
 // Up to 16 NB rows: a workgroup takes 16 MT outputs and all inputs, its WK
 // waves sharing the 64-input steps; the waves' sums are joined in LDS.  Bound
-// by the weights' bytes (and, at one tile of rows, by latency).  Rows that are
-// not there cost no loads, only idle columns of the matrix instruction.
+// by the weights' bytes (1536 -> 57,344, one FP32 row: 17.4 us, 5.1 TB/s), where these
+// are few by latency (1536 -> 6144, one FP32 row: 5.1 us; 1536 -> 1536, 7 BF16 rows: 4.0).
+// Rows that are not there cost no loads, only idle columns of the matrix instruction.
 template <typename XT, int NS, int NB, int MT, int WK, bool VECX>
 __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 {
@@ -548,7 +549,8 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 }
 
 // dbias from its parts (the first 256 threads of a workgroup: 64 outputs, a quarter of
-// the parts per wave; s_sum: 256 floats of LDS).
+// the parts per wave; s_sum: 256 floats of LDS).  Beside a product it is hidden; alone
+// 16 parts of 6144 take 2.8 us, 157 of 12,000 (7.5 MB) 5.2.
 __device__ inline void bias_sums(const BiasArgs& a, int wg, float* s_sum)
 {
     const int m = min(wg * 64 + (int)threadIdx.x % 64, a.M - 1), w = threadIdx.x / 64;
@@ -625,6 +627,11 @@ constexpr int fused_tile_lds()
 // KS groups of these waves share the steps, each with a ring of its own, and the first
 // adds up their sums: where there are fewer tiles than compute units, one group leaves
 // most of its unit's issue slots empty.
+// Bound by how densely the waves issue products between their waits: 16,384 BF16 rows
+// of 1536 -> 6144 with GELU and the values before it 318 us, 972 TFLOP/s (the product
+// alone 279 us, 1108 TFLOP/s); 2500 FP32 rows, two planes, 91 us and 1034 TFLOP/s, the
+// matrix units busy 44% of the time, LDS 4%; 8192 rows of 6144 -> 1536 136 us, 1137 TFLOP/s.
+// Codes widened by byte moves and packed F16 sums instead of conversions: no change.
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
 __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
 {
@@ -889,7 +896,8 @@ inline dim3 row_grid(int64_t rows, int64_t vectors)
 }
 
 // Joins the sums of a product whose steps were split, the parts in ascending order,
-// then the epilogue.  part: [splits][B] rows of ld elements.
+// then the epilogue.  part: [splits][B] rows of ld elements.  Bound by memory and its
+// launch (four parts of 500 rows of 1536: 6.2 us for 15 MB).
 __global__ __launch_bounds__(256) void k_fused_join(FusedArgs a, const float* __restrict__ part, int64_t ld)
 {
     const int m = (blockIdx.x * 64 + threadIdx.x % 64) * 8;
@@ -913,7 +921,8 @@ __global__ __launch_bounds__(256) void k_fused_join(FusedArgs a, const float* __
 }
 
 // Copies rows of n 16-bit elements at any alignment for the product: rows of `ld`
-// (n rounded up to 8) elements, zeros past n.
+// (n rounded up to 8) elements, zeros past n.  Bound by memory (2500 rows of 1536 of
+// them, one element off: 7.6 us, 2.0 TB/s: 2-byte loads).
 __global__ __launch_bounds__(256) void k_fused_align(const uint16_t* __restrict__ x, int64_t ld_x, int B, int n, int64_t ld,
                                                      uint16_t* __restrict__ out)
 {
@@ -1017,7 +1026,7 @@ struct GateArgs {
     const void *dy, *pre;
     int64_t ld_dy, ld_pre;
     int act, B, M, rows;  // rows of a workgroup
-    int along, groups;    // threads of a row, and the rows that a workgroup has at a time
+    int along, groups;    // k_fused_gate: threads of a row, and the rows that a workgroup has at a time
     const float* scale;   // [M rounded up to 16]
     void* gs;             // NULL: only the bias gradient
     int64_t ld_gs, plane; // elements between rows and planes of gs
@@ -1025,16 +1034,16 @@ struct GateArgs {
     float* partial;       // [workgroups down][M] column sums of g, or NULL
 };
 
-// A workgroup walks `rows` whole rows, `groups` at a time, g * scale of a row staying in
-// registers until the row's largest is known, and goes to gs in NS scaled F16 planes
-// (NS = 0: as FP32 rows).  BF16 dy take one plane (11 bits: dx of 8192 rows is off by
-// 0.0017 of its size, which is the rounding of dx itself; one BF16 plane left 0.0023), F16
-// and FP32 ones two.  A thread has one vector of outputs and their sums over the rows,
-// which the groups join in LDS and leave in partial[workgroup]; the next row's loads are on
-// their way while this one's largest is found.  LONG: any number of outputs, read twice,
-// the sums in `partial` itself.  Bound by memory, and about as much by the slope's
-// arithmetic (8192 rows of 6144, BF16, 302 MB: 67 us, 4.5 TB/s; with the product behind
-// 205 us, 213 without the loads ahead, 215 in 256 workgroups, 208 in 1024).
+// Rows of up to 8,192 outputs in whole vectors: a workgroup walks `rows` of them, `groups`
+// at a time, g * scale of a row staying in registers until the row's largest is known, and
+// goes to gs in NS scaled F16 planes (NS = 0: as FP32 rows).  BF16 dy take one plane (11
+// bits: dx of 8192 rows is off by 0.0017 of its size, which is the rounding of dx itself;
+// one BF16 plane left 0.0023), F16 and FP32 ones two.  A thread has one vector of outputs
+// and their sums over the rows, which the groups join in LDS and leave in
+// partial[workgroup]; the next row's loads are on their way while this one's largest is
+// found.  Bound by memory, and about as much by the slope's arithmetic (8192 rows of
+// 6144, BF16, 302 MB: 65 us, 4.7 TB/s; with the product behind 205 us, 213 without the
+// loads ahead, 215 in 256 workgroups, 208 in 1024).
 constexpr int kGateParts = 512;  // the most parts that the bias gradient comes in
 
 template <typename T, int NS>
@@ -1046,7 +1055,7 @@ __device__ inline void gate_put(const GateArgs& a, int64_t b, int m, const float
         put_planes<NS>(static_cast<uint16_t*>(a.gs) + b * a.ld_gs + m, a.plane, v, factor);
 }
 
-template <typename T, int NS, bool LONG, bool VEC>
+template <typename T, int NS>
 __global__ __launch_bounds__(1024) void k_fused_gate(GateArgs a)
 {
     __shared__ float s_top[2][16];
@@ -1056,88 +1065,123 @@ __global__ __launch_bounds__(1024) void k_fused_gate(GateArgs a)
     const int64_t b0 = (int64_t)blockIdx.x * a.rows, b1 = min((int64_t)a.B, b0 + a.rows);
     const T* const dy = static_cast<const T*>(a.dy);
     const T* const pre = static_cast<const T*>(a.pre);
-    float* const partial = a.partial ? a.partial + blockIdx.x * (int64_t)a.M : nullptr;
+    float sc[8], sum[8] = {};
+    GateRaw<T> raw{};
+    // (rows past the last are zeros)
+    auto read = [&](int64_t b) __attribute__((always_inline)) {
+        raw = gate_read<T, true>(dy + b * a.ld_dy, pre + b * a.ld_pre, m0, b < b1 ? a.M : 0, a.act);
+    };
+    read(b0 + group);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        sc[e] = m0 + e < a.M ? a.scale[m0 + e] : 0.0f;
     int turn = 0;
-    if constexpr (!LONG) {
-        float sc[8], sum[8] = {};
-        GateRaw<T> raw{};
-        // (rows past the last are zeros)
-        auto read = [&](int64_t b) __attribute__((always_inline)) {
-            raw = gate_read<T, VEC>(dy + b * a.ld_dy, pre + b * a.ld_pre, m0, b < b1 ? a.M : 0, a.act);
-        };
-        read(b0 + group);
+    for (int64_t first = b0; first < b1; first += a.groups, turn ^= 1) {
+        const int64_t b = first + group;
+        const bool live = b < b1;
+        float g[8];
+        gate_values(raw, a.act, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            sum[e] += g[e];
+            g[e] *= sc[e];
+        }
+        if (first + a.groups < b1)
+            read(b + a.groups);
+        if (!a.gs)
+            continue;
+        RowPower power{};
+        if constexpr (NS > 0) {
+            power = row_power(largest_of_waves(largest(g, 0.0f), s_top[turn], group * waves, waves));
+            if (live && m0 == 0)
+                a.undo[b] = power.undo;
+        }
+        if (live && m0 < a.ld_gs)
+            gate_put<T, NS>(a, b, m0, g, power.factor);
+    }
+    if (!a.partial)
+        return;
+    // [2 halves of a vector][groups - 1][along]
+    f32x4* const s_sum = reinterpret_cast<f32x4*>(s_fused) + (int)threadIdx.x - a.along;
+    const int total = (a.groups - 1) * a.along;
+    if (group > 0) {
+        s_sum[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
+        s_sum[total] = f32x4{sum[4], sum[5], sum[6], sum[7]};
+    }
+    __syncthreads();
+    if (group > 0)
+        return;
+    for (int k = 1; k < a.groups; ++k)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            sc[e] = m0 + e < a.M ? a.scale[m0 + e] : 0.0f;
-        for (int64_t first = b0; first < b1; first += a.groups, turn ^= 1) {
-            const int64_t b = first + group;
-            const bool live = b < b1;
-            float g[8], top = 0.0f;
-            gate_values(raw, a.act, g);
+            sum[e] += s_sum[k * a.along + e / 4 * total][e % 4];
+    write_w<float, 8>(a.partial + blockIdx.x * (int64_t)a.M + m0, sum, a.M % 8 == 0 && m0 < a.M, a.M - m0);
+}
+
+// Any rows, in two kernels that each read dy and pre: the rows' largest, a workgroup a
+// row; then a workgroup takes 256 outputs of `rows` rows.  Bound by memory (2500 FP32 rows
+// of 12,000: 85 us for the 240 MB, and some 75 to read them again and write 120; one
+// workgroup walking whole rows twice took 248 us, one that kept four vectors a thread
+// ran out of registers and took 316).
+template <typename T, bool VEC>
+__global__ __launch_bounds__(512) void k_fused_gate_top(GateArgs a)
+{
+    __shared__ float s_top[16];
+    const int64_t b = blockIdx.x;
+    float top = 0.0f;
+    for (int m = threadIdx.x * 8; m < a.M; m += 512 * 8) {
+        float g[8];
+        gate_values(gate_read<T, VEC>(static_cast<const T*>(a.dy) + b * a.ld_dy, static_cast<const T*>(a.pre) + b * a.ld_pre, m,
+                                      a.M, a.act), a.act, g);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            g[e] *= a.scale[min(m + e, a.M - 1)];
+        top = largest(g, top);
+    }
+    top = largest_of_waves(top, s_top, 0, 8);
+    if (threadIdx.x == 0)
+        a.undo[b] = row_power(top).undo;
+}
+
+constexpr int kGateCols = 256;
+
+template <typename T, int NS, bool VEC>
+__global__ __launch_bounds__(256) void k_fused_gate_columns(GateArgs a)
+{
+    const int m = blockIdx.x * kGateCols + threadIdx.x % 32 * 8;
+    const int64_t b0 = (int64_t)blockIdx.y * a.rows, b1 = min((int64_t)a.B, b0 + a.rows);
+    float sc[8], sum[8] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        sc[e] = m + e < a.M ? a.scale[m + e] : 0.0f;
+    if (m < a.M)
+        for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
+            float g[8];
+            gate_values(gate_read<T, VEC>(static_cast<const T*>(a.dy) + b * a.ld_dy, static_cast<const T*>(a.pre) + b * a.ld_pre,
+                                          m, a.M, a.act), a.act, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 sum[e] += g[e];
                 g[e] *= sc[e];
             }
-            if (first + a.groups < b1)
-                read(b + a.groups);
-            if (!a.gs)
-                continue;
-            RowPower power{};
-            if constexpr (NS > 0) {
-                power = row_power(largest_of_waves(largest(g, top), s_top[turn], group * waves, waves));
-                if (live && m0 == 0)
-                    a.undo[b] = power.undo;
-            }
-            if (live && m0 < a.ld_gs)
-                gate_put<T, NS>(a, b, m0, g, power.factor);
+            // (the power is the inverse of its inverse: 254 less its exponent)
+            if (a.gs)
+                gate_put<T, NS>(a, b, m, g, NS == 0 ? 1.0f : __uint_as_float((254u << 23) - __float_as_uint(a.undo[b])));
         }
-        if (!partial)
-            return;
-        // [groups - 1][along] vectors
-        f32x4* const s_sum = reinterpret_cast<f32x4*>(s_fused) + (int)threadIdx.x - a.along;
-        const int total = (a.groups - 1) * a.along;
-        if (group > 0) {
-            s_sum[0] = f32x4{sum[0], sum[1], sum[2], sum[3]};
-            s_sum[total] = f32x4{sum[4], sum[5], sum[6], sum[7]};
-        }
-        __syncthreads();
-        if (group > 0)
-            return;
-        for (int k = 1; k < a.groups; ++k)
+    if (!a.partial)
+        return;
+    __shared__ float s_sum[8][kGateCols];
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                sum[e] += s_sum[k * a.along + e / 4 * total][e % 4];
-        write_w<float, 8>(partial + m0, sum, a.M % 8 == 0 && m0 < a.M, a.M - m0);
-    } else {
-        for (int64_t b = b0; b < b1; ++b, turn ^= 1) {
-            float g[8], top = 0.0f;
-            for (int pass = NS == 0 ? 1 : 0; pass < 2; ++pass) {
-                RowPower power{};
-                if (NS > 0 && pass == 1) {
-                    power = row_power(largest_of_waves(top, s_top[turn], 0, waves));
-                    if (a.gs && threadIdx.x == 0)
-                        a.undo[b] = power.undo;
-                }
-                for (int m = m0; m < a.M; m += a.along * 8) {
-                    gate_values(gate_read<T, VEC>(dy + b * a.ld_dy, pre + b * a.ld_pre, m, a.M, a.act), a.act, g);
-                    float v[8];
+    for (int e = 0; e < 8; ++e)
+        s_sum[threadIdx.x / 32][threadIdx.x % 32 * 8 + e] = sum[e];
+    __syncthreads();
+    const int col = blockIdx.x * kGateCols + threadIdx.x;
+    if (col < a.M) {
+        float v = s_sum[0][threadIdx.x];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[e] = m + e < a.M ? g[e] * a.scale[m + e] : 0.0f;
-                    if (pass == 0) {
-                        top = largest(v, top);
-                        continue;
-                    }
-                    if (a.gs)
-                        gate_put<T, NS>(a, b, m, v, power.factor);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (partial && m + e < a.M)
-                            partial[m + e] = b == b0 ? g[e] : partial[m + e] + g[e];
-                }
-            }
-        }
+        for (int r = 1; r < 8; ++r)
+            v += s_sum[r][threadIdx.x];
+        a.partial[(int64_t)blockIdx.y * a.M + col] = v;
     }
 }
 

@@ -435,7 +435,7 @@ def test_every_tile_shape_of_the_gradient(sp, yk, shape, K, M, B, split):
 
 
 # outputs on both sides of what a workgroup's threads hold, rows that the vectors do not fit
-@pytest.mark.parametrize("M", [40, 2048, 2056, 4100, 8192, 8200])
+@pytest.mark.parametrize("M", [40, 2048, 2056, 4100, 8192, 8200, 14000, 33000])
 @pytest.mark.parametrize("yk", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("B", [33, 1100])
 def test_gate_forms(sp, yk, M, B):
