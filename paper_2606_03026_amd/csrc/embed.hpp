@@ -267,9 +267,13 @@ __device__ inline void put_row(T* p, const float (&v)[VEC], float scale, bool ac
     }
 }
 
-constexpr int kMaxRun = 32;  // tokens of a run: its keys, and the next one, along the lanes of a wave
+// Tokens of a run; its keys and its two neighbours lie along the lanes of a wave.  A 352 MB
+// table's gradient by 12, 16, 24 and 32 tokens: 2,500 tokens 68, 67, 68, 68 us; 16,384
+// 87, 82, 81, 84; 60,000 tokens of a 32,000 x 256 table 88, 82, 78, 76.
+constexpr int kRun = 24;
+static_assert(kRun + 2 <= 64, "a run's keys lie along a wave");
 
-// Workgroups below sum_wgs: each wave adds up one run (`run` tokens of the
+// Workgroups below sum_wgs: each wave adds up one run (kRun tokens of the
 // sorted list) for 64 VEC columns.  partial[2 r] holds run r's sum of a row that began in an
 // earlier run, partial[2 r + 1] that of a row that begins in run r and goes
 // on.  The other workgroups zero the rows that no token names.  Bound by memory: 16,384
@@ -277,7 +281,7 @@ constexpr int kMaxRun = 32;  // tokens of a run: its keys, and the next one, alo
 template <typename TG, typename TD, int VEC>
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict__ grad, int64_t ld_grad,
                                                            const uint32_t* __restrict__ keys,
-                                                           const int* __restrict__ order, int T, int D, int run,
+                                                           const int* __restrict__ order, int T, int D,
                                                            int sum_wgs, float scale, int accumulate,
                                                            TD* __restrict__ dtable, int64_t ld_table,
                                                            float* __restrict__ partial, FillArgs fill)
@@ -287,10 +291,10 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
     const int blocks = (D + 64 * VEC - 1) / (64 * VEC), lane = threadIdx.x % 64;
     const int unit = __builtin_amdgcn_readfirstlane(blockIdx.x * (kEmbedBlock / 64) + threadIdx.x / 64);
     const int r = unit / blocks;
-    const int i0 = r * run;
+    const int i0 = r * kRun;
     if (i0 >= T)
         return;
-    const int n = min(run, T - i0);
+    const int n = min(kRun, T - i0);
     // column offset; lanes past the row repeat its last columns and store nothing
     const int col = (unit % blocks * 64 + lane) * VEC;
     const bool inside = col < D;
@@ -343,7 +347,7 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
 // Workgroups from join_wgs on zero rows that no token names.  Bound by the reads that
 // depend on each other (16,384 tokens, with 32 MB written: 10 us).
 template <typename TD, int VEC>
-__global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __restrict__ keys, int T, int D, int run,
+__global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __restrict__ keys, int T, int D,
                                                             float scale, int accumulate, TD* __restrict__ dtable,
                                                             int64_t ld_table, const float* __restrict__ partial,
                                                             int join_wgs, FillArgs fill)
@@ -356,11 +360,11 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __re
     const int col = (unit % blocks * 64 + lane) * VEC;
     const bool inside = col < D;
     const int d = inside ? col : D - VEC;
-    const int64_t i0 = (int64_t)r * run, i1 = i0 + run;
+    const int64_t i0 = (int64_t)r * kRun, i1 = i0 + kRun;
     if (i1 >= T)
         return;
     // lane 0: the key before this run; lane 1: its last; lane 2 + l: the first of the l-th run after it
-    const int64_t at = lane == 0 ? i0 - 1 : lane == 1 ? i1 - 1 : i1 + (int64_t)(lane - 2) * run;
+    const int64_t at = lane == 0 ? i0 - 1 : lane == 1 ? i1 - 1 : i1 + (int64_t)(lane - 2) * kRun;
     uint32_t key_l = at >= 0 && at < T ? keys[at] : kNoToken;
     float sum[VEC];
     load_cols<float, VEC>(partial + (int64_t)(2 * r + 1) * D + d, sum);  // (asked for with the keys; there if a row goes on)
@@ -390,7 +394,7 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __re
         if (more < 62)
             break;
         q += 62;
-        const int64_t next = q * run + (int64_t)(lane - 2) * run;
+        const int64_t next = q * kRun + (int64_t)(lane - 2) * kRun;
         key_l = lane >= 2 && next < T ? keys[next] : kNoToken;
     }
     if (inside)

@@ -19,15 +19,10 @@ using spk::hip_fail;
 using spk::is_float_type;
 using spk::type_bytes;
 
-// Tokens a run holds: short ones where there are few tokens to spread over the chip.
-int run_length(int32_t T) { return T <= 4096 ? 8 : 16; }
-
-static_assert(32 <= spk::kMaxRun, "a run's keys lie along a wave");
-
 // Of the table's zeros, the bytes written beside the merging, the sums and their
 // joining (a smaller table's shares below); the rest goes beside the sorting.  A
-// 352 MB table's gradient, 2,500 tokens: 70 us, with nothing beside the joining and
-// 128 MB beside the sorting 71; 16,384 tokens: 82 and 85.
+// 352 MB table's gradient, in runs of 8 or 16: 2,500 tokens 70 us, with nothing beside
+// the joining and 128 MB beside the sorting 71; 16,384 tokens 82 and 85.
 constexpr int64_t kFillBesideMerge = 48ll << 20, kFillBesideSums = 160ll << 20, kFillBesideJoin = 32ll << 20;
 
 bool rows_vectorize(const void* p, int type, int64_t ld, int32_t D)
@@ -103,7 +98,7 @@ struct GradSpace {
 int64_t grad_space(int32_t T, int32_t D, void* base, GradSpace* out)
 {
     const int64_t list = ((int64_t)T * 4 + 255) / 256 * 256;
-    const int64_t runs = ((int64_t)T + run_length(T) - 1) / run_length(T);
+    const int64_t runs = ((int64_t)T + spk::kRun - 1) / spk::kRun;
     char* p = static_cast<char*>(base);
     if (out) {
         out->keys = reinterpret_cast<uint32_t*>(p);
@@ -136,18 +131,17 @@ template <typename TG, typename TD, int VEC>
 void launch_grad(const Grad& a, const spk::FillArgs& fill, const spk::FillArgs& with_join)
 {
     constexpr int waves = spk::kEmbedBlock / 64;
-    const int run = run_length(a.T);
     const int64_t blocks = (a.D + 64 * VEC - 1) / (64 * VEC);
-    const int64_t runs = ((int64_t)a.T + run - 1) / run;
+    const int64_t runs = ((int64_t)a.T + spk::kRun - 1) / spk::kRun;
     const int64_t sum_wgs = (runs * blocks + waves - 1) / waves;
     const int64_t wgs = sum_wgs + spk::fill_wgs(fill);
     if (wgs > 0)
         hipLaunchKernelGGL((spk::k_embed_sum<TG, TD, VEC>), dim3((unsigned)wgs), dim3(spk::kEmbedBlock), 0, a.st,
-                           static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.D, run, (int)sum_wgs,
+                           static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.D, (int)sum_wgs,
                            a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, fill);
     if (runs > 1)
         hipLaunchKernelGGL((spk::k_embed_join<TD, VEC>), dim3((unsigned)(sum_wgs + spk::fill_wgs(with_join))),
-                           dim3(spk::kEmbedBlock), 0, a.st, a.ws.keys, a.T, a.D, run, a.scale, a.accumulate,
+                           dim3(spk::kEmbedBlock), 0, a.st, a.ws.keys, a.T, a.D, a.scale, a.accumulate,
                            static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, (int)sum_wgs, with_join);
 }
 
@@ -265,7 +259,7 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
         // Rows zeroed beside the sorting, before it is known which are named (those are
         // then written again); the others go beside the sums and their joining.
         const int64_t all = fill.count * fill.bytes;
-        if (T > run_length(T))
+        if (T > spk::kRun)
             with_join = take_rows(&fill, std::min<int64_t>(kFillBesideJoin, all / 8));
         const int64_t beside_sums = std::min<int64_t>(kFillBesideSums, all / 2);
         const int64_t beside_merge = one ? 0 : std::min<int64_t>(kFillBesideMerge, all / 8);
