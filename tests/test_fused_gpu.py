@@ -11,9 +11,8 @@ independent, stay within
 (parts: three BF16 parts of an FP32 activation or gradient at most; 32: waves, scale, bias).  The
 activation adds at most 1e-6 + 4e-7 |y| (its polynomial's 1.7e-7 and ten FP32
 operations), its slope is at most 1.13 in size, and storing rounds by half a
-unit of the type.  In the backward pass each g * scale enters as one BF16
-value (half a unit of BF16) for BF16 dy and with 16 bits (cut, not rounded)
-for F16.
+unit of the type.  In the backward pass each g * scale enters with 11
+bits or more for BF16 dy (the bound allows 8) and with 16 or more for F16.
 """
 import numpy as np
 import pytest
