@@ -26,9 +26,8 @@
  * multiplied on the matrix cores.  All sums are FP32, in an order that depends
  * on the sizes alone; equal calls give equal bits (a row's bits may depend on
  * B).  z stays FP32 up to y; outputs are rounded once.  In the backward pass
- * g * scale is FP32; where dy is BF16 it enters the product scaled as above and
- * rounded to one F16 part, else in two such parts, or of up to FUSED_FEW_ROWS
- * rows in three BF16 parts where dy is FP32, two (16 bits) where it is F16.  dbias
+ * g * scale is FP32 and enters the product in two such F16 parts, or of up to
+ * FUSED_FEW_ROWS rows in three BF16 parts (two, 16 bits, where dy is F16).  dbias
  * is summed in FP32 from the unrounded g.
  *
  * Data layout (DEVICE pointers):

@@ -156,10 +156,10 @@ int64_t split_bytes(const TilePlan& p, int32_t B, int32_t n_out)
 template <typename OT, int NS>
 void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
 {
-    const TilePlan p = tile_plan(NS, a.B, a.n_out, a.steps);
+    const TilePlan p = tile_plan(NS, a.B, a.n_out, a.w_steps);
     FusedArgs t = a;
     t.splits = p.splits;
-    t.split_steps = (a.steps + p.splits - 1) / p.splits;
+    t.split_steps = (a.w_steps + p.splits - 1) / p.splits * (a.steps / a.w_steps);
     if (p.splits > 1) {
         t.y = part, t.y_type = SPIKE_TYPE_F32, t.ld_y = spk::fused_pad(a.n_out, 8), t.split_stride = t.ld_y * a.B;
         t.scale = t.row_scale = t.bias = nullptr, t.act = 0, t.residual = t.pre = nullptr, t.vec_out = 1;
@@ -271,40 +271,52 @@ int gate_rows(int32_t B)
 }
 int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 
-// What g * scale is kept in between the gate and the product: scaled F16 planes and what
-// undoes the scaling, or (0) FP32 rows where the product takes few of them, which it cuts itself.
-int gate_planes(int y_type, int32_t B) { return y_type == SPIKE_TYPE_BF16 ? 1 : B <= kFewRows ? 0 : 2; }
-int64_t gate_plane_bytes(int y_type, int32_t B, int32_t M)
-{
-    const int ns = gate_planes(y_type, B);
-    return ns == 0 ? spk::fused_pad(plane_stride(M) * B * 4, 16) : planes_bytes(ns, B, M);
-}
-int64_t gate_bytes(int y_type, int32_t B, int32_t M)
-{
-    return gate_plane_bytes(y_type, B, M) + spk::fused_pad((int64_t)B * 4, 16);
-}
+// What g * scale is kept in between the gate and the product: two scaled F16 planes and what
+// undoes the scaling, apart or side by side in a row; or FP32 rows where the product takes few
+// of them, which it cuts itself.  Side by side (a row's planes are whole steps), a tile of one
+// plane walks them one after the other; apart, a tile of two takes them together.  BF16 rows, us,
+// side by side and apart: 6144 -> 1536 inputs, 8192 rows 350 and 329, 64 rows 24.3 and 23.2;
+// 1536 -> 1536, 1000 rows 31 and 33; 1536 -> 6144, 16,384 rows 533 and 543, 500 rows 48 and 33.
+enum GateForm { kGateRows, kGateApart, kGateBeside };
 
-template <typename T, int NS, bool VEC>
+GateForm gate_form(int y_type, int32_t B)
+{
+    return y_type == SPIKE_TYPE_BF16 ? (B <= kFewRows ? kGateRows : kGateBeside)
+                                     : B <= kFewRows ? kGateRows : kGateApart;
+}
+int gate_width(GateForm form, int32_t M) { return (int)spk::fused_pad(M, form == kGateBeside ? spk::kFusedStep : 8); }
+int64_t gate_plane_bytes(GateForm form, int32_t B, int32_t M)
+{
+    return spk::fused_pad((int64_t)gate_width(form, M) * B * 4, 16);  // FP32, or twice 16 bits
+}
+int64_t gate_bytes(GateForm form, int32_t B, int32_t M)
+{
+    return gate_plane_bytes(form, B, M) + spk::fused_pad((int64_t)B * 4, 16);
+}
+// Planes that the product takes at a time.
+int gate_planes(GateForm form) { return form == kGateApart ? 2 : 1; }
+
+template <typename T, bool PLANES, bool VEC>
 void launch_long_gate(const spk::GateArgs& a, hipStream_t st)
 {
-    if (NS > 0 && a.gs)
+    if (PLANES && a.gs)
         hipLaunchKernelGGL((spk::k_fused_gate_top<T, VEC>), dim3((unsigned)a.B), dim3(512), 0, st, a);
     const dim3 grid((unsigned)((a.M + spk::kGateCols - 1) / spk::kGateCols), (unsigned)((a.B + a.rows - 1) / a.rows));
-    hipLaunchKernelGGL((spk::k_fused_gate_columns<T, NS, VEC>), grid, dim3(256), 0, st, a);
+    hipLaunchKernelGGL((spk::k_fused_gate_columns<T, PLANES, VEC>), grid, dim3(256), 0, st, a);
 }
 
 // Returns the parts that the bias gradient came in: gate_parts at most.
-template <typename T, int NS>
+template <typename T, bool PLANES>
 int launch_gate(spk::GateArgs a, bool vec, hipStream_t st)
 {
     a.rows = gate_rows(a.B);
     if (!vec || a.M > 8192) {
         a.rows = std::max(a.rows, 16);
-        vec ? launch_long_gate<T, NS, true>(a, st) : launch_long_gate<T, NS, false>(a, st);
+        vec ? launch_long_gate<T, PLANES, true>(a, st) : launch_long_gate<T, PLANES, false>(a, st);
     } else {
         a.along = (a.M + 511) / 512 * 64;
         a.groups = std::min(a.rows, std::max(1, 768 / a.along));
-        hipLaunchKernelGGL((spk::k_fused_gate<T, NS>), dim3((unsigned)gate_parts(a.B)), dim3(a.along * a.groups),
+        hipLaunchKernelGGL((spk::k_fused_gate<T, PLANES>), dim3((unsigned)gate_parts(a.B)), dim3(a.along * a.groups),
                            (a.groups - 1) * a.along * 32, st, a);
     }
     return (a.B + a.rows - 1) / a.rows;
@@ -405,7 +417,7 @@ int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t 
     if (int rc = check_device(h->device))
         return rc;
     FusedArgs a{};
-    a.P = h->P, a.n_out = h->M, a.n_in = h->K, a.steps = (h->K + spk::kFusedStep - 1) / spk::kFusedStep;
+    a.P = h->P, a.n_out = h->M, a.n_in = h->K, a.steps = a.w_steps = (h->K + spk::kFusedStep - 1) / spk::kFusedStep;
     a.x = x, a.ld_x = ld_x, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
     a.residual = residual, a.ld_residual = ld_residual, a.y = y, a.y_type = y_type, a.ld_y = ld_y;
     a.pre = pre, a.ld_pre = ld_pre;
@@ -439,11 +451,12 @@ int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
 {
     if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(y_type))
         return -1;
-    const int64_t sums = B <= kFewRows ? 0
-                                       : split_bytes(tile_plan(gate_planes(y_type, B), B, h->K,
-                                                               (h->M + spk::kFusedStep - 1) / spk::kFusedStep),
-                                                     B, h->K);
-    return gate_bytes(y_type, B, h->M) + sums + spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
+    const GateForm form = gate_form(y_type, B);
+    const int64_t sums = form == kGateRows ? 0
+                                           : split_bytes(tile_plan(gate_planes(form), B, h->K,
+                                                                   (h->M + spk::kFusedStep - 1) / spk::kFusedStep),
+                                                         B, h->K);
+    return gate_bytes(form, B, h->M) + sums + spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
 }
 
 int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_t ld_dy, const void* pre, int64_t ld_pre,
@@ -478,22 +491,26 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return rc;
     if (act == DENSE_ACT_NONE)
         pre = nullptr;
+    const GateForm form = gate_form(y_type, B);
+    const int width = gate_width(form, h->M);
     int parts = 0;
     float* partial = nullptr;
     float* undo = nullptr;
     if (B > 0) {
-        undo = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_plane_bytes(y_type, B, h->M));
+        undo = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_plane_bytes(form, B, h->M));
         if (dbias)
-            partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M));
+            partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(form, B, h->M));
         spk::GateArgs g{};
         g.dy = dy, g.ld_dy = ld_dy, g.pre = pre, g.ld_pre = ld_pre, g.act = act, g.B = B, g.M = h->M;
-        g.scale = h->scale, g.gs = dx ? workspace : nullptr, g.ld_gs = plane_stride(h->M), g.plane = g.ld_gs * B;
+        g.scale = h->scale, g.gs = dx ? workspace : nullptr, g.width = width;
+        g.ld_gs = form == kGateBeside ? 2 * width : width, g.plane = form == kGateBeside ? width : (int64_t)width * B;
         g.undo = undo, g.partial = partial;
         const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
+        const bool rows = form == kGateRows;
         switch (y_type) {
-        case SPIKE_TYPE_F32: parts = B <= kFewRows ? launch_gate<float, 0>(g, vec, st) : launch_gate<float, 2>(g, vec, st); break;
-        case SPIKE_TYPE_BF16: parts = launch_gate<spk::bf16, 1>(g, vec, st); break;
-        default: parts = B <= kFewRows ? launch_gate<spk::f16, 0>(g, vec, st) : launch_gate<spk::f16, 2>(g, vec, st); break;
+        case SPIKE_TYPE_F32: parts = rows ? launch_gate<float, false>(g, vec, st) : launch_gate<float, true>(g, vec, st); break;
+        case SPIKE_TYPE_BF16: parts = rows ? launch_gate<spk::bf16, false>(g, vec, st) : launch_gate<spk::bf16, true>(g, vec, st); break;
+        default: parts = rows ? launch_gate<spk::f16, false>(g, vec, st) : launch_gate<spk::f16, true>(g, vec, st); break;
         }
     }
     // the bias gradient's parts are summed beside the product of many rows, else by themselves
@@ -504,22 +521,23 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
     if (dx && B > 0) {
         FusedArgs a{};
         // the rows of g * scale are padded with zeros, as the weights are
-        a.P = h->Pt, a.n_out = h->K, a.n_in = (int)plane_stride(h->M), a.steps = (h->M + spk::kFusedStep - 1) / spk::kFusedStep;
-        a.x = workspace, a.ld_x = plane_stride(h->M), a.plane = plane_stride(h->M) * B, a.B = B;
+        a.P = h->Pt, a.n_out = h->K, a.w_steps = (h->M + spk::kFusedStep - 1) / spk::kFusedStep;
+        a.ld_x = form == kGateBeside ? 2 * width : width, a.n_in = (int)a.ld_x;
+        a.steps = form == kGateBeside ? 2 * a.w_steps : a.w_steps;
+        a.x = workspace, a.plane = (int64_t)width * B, a.B = B;
         a.y = dx, a.y_type = x_type, a.ld_y = ld_dx;
         a.vec_out = whole(dx, x_type, ld_dx);
         if (beside)
             a.bias_sums = sums;
-        // the workspace: g * scale (and its rows' scalings), the parts of the bias gradient, the sums of a split product
-        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(y_type, B, h->M) +
-                                               spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
-        const bool few = B <= kFewRows;
-        if (gate_planes(y_type, B) > 0)
+        if (form != kGateRows)
             a.row_scale = undo;
-        switch (y_type) {
-        case SPIKE_TYPE_F32: few ? few_rows<float, 3>(a, true, st) : launch_planes<spk::f16, 2>(a, part, st); break;
-        case SPIKE_TYPE_BF16: few ? few_rows<spk::f16, 1>(a, true, st) : launch_planes<spk::f16, 1>(a, part, st); break;
-        default: few ? few_rows<float, 2>(a, true, st) : launch_planes<spk::f16, 2>(a, part, st); break;
+        // the workspace: g * scale (and its rows' scalings), the parts of the bias gradient, the sums of a split product
+        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(form, B, h->M) +
+                                               spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
+        switch (form) {
+        case kGateRows: y_type == SPIKE_TYPE_F16 ? few_rows<float, 2>(a, true, st) : few_rows<float, 3>(a, true, st); break;
+        case kGateApart: launch_planes<spk::f16, 2>(a, part, st); break;
+        case kGateBeside: launch_planes<spk::f16, 1>(a, part, st); break;
         }
     }
     const hipError_t e = hipGetLastError();

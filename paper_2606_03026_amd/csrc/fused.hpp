@@ -103,7 +103,7 @@ __device__ inline float below_bf16(float x)
     return FIRST && __builtin_isinf(x) ? 0.0f : r;
 }
 
-// Rows of FP32 values enter the product of many rows as NS planes of F16 values: a row is
+// Rows of FP32 values enter the product of many rows as two planes of F16 values: a row is
 // scaled by the power of two that brings its largest size to [2^14, 2^15), then
 // rounded, and what that leaves is rounded again for the second plane.
 __device__ inline float largest(const float (&v)[8], float top)
@@ -144,8 +144,7 @@ __device__ inline float largest_of_waves(float top, float (&s_top)[16], int firs
     return top;
 }
 
-// 8 values at p (and p + plane).  Of an infinite one nothing is left for the second.
-template <int NS>
+// 8 values at p and p + plane.  Of an infinite one nothing is left for the second.
 __device__ inline void put_planes(uint16_t* p, int64_t plane, const float (&v)[8], float factor)
 {
     f16x8 hi, lo;
@@ -153,12 +152,10 @@ __device__ inline void put_planes(uint16_t* p, int64_t plane, const float (&v)[8
     for (int e = 0; e < 8; ++e) {
         const float x = v[e] * factor;
         hi[e] = (f16)in_fp32<f16>(x);
-        if (NS > 1)
-            lo[e] = (f16)(__builtin_isinf(x) ? 0.0f : x - (float)hi[e]);
+        lo[e] = (f16)(__builtin_isinf(x) ? 0.0f : x - (float)hi[e]);
     }
     *reinterpret_cast<f16x8*>(p) = hi;
-    if (NS > 1)
-        *reinterpret_cast<f16x8*>(p + plane) = lo;
+    *reinterpret_cast<f16x8*>(p + plane) = lo;
 }
 
 // 8 activations as they were loaded.
@@ -329,6 +326,7 @@ struct BiasArgs {
 struct FusedArgs {
     const int8_t* P;     // weights, laid out
     int n_out, n_in, steps;
+    int w_steps;         // k_fused_tile: steps of an output's weights; walked again by the steps past them
     const void* x;
     int64_t ld_x;
     int64_t plane;       // elements between the planes of cut activations
@@ -540,10 +538,6 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     for (int v = 1; v < WK; ++v)
         sum += s_sum[v][w][lane];
     const int64_t b = b0 + w % NB * 16 + c;
-    if constexpr (__is_same(XT, f16)) {
-        if (a.row_scale)
-            sum *= a.row_scale[min(b, (int64_t)a.B - 1)];
-    }
     float z[4] = {sum[0], sum[1], sum[2], sum[3]};
     columns.store(a, b, z);
 }
@@ -615,7 +609,8 @@ constexpr int fused_tile_lds()
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
 // activations are NS planes of 16-bit parts (BF16 or F16 rows as they are, FP32
 // ones and gradients in scaled F16 planes), rows of ld_x elements at 16-byte boundaries, n_in a
-// multiple of 8.  A ring of D stages in LDS holds 64 inputs of the rows and, for
+// multiple of 8.  Two planes may also lie side by side in a row (NS = 1): steps past
+// w_steps, the second plane's, take the same weights again.  A ring of D stages in LDS holds 64 inputs of the rows and, for
 // each wave, of its weights; a stage is fetched D - 1 steps ahead by loads that
 // need no registers.  A row of a stage is 8 chunks of 16 bytes; chunk c of row r
 // lies at c ^ (r % 8) (the lanes' global chunks are exchanged), so that an
@@ -630,7 +625,8 @@ constexpr int fused_tile_lds()
 // Bound by how densely the waves issue products between their waits: 16,384 BF16 rows
 // of 1536 -> 6144 with GELU and the values before it 318 us, 972 TFLOP/s (the product
 // alone 279 us, 1108 TFLOP/s); 2500 FP32 rows, two planes, 91 us and 1034 TFLOP/s, the
-// matrix units busy 44% of the time, LDS 4%; 8192 rows of 6144 -> 1536 136 us, 1137 TFLOP/s.
+// matrix units busy 44% of the time, LDS 4%; 8192 rows of 6144 -> 1536, two planes one after
+// the other, 263 us and 1176 TFLOP/s.
 // Codes widened by byte moves and packed F16 sums instead of conversions: no change.
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
 __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
@@ -679,7 +675,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     uint32_t w_at[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)  // tiles past the outputs repeat the last one; their results are not stored
-        w_at[t] = ((uint32_t)min(tile0 + t, tiles - 1) * a.steps + first) * 1024u;
+        w_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * a.w_steps * 1024u;
     __amdgpu_buffer_rsrc_t xr[NS];
 #pragma unroll
     for (int p = 0; p < NS; ++p)
@@ -698,10 +694,11 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     auto fetch = [&](int buf, int s) __attribute__((always_inline)) {
         const bool live = s < steps && (first + s) * kFusedStep + 8 * chunk < a.n_in;
         const uint32_t at = s < steps ? s : 0, to = lds + buf * kStage;
+        const uint32_t step = first + at, w_step = step - (step >= (uint32_t)a.w_steps ? a.w_steps : 0);
         auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + at * 1024u,
+                load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + w_step * 1024u,
                             to + kWeights + (w * MT + t) * 1024);
         };
         if (kWeightsFirst)
@@ -971,7 +968,7 @@ __global__ __launch_bounds__(256) void k_fused_cut(const float* __restrict__ x, 
         for (int k = k0; k < ld; k += 2048) {
             if (k > k0)
                 read_w<float, 8>(p + k, held, vec && k + 8 <= n, n - k);
-            put_planes<2>(out + b * ld + k, plane, held, power.factor);
+            put_planes(out + b * ld + k, plane, held, power.factor);
         }
     }
 }
@@ -1029,6 +1026,7 @@ struct GateArgs {
     int along, groups;    // k_fused_gate: threads of a row, and the rows that a workgroup has at a time
     const float* scale;   // [M rounded up to 16]
     void* gs;             // NULL: only the bias gradient
+    int width;            // elements that a row of gs has in a plane: M and zeros
     int64_t ld_gs, plane; // elements between rows and planes of gs
     float* undo;          // [B] inverses of the rows' scalings
     float* partial;       // [workgroups down][M] column sums of g, or NULL
@@ -1036,26 +1034,24 @@ struct GateArgs {
 
 // Rows of up to 8,192 outputs in whole vectors: a workgroup walks `rows` of them, `groups`
 // at a time, g * scale of a row staying in registers until the row's largest is known, and
-// goes to gs in NS scaled F16 planes (NS = 0: as FP32 rows).  BF16 dy take one plane (11
-// bits: dx of 8192 rows is off by 0.0017 of its size, which is the rounding of dx itself;
-// one BF16 plane left 0.0023), F16 and FP32 ones two.  A thread has one vector of outputs
-// and their sums over the rows, which the groups join in LDS and leave in
+// goes to gs in two scaled F16 planes (PLANES; else as FP32 rows): g * scale is an FP32
+// value whatever the type of dy, and dx may be FP32 (one plane, 11 bits, left 2e-4 of its
+// size there).  A thread has one vector of outputs and their sums over the rows, which the groups join in LDS and leave in
 // partial[workgroup]; the next row's loads are on their way while this one's largest is
 // found.  Bound by memory, and about as much by the slope's arithmetic (8192 rows of
-// 6144, BF16, 302 MB: 65 us, 4.7 TB/s; with the product behind 205 us, 213 without the
-// loads ahead, 215 in 256 workgroups, 208 in 1024).
+// 6144, BF16, 403 MB: 87 us, 4.6 TB/s).
 constexpr int kGateParts = 512;  // the most parts that the bias gradient comes in
 
-template <typename T, int NS>
+template <bool PLANES>
 __device__ inline void gate_put(const GateArgs& a, int64_t b, int m, const float (&v)[8], float factor)
 {
-    if constexpr (NS == 0)
-        write_w<float, 8>(static_cast<float*>(a.gs) + b * a.ld_gs + m, v, true, 8);
+    if constexpr (PLANES)
+        put_planes(static_cast<uint16_t*>(a.gs) + b * a.ld_gs + m, a.plane, v, factor);
     else
-        put_planes<NS>(static_cast<uint16_t*>(a.gs) + b * a.ld_gs + m, a.plane, v, factor);
+        write_w<float, 8>(static_cast<float*>(a.gs) + b * a.ld_gs + m, v, true, 8);
 }
 
-template <typename T, int NS>
+template <typename T, bool PLANES>
 __global__ __launch_bounds__(1024) void k_fused_gate(GateArgs a)
 {
     __shared__ float s_top[2][16];
@@ -1091,13 +1087,13 @@ __global__ __launch_bounds__(1024) void k_fused_gate(GateArgs a)
         if (!a.gs)
             continue;
         RowPower power{};
-        if constexpr (NS > 0) {
+        if constexpr (PLANES) {
             power = row_power(largest_of_waves(largest(g, 0.0f), s_top[turn], group * waves, waves));
             if (live && m0 == 0)
                 a.undo[b] = power.undo;
         }
-        if (live && m0 < a.ld_gs)
-            gate_put<T, NS>(a, b, m0, g, power.factor);
+        if (live && m0 < a.width)
+            gate_put<PLANES>(a, b, m0, g, power.factor);
     }
     if (!a.partial)
         return;
@@ -1145,7 +1141,7 @@ __global__ __launch_bounds__(512) void k_fused_gate_top(GateArgs a)
 
 constexpr int kGateCols = 256;
 
-template <typename T, int NS, bool VEC>
+template <typename T, bool PLANES, bool VEC>
 __global__ __launch_bounds__(256) void k_fused_gate_columns(GateArgs a)
 {
     const int m = blockIdx.x * kGateCols + threadIdx.x % 32 * 8;
@@ -1154,7 +1150,7 @@ __global__ __launch_bounds__(256) void k_fused_gate_columns(GateArgs a)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
         sc[e] = m + e < a.M ? a.scale[m + e] : 0.0f;
-    if (m < a.M)
+    if (m < a.width)  // (g past M is 0)
         for (int64_t b = b0 + threadIdx.x / 32; b < b1; b += 8) {
             float g[8];
             gate_values(gate_read<T, VEC>(static_cast<const T*>(a.dy) + b * a.ld_dy, static_cast<const T*>(a.pre) + b * a.ld_pre,
@@ -1166,7 +1162,7 @@ __global__ __launch_bounds__(256) void k_fused_gate_columns(GateArgs a)
             }
             // (the power is the inverse of its inverse: 254 less its exponent)
             if (a.gs)
-                gate_put<T, NS>(a, b, m, g, NS == 0 ? 1.0f : __uint_as_float((254u << 23) - __float_as_uint(a.undo[b])));
+                gate_put<PLANES>(a, b, m, g, PLANES ? __uint_as_float((254u << 23) - __float_as_uint(a.undo[b])) : 1.0f);
         }
     if (!a.partial)
         return;

@@ -1,0 +1,75 @@
+"""How many bits of an operand the fused projection keeps (dense_fused.h).
+
+Every output here has one code that is not zero, so it is a single product and
+nothing of a sum's rounding hides what an operand lost.  With u = 2^-24 and q
+the code:
+
+    rows of up to FUSED_FEW_ROWS: every bit of an FP32 operand takes part; its
+    parts' products (exact) are added and scaled: 4 u of the result
+    more rows: an FP32 operand enters to 2^-23 of itself or 2^-39 of its row's
+    largest, whichever is more; then 4 u as above
+
+In the gradient g * scale is the operand, rounded once: 1 u more.  2^-149 (1 + |q|)
+is for values that are subnormal.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import step_oracle as so
+from tests.test_fused_gpu import TYPES, act_code, dev, handle, host
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+FEW = 32
+
+
+@pytest.fixture(scope="module")
+def sp():
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2606_03026_amd import _binding
+    return _binding
+
+
+def one_code(r, outputs, inputs):
+    """Codes [outputs][inputs] of which one in each row is not zero."""
+    Q = np.zeros((outputs, inputs), np.int8)
+    Q[np.arange(outputs), r.integers(0, inputs, outputs)] = r.choice([-127, -90, -3, 1, 2, 55, 100, 127], outputs)
+    return Q
+
+
+def columns(Q):
+    return np.ascontiguousarray(Q.T)
+
+
+def limit(want, operand, Q, rows, extra):
+    """operand: [B][n] as it enters, Q: [outputs][n] with one code a row."""
+    q = np.abs(Q.astype(np.float64)).sum(axis=1)
+    lim = (4 + extra) * U * np.abs(want) + 2.0 ** -149 * (1 + q)
+    if rows > FEW:
+        lim = lim + 2.0 ** -23 * np.abs(want) + 2.0 ** -39 * np.abs(operand).max(axis=1, keepdims=True) * q
+    return lim
+
+
+SIZES = [(200, 200, 0, 0), (200, 1000, 0, 0), (96, 2100, 3, 1), (64, 8200, 0, 0), (101, 90, 0, 0)]
+
+
+@pytest.mark.parametrize("B", [1, 20, 32, 33, 70, 600])
+@pytest.mark.parametrize("K,M,pad,offset", SIZES)
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+def test_gradient_operand(sp, B, K, M, pad, offset, yk, act):
+    """g * scale is an FP32 value whatever the type of dy, and dx may be FP32."""
+    r = np.random.default_rng([41, B, K, M])
+    p = {"Q": columns(one_code(r, K, M)), "scale": r.uniform(0.5, 1.5, M).astype(np.float32)}
+    dy, z = dev(r.normal(size=(B, M)), yk, pad, offset), dev(r.normal(size=(B, M)), yk, pad, offset)
+    dx = torch.full((B, K), float("nan"), device="cuda")
+    h = handle(sp, p, backward=True)
+    sp.dense_fused_backward(h, dy, dx=dx, pre=z if act != "none" else None, act=act_code(sp, act))
+    torch.cuda.synchronize()
+    want, _, g = so.fused_backward(p["Q"], np.ones(M), host(dy) * p["scale"].astype(np.float64), host(z), act)
+    lim = limit(want, g, columns(p["Q"]), B, 1)
+    got = host(dx)
+    assert (np.abs(got - want) <= lim).all(), np.nanmax(np.abs(got - want) / lim)
+    h.close()
