@@ -27,8 +27,8 @@
  * on the sizes alone; equal calls give equal bits (a row's bits may depend on
  * B).  z stays FP32 up to y; outputs are rounded once.  In the backward pass
  * g * scale is FP32 and enters the product in two such F16 parts, or of up to
- * FUSED_FEW_ROWS rows in three BF16 parts (two, 16 bits, where dy is F16).  dbias
- * is summed in FP32 from the unrounded g.
+ * FUSED_FEW_ROWS rows in three BF16 parts.  dbias is summed in FP32 from the
+ * unrounded g.
  *
  * Data layout (DEVICE pointers):
  *   Q         int8 [M][K] row-major, scale float [M] (as in dense_proj.h); read

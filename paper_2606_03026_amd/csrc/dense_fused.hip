@@ -535,7 +535,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(form, B, h->M) +
                                                spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
         switch (form) {
-        case kGateRows: y_type == SPIKE_TYPE_F16 ? few_rows<float, 2>(a, true, st) : few_rows<float, 3>(a, true, st); break;
+        case kGateRows: few_rows<float, 3>(a, true, st); break;
         case kGateApart: launch_planes<spk::f16, 2>(a, part, st); break;
         case kGateBeside: launch_planes<spk::f16, 1>(a, part, st); break;
         }

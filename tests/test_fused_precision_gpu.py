@@ -57,7 +57,7 @@ SIZES = [(200, 200, 0, 0), (200, 1000, 0, 0), (96, 2100, 3, 1), (64, 8200, 0, 0)
 
 @pytest.mark.parametrize("B", [1, 20, 32, 33, 70, 600])
 @pytest.mark.parametrize("K,M,pad,offset", SIZES)
-@pytest.mark.parametrize("yk", ["bf16", "f32"])
+@pytest.mark.parametrize("yk", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("act", ["none", "relu"])
 def test_gradient_operand(sp, B, K, M, pad, offset, yk, act):
     """g * scale is an FP32 value whatever the type of dy, and dx may be FP32."""
