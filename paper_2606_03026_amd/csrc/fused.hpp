@@ -205,10 +205,12 @@ __device__ inline __amdgpu_buffer_rsrc_t rows_resource(const XT* row0)
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<XT*>(row0), 0, (int)kBufMaxBytes, kBufferFlags);
 }
 
-// Their NS operand parts.
+// Their NS operand parts.  Returns (in its lower half) what three parts leave of FP32 values:
+// BF16's smallest step is 2^-133, FP32's 2^-149.
 template <typename XT, int NS>
-__device__ inline void split_raw(const Raw<XT>& r, u32x4 (&part)[NS])
+__device__ inline uint32_t split_raw(const Raw<XT>& r, u32x4 (&part)[NS])
 {
+    uint32_t left = 0;
     if constexpr (sizeof(XT) == 4) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -221,9 +223,29 @@ __device__ inline void split_raw(const Raw<XT>& r, u32x4 (&part)[NS])
                     b = s == 0 ? below_bf16<true>(b) : below_bf16<false>(b);
                 }
             }
+            left |= __float_as_uint(a) | __float_as_uint(b);
         }
     } else {
         part[0] = r.v;
+    }
+    return left & 0xffffu;
+}
+
+// That rest: the lower 16 bits of a subnormal value, as two operands of 8 bits in units of 2^-149.
+__device__ inline void split_rest(const Raw<float>& r, u32x4 (&part)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float v[2][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float x = below_bf16<false>(below_bf16<true>(r.v[i / 2][i % 2 * 2 + e]));
+            const uint32_t bits = __float_as_uint(x);
+            v[0][e] = __builtin_copysignf((float)(bits & 0xff00u), x);
+            v[1][e] = __builtin_copysignf((float)(bits & 0xffu), x);
+        }
+        part[0][i] = high_halves(v[0][0], v[0][1]);
+        part[1][i] = high_halves(v[1][0], v[1][1]);
     }
 }
 
@@ -451,8 +473,10 @@ struct OutputColumns {
 
 // Up to 16 NB rows: a workgroup takes 16 MT outputs and all inputs, its WK
 // waves sharing the 64-input steps; the waves' sums are joined in LDS.  Bound
-// by the weights' bytes (1536 -> 57,344, one FP32 row: 17.4 us, 5.1 TB/s), where these
-// are few by latency (1536 -> 6144, one FP32 row: 5.1 us; 1536 -> 1536, 7 BF16 rows: 4.0).
+// by the weights' bytes (1536 -> 57,344, one FP32 row: 19.6 us, 4.5 TB/s; BF16 16.8, 5.2),
+// where these are few by latency (1536 -> 6144, one FP32 row: 5.1 us; 1536 -> 1536, 7 BF16
+// rows: 3.3).  Asking whether three parts left anything costs 0 to 8% of an FP32 call (6144 ->
+// 1536, 7 rows: 10.2 us without, 11.3).
 // Rows that are not there cost no loads, only idle columns of the matrix instruction.
 template <typename XT, int NS, int NB, int MT, int WK, bool VECX>
 __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
@@ -514,12 +538,21 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     u32x4 part[NS];
-                    split_raw<XT, NS>(x[u][n][h], part);
+                    const uint32_t left = split_raw<XT, NS>(x[u][n][h], part);
 #pragma unroll
                     for (int p = 0; p < NS; ++p)
 #pragma unroll
                         for (int t = 0; t < MT; ++t)
                             acc[t][n] = mfma16<OT>(wo[t], part[p], acc[t][n]);
+                    if constexpr (NS == 3) {
+                        if (__builtin_expect(__any(left != 0), 0)) {  // (values below 2^-110 only)
+                            u32x4 rest[2];
+                            split_rest(x[u][n][h], rest);
+#pragma unroll
+                            for (int t = 0; t < MT; ++t)
+                                acc[t][n] += mfma16<OT>(wo[t], rest[0], mfma16<OT>(wo[t], rest[1], f32x4{})) * 0x1p-149f;
+                        }
+                    }
                 }
             }
         }

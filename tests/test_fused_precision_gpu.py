@@ -43,12 +43,12 @@ def columns(Q):
     return np.ascontiguousarray(Q.T)
 
 
-def limit(want, operand, Q, rows, extra):
-    """operand: [B][n] as it enters, Q: [outputs][n] with one code a row."""
+def limit(want, operand, Q, rows, extra, scale=1.0):
+    """operand: [B][n] as it enters, Q: [outputs][n] with one code a row, scale: of the outputs."""
     q = np.abs(Q.astype(np.float64)).sum(axis=1)
-    lim = (4 + extra) * U * np.abs(want) + 2.0 ** -149 * (1 + q)
+    lim = (4 + extra) * U * np.abs(want) + 2.0 ** -149 * (1 + q) * np.maximum(scale, 1)
     if rows > FEW:
-        lim = lim + 2.0 ** -23 * np.abs(want) + 2.0 ** -39 * np.abs(operand).max(axis=1, keepdims=True) * q
+        lim = lim + 2.0 ** -23 * np.abs(want) + 2.0 ** -39 * np.abs(operand).max(axis=1, keepdims=True) * q * scale
     return lim
 
 
@@ -70,6 +70,45 @@ def test_gradient_operand(sp, B, K, M, pad, offset, yk, act):
     torch.cuda.synchronize()
     want, _, g = so.fused_backward(p["Q"], np.ones(M), host(dy) * p["scale"].astype(np.float64), host(z), act)
     lim = limit(want, g, columns(p["Q"]), B, 1)
+    got = host(dx)
+    assert (np.abs(got - want) <= lim).all(), np.nanmax(np.abs(got - want) / lim)
+    h.close()
+
+
+def wide(r, B, n):
+    """FP32 values of every size up to 1e34, subnormal ones among them."""
+    x = r.uniform(1, 2, (B, n)) * r.choice([-1, 1], (B, n)) * 10.0 ** r.uniform(-44, 33, (B, n))
+    return x.astype(np.float32)
+
+
+@pytest.mark.parametrize("B", [1, 16, 20, 32, 33, 300])
+@pytest.mark.parametrize("K,M", [(130, 130), (300, 5000), (64, 33000)])
+def test_wide_activations(sp, B, K, M):
+    """FP32 activations of any size beside each other: up to FUSED_FEW_ROWS rows keep all of their bits."""
+    r = np.random.default_rng([42, B, K, M])
+    p = {"Q": one_code(r, M, K), "scale": r.uniform(0.5, 1.5, M).astype(np.float32)}
+    x, y = dev(wide(r, B, K)), torch.full((B, M), float("nan"), device="cuda")
+    h = handle(sp, p)
+    sp.dense_fused_forward(h, x, y)
+    torch.cuda.synchronize()
+    want = so.fused_pre(p["Q"], p["scale"], host(x))
+    lim = limit(want, host(x), p["Q"], B, 0, p["scale"].astype(np.float64))
+    got = host(y)
+    assert (np.abs(got - want) <= lim).all(), np.nanmax(np.abs(got - want) / lim)
+    h.close()
+
+
+@pytest.mark.parametrize("B", [1, 32, 33, 300])
+def test_wide_gradients(sp, B):
+    r = np.random.default_rng([43, B])
+    p = {"Q": columns(one_code(r, 150, 150)), "scale": (2.0 ** r.integers(-3, 3, 150)).astype(np.float32)}
+    dy, dx = dev(wide(r, B, 150)), torch.full((B, 150), float("nan"), device="cuda")
+    h = handle(sp, p, backward=True)
+    sp.dense_fused_backward(h, dy, dx=dx)
+    torch.cuda.synchronize()
+    want, _, _ = so.fused_backward(p["Q"], p["scale"], host(dy))
+    # (g * scale rounds to a multiple of 2^-149 where it is subnormal)
+    lim = limit(want, host(dy) * p["scale"], columns(p["Q"]), B, 1) + 2.0 ** -149 * 127
     got = host(dx)
     assert (np.abs(got - want) <= lim).all(), np.nanmax(np.abs(got - want) / lim)
     h.close()
