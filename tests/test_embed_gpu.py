@@ -222,3 +222,21 @@ def test_refusals(sp):
         sp.spike_embed_backward(out[:, :11], ids, t)
     with pytest.raises(sp.SpikeError, match="workspace"):
         sp.spike_embed_backward(out, ids, t, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("T", [23, 24, 25, 47, 48, 49, 71, 72, 73])
+@pytest.mark.parametrize("D,kind", [(40, "f32"), (37, "bf16")])
+def test_ends_of_runs(sp, T, D, kind):
+    """Token counts around the run length (24) and its multiples: one row for all tokens, rows that begin and
+    end at every place of a run, padding behind them."""
+    r = np.random.default_rng([26, T, D])
+    g = rows(r.integers(-3, 4, (T, D)), kind)
+    start = r.integers(-5, 6, (9, D)).astype(np.float32)
+    for ids in [np.full(T, 4), np.where(np.arange(T) < T - 1, 2, -1)] + [np.where(np.arange(T) < c, 1, 7) for c in (1, 22, 23, 24, 25, T - 1)]:
+        ids = r.permutation(ids)
+        for accumulate in (False, True):
+            dt = rows(start, "f32")
+            sp.spike_embed_backward(g, torch.from_numpy(ids).cuda(), dt, accumulate=accumulate)
+            torch.cuda.synchronize()
+            want = so.embed_backward(g.double().cpu().numpy(), ids, 9, 1.0, start if accumulate else None)
+            assert (dt.double().cpu().numpy() == want).all(), (ids.tolist(), accumulate)

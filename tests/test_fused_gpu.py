@@ -528,3 +528,18 @@ def test_backward_forms(sp, yk, K, M, B):
     assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)))
     assert (db.cpu().numpy() == wb).all()
     h.close()
+
+
+@pytest.mark.parametrize("xk,yk", [("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("K,M,B", [(6000, 70, 40), (2000, 72, 40), (1000, 520, 300), (200, 96, 9)])
+def test_residual_in_place_of_every_form(sp, xk, yk, K, M, B):
+    """y is the residual: the sums in one part, split over workgroups and joined, and few rows, give the same as apart."""
+    p = problem(K, M, B)
+    h = handle(sp, p)
+    x, r = dev(p["x"], xk), dev(p["residual"], yk)
+    y = torch.empty_like(r)
+    sp.dense_fused_forward(h, x, y, act=sp.DENSE_ACT_GELU, residual=r)
+    sp.dense_fused_forward(h, x, r, act=sp.DENSE_ACT_GELU, residual=r)
+    torch.cuda.synchronize()
+    assert torch.isfinite(y.float()).all() and torch.equal(r, y)
+    h.close()
