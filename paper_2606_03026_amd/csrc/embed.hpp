@@ -77,7 +77,8 @@ constexpr int kSortPartKeys = kSortChunk / kSortParts;
 constexpr int kSortPartStride = kSortPartKeys + 4;  // the parts' reads fall into different LDS banks
 
 // Rows [first, first + count) of a table whose rows of `bytes` bytes lie `step`
-// bytes apart, to be zeroed by workgroups of kFillRows rows each.
+// bytes apart, to be zeroed by workgroups of kFillRows rows each, and as many again
+// kFillWgs groups on: a launch has to stay below 2^32 threads, a table of 2^28 rows has not.
 struct FillArgs {
     char* table;
     int64_t step, bytes;
@@ -86,7 +87,8 @@ struct FillArgs {
 };
 
 constexpr int kFillRows = 8;
-inline int64_t fill_wgs(const FillArgs& f) { return ((int64_t)f.count + kFillRows - 1) / kFillRows; }
+constexpr int kFillWgs = 1 << 20;  // the most workgroups that zero rows in a launch
+inline int fill_wgs(const FillArgs& f) { return f.count / kFillRows < kFillWgs ? (f.count + kFillRows - 1) / kFillRows : kFillWgs; }
 
 __device__ inline void zero_row(const FillArgs& f, int row)
 {
@@ -102,12 +104,13 @@ __device__ inline void zero_row(const FillArgs& f, int row)
 // All of this workgroup's rows.
 __device__ inline void zero_rows(const FillArgs& f, int wg)
 {
-    for (int r = threadIdx.x / 64; r < kFillRows && wg * kFillRows + r < f.count; r += kEmbedBlock / 64)
-        zero_row(f, f.first + wg * kFillRows + r);
+    for (int row0 = wg * kFillRows; row0 < f.count; row0 += kFillWgs * kFillRows)
+        for (int r = row0 + threadIdx.x / 64; r < row0 + kFillRows && r < f.count; r += kEmbedBlock / 64)
+            zero_row(f, f.first + r);
 }
 
-// Those of its rows that none of the T sorted keys names.
-__device__ inline void zero_unnamed_rows(const FillArgs& f, int wg, const uint32_t* __restrict__ keys, int T)
+// Those of a group's rows that none of the T sorted keys names.
+__device__ inline void zero_unnamed_group(const FillArgs& f, int wg, const uint32_t* __restrict__ keys, int T)
 {
     __shared__ int named[kFillRows];
     const int v0 = f.first + wg * kFillRows;
@@ -135,6 +138,14 @@ __device__ inline void zero_unnamed_rows(const FillArgs& f, int wg, const uint32
     for (int r = threadIdx.x / 64; r < kFillRows && wg * kFillRows + r < f.count; r += kEmbedBlock / 64)
         if (!named[r])
             zero_row(f, v0 + r);
+}
+
+__device__ inline void zero_unnamed_rows(const FillArgs& f, int wg, const uint32_t* __restrict__ keys, int T)
+{
+    for (int group = wg; group * kFillRows < f.count; group += kFillWgs) {
+        zero_unnamed_group(f, group, keys, T);
+        __syncthreads();  // (its marks are read)
+    }
 }
 
 // Sorts each chunk of kSortChunk tokens by (key, position): a token's place

@@ -240,3 +240,21 @@ def test_ends_of_runs(sp, T, D, kind):
             torch.cuda.synchronize()
             want = so.embed_backward(g.double().cpu().numpy(), ids, 9, 1.0, start if accumulate else None)
             assert (dt.double().cpu().numpy() == want).all(), (ids.tolist(), accumulate)
+
+
+@pytest.mark.parametrize("V,D", [(3 * 2 ** 23 + 5, 8), (2 ** 23 + 9, 3), (2 ** 28, 8)])
+@pytest.mark.parametrize("T", [0, 20, 100, 5000])
+def test_tables_of_many_rows(sp, V, D, T):
+    """More rows than the zeroing workgroups of a launch take once: all of them end up written."""
+    r = np.random.default_rng([27, V % 1000, D, T])
+    ids = np.where(r.random(T) < 0.5, r.integers(0, V, T), r.choice([0, V - 1, V // 2, 2 ** 23, 2 ** 23 - 1], T))
+    g = rows(r.integers(-3, 4, (T, D)).reshape(T, D), "bf16")
+    dt = torch.full((V, D), 5.0, dtype=torch.bfloat16, device="cuda")
+    sp.spike_embed_backward(g, torch.from_numpy(ids).cuda(), dt)
+    torch.cuda.synchronize()
+    named, place = np.unique(ids, return_inverse=True)
+    want = torch.from_numpy(so.embed_backward(g.double().cpu().numpy(), place, len(named), 1.0)).float().to(torch.bfloat16)
+    at = torch.from_numpy(named).cuda()
+    assert torch.equal(dt[at].cpu(), want)
+    dt[at] = 0
+    assert not any(bool(part.any()) for part in dt.view(-1).split(1 << 28))
