@@ -127,8 +127,9 @@ struct Grad {
 template <typename TG>
 constexpr int vector_of() { return sizeof(TG) == 4 ? 4 : 8; }
 
+// (a launch that failed is the last one: the next reads what it should have written)
 template <typename TG, typename TD, int VEC>
-void launch_grad(const Grad& a, const spk::FillArgs& fill, const spk::FillArgs& with_join)
+hipError_t launch_grad(const Grad& a, const spk::FillArgs& fill, const spk::FillArgs& with_join)
 {
     constexpr int waves = spk::kEmbedBlock / 64;
     const int64_t blocks = (a.D + 64 * VEC - 1) / (64 * VEC);
@@ -139,14 +140,17 @@ void launch_grad(const Grad& a, const spk::FillArgs& fill, const spk::FillArgs& 
         hipLaunchKernelGGL((spk::k_embed_sum<TG, TD, VEC>), dim3((unsigned)wgs), dim3(spk::kEmbedBlock), 0, a.st,
                            static_cast<const TG*>(a.grad), a.ld_grad, a.ws.keys, a.ws.order, a.T, a.D, (int)sum_wgs,
                            a.scale, a.accumulate, static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, fill);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess)
+        return e;
     if (runs > 1)
         hipLaunchKernelGGL((spk::k_embed_join<TD, VEC>), dim3((unsigned)(sum_wgs + spk::fill_wgs(with_join))),
                            dim3(spk::kEmbedBlock), 0, a.st, a.ws.keys, a.T, a.D, a.scale, a.accumulate,
                            static_cast<TD*>(a.dtable), a.ld_table, a.ws.partial, (int)sum_wgs, with_join);
+    return hipGetLastError();
 }
 
 template <typename TG>
-void grad_table(const Grad& a, int table_type, bool vec, const spk::FillArgs& fill, const spk::FillArgs& with_join)
+hipError_t grad_table(const Grad& a, int table_type, bool vec, const spk::FillArgs& fill, const spk::FillArgs& with_join)
 {
     constexpr int V = vector_of<TG>();
     switch (table_type) {
@@ -271,18 +275,22 @@ int spike_embed_backward(const void* grad, int32_t grad_type, int64_t ld_grad, c
         else
             hipLaunchKernelGGL(spk::k_embed_sort<int32_t>, grid, block, 0, a.st, static_cast<const int32_t*>(ids), T, V,
                                k, o, wgs, with_sort);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess)
+            return hip_fail(e, "embedding gradient launch");
         if (!one) {
             const spk::FillArgs with_merge = take_rows(&fill, beside_merge);
             hipLaunchKernelGGL(spk::k_embed_merge, dim3((unsigned)(wgs + spk::fill_wgs(with_merge))), block, 0, a.st, k, o,
                                T, a.ws.keys, a.ws.order, wgs, with_merge);
+            if (const hipError_t e = hipGetLastError(); e != hipSuccess)
+                return hip_fail(e, "embedding gradient launch");
         }
     }
+    hipError_t e = hipSuccess;
     switch (grad_type) {
-    case SPIKE_TYPE_F32: grad_table<float>(a, table_type, vec, fill, with_join); break;
-    case SPIKE_TYPE_BF16: grad_table<spk::bf16>(a, table_type, vec, fill, with_join); break;
-    default: grad_table<spk::f16>(a, table_type, vec, fill, with_join); break;
+    case SPIKE_TYPE_F32: e = grad_table<float>(a, table_type, vec, fill, with_join); break;
+    case SPIKE_TYPE_BF16: e = grad_table<spk::bf16>(a, table_type, vec, fill, with_join); break;
+    default: e = grad_table<spk::f16>(a, table_type, vec, fill, with_join); break;
     }
-    const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "embedding gradient launch");
 }
 

@@ -106,3 +106,16 @@ def test_zeroing_of_the_largest_tables(record):
         assert launches and all(g * b < 1 << 32 and g < 1 << 31 for g, b in launches), (s, launches)
     (rc, launches), = record([gradient(0, 57344, 1536)])
     assert launches == [[57344 // 8, 256]]
+
+
+SPIKE_EHIP = -2
+
+
+@pytest.mark.parametrize("T,n", [(20, 2), (100, 3), (5000, 4)])
+def test_nothing_follows_a_failed_launch_of_the_embedding_gradient(record, T, n):
+    """The sums take rows by the keys and positions that the sorting wrote."""
+    for fail in range(n):
+        (rc, launches), = record([gradient(T, 1000, 64, fail=fail)])
+        assert rc == SPIKE_EHIP and len(launches) == fail + 1, (fail, launches)
+    (rc, launches), = record([gradient(T, 1000, 64)])
+    assert rc == 0 and len(launches) == n
