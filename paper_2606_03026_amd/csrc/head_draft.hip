@@ -53,8 +53,9 @@ Plan make_plan(int32_t S, int32_t G, int32_t V, bool dist)
     return p;
 }
 
+// (the race reads what the statistics wrote or cleared: it does not follow if they were refused)
 template <typename T, int VEC>
-void launch(const spk::DraftArgs& a, hipStream_t st)
+hipError_t launch(const spk::DraftArgs& a, hipStream_t st)
 {
     const dim3 block(spk::kDraftBlock), stats((unsigned)((int64_t)a.S * a.rows * a.parts)),
         race((unsigned)((int64_t)a.S * a.race_parts));
@@ -62,10 +63,13 @@ void launch(const spk::DraftArgs& a, hipStream_t st)
         hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 1>), stats, block, 0, st, a);
     else
         hipLaunchKernelGGL((spk::k_draft_stats<T, VEC, 2>), stats, block, 0, st, a);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess)
+        return e;
     if (a.race_len <= spk::kDraftStretch)
         hipLaunchKernelGGL((spk::k_draft_race<T, VEC, 1>), race, block, 0, st, a);
     else
         hipLaunchKernelGGL((spk::k_draft_race<T, VEC, 2>), race, block, 0, st, a);
+    return hipGetLastError();
 }
 
 bool rows_vectorize(const void* p, int type, int64_t ld) { return aligned_to(p, 16) && ld * spk::type_bytes(type) % 16 == 0; }
@@ -124,12 +128,12 @@ int head_draft_verify(const void* target, int64_t ld_target, const void* draft, 
                      (!dist || rows_vectorize(draft, logits_type, ld_draft)) &&
                      rows_vectorize(noise, SPIKE_TYPE_F32, ld_noise);
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
     switch (logits_type) {
-    case SPIKE_TYPE_F32: vec ? launch<float, 8>(a, st) : launch<float, 1>(a, st); break;
-    case SPIKE_TYPE_BF16: vec ? launch<spk::bf16, 8>(a, st) : launch<spk::bf16, 1>(a, st); break;
-    default: vec ? launch<spk::f16, 8>(a, st) : launch<spk::f16, 1>(a, st); break;
+    case SPIKE_TYPE_F32: e = vec ? launch<float, 8>(a, st) : launch<float, 1>(a, st); break;
+    case SPIKE_TYPE_BF16: e = vec ? launch<spk::bf16, 8>(a, st) : launch<spk::bf16, 1>(a, st); break;
+    default: e = vec ? launch<spk::f16, 8>(a, st) : launch<spk::f16, 1>(a, st); break;
     }
-    const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "draft verification launch");
 }
 

@@ -119,3 +119,24 @@ def test_nothing_follows_a_failed_launch_of_the_embedding_gradient(record, T, n)
         assert rc == SPIKE_EHIP and len(launches) == fail + 1, (fail, launches)
     (rc, launches), = record([gradient(T, 1000, 64)])
     assert rc == 0 and len(launches) == n
+
+
+def verify(S, G, V, fail=-1):
+    return ["head_draft_verify", "plplipppplpiiippppplp",
+            [D, V, D, V, F32, D, None, D, D, V, None, S, G, V, D, D, None, None, D, 1 << 40, None], fail]
+
+
+def test_nothing_follows_a_failed_launch_of_the_draft_verification(record):
+    """The race goes by the statistics and the record that the first kernel wrote or cleared."""
+    for S, G, V in ((1, 4, 57344), (64, 4, 57344), (3, 0, 50)):
+        for fail, n in ((0, 1), (1, 2)):
+            (rc, launches), = record([verify(S, G, V, fail)])
+            assert rc == SPIKE_EHIP and len(launches) == n
+        (rc, launches), = record([verify(S, G, V)])
+        assert rc == 0 and len(launches) == 2
+
+
+def test_largest_draft_verifications(record):
+    sizes = [(S, G, V) for S in (1, 64, 4096) for G in (0, 31) for V in (1, 57344, 1 << 30)]
+    for s, (rc, launches) in zip(sizes, record([verify(*s) for s in sizes])):
+        assert rc == 0 and all(g * b < 1 << 32 for g, b in launches), (s, launches)
