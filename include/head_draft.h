@@ -10,7 +10,7 @@
  *     draft i is accepted iff uniform_i * q_i(d_i) < p_i(d_i) and every earlier one is
  *     j = number of accepted drafts
  *     r = max(p_j - q_j, 0); r = p_j after the last draft, and where p_j - q_j is positive nowhere
- *     next token = the v with the largest r(v) / noise(v), the lowest such v; -1 where r is zero throughout
+ *     next token = the v with the largest r(v) / noise(v), the lowest such v; -1 where none is positive
  *
  * With uniform_i uniform on [0, 1) and noise(v) exponential with mean one
  * (an exponential race: v wins with probability r(v) / sum r), the tokens are
@@ -24,7 +24,8 @@
  *    probability equally.  A row without any other logit has probability zero
  *    throughout: its draft is refused, and its next token is -1.
  *  - A drafted token outside [0, V) has probability zero and is refused.
- *  - noise entries that are not positive never win.
+ *  - noise entries that are not positive, or so large that the quotient is zero,
+ *    never win, nor do others in their place: r is as above.
  *
  * Precision: FP32, with the hardware's base-2 exponential and reciprocal (of
  * noise; within one unit in the last place); the sums of the exponentials are

@@ -25,9 +25,9 @@ struct DraftPart {
     float sum;
 };
 
-// Per sequence, for the race: the best r(v) / noise(v), or where there is none the
+// Per sequence, for the race: the best r(v) / noise(v), or where r is zero throughout the
 // best p(v) / noise(v), as a code that is larger the better the value and, of equal
-// values, the lower v; 0: none.  `done` counts the workgroups that have added theirs.
+// values, the lower v; upper half without its sign 0: none.  `done` counts the workgroups that have added theirs.
 struct DraftBest {
     unsigned long long code;
     unsigned int done, pad;
@@ -264,13 +264,14 @@ __device__ inline float draft_prob(const DraftDist& d, float x, int v, bool hot,
     return x == -INFINITY ? 0.0f : draft_term(x, d.top, rate) * d.scale;
 }
 
-// r / noise wins over every p / noise; both are positive, so their bits are ordered as they are.
+// A token of the residual goes before every other, one that its noise keeps from winning
+// (a score of 0) too: then r is not zero throughout.  No score is negative, so their bits
+// are ordered as they are.
 __device__ inline unsigned long long draft_code(float score, int v, bool residual)
 {
-    if (!(score > 0.0f))
-        return 0ull;
     return (unsigned long long)(__float_as_uint(score) | (residual ? 0x80000000u : 0u)) << 32 | (uint32_t)~v;
 }
+__device__ inline int draft_token(unsigned long long code) { return (code >> 32 & 0x7fffffffu) ? (int)~(uint32_t)code : -1; }
 
 // One workgroup per (part, sequence): each decides on the drafts, then races its part,
 // ROUNDS stretches of 2,048 at a time, all loads of a kind in flight.  Bound by its chain
@@ -368,8 +369,9 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
                 const int v = first + r * kDraftStretch + (int)threadIdx.x * 8 + k;
                 const float p = draft_prob(dp, draft_nan_low((float)x[r][k]), v, greedy, rate);
                 const float left = p - draft_prob(dq, draft_nan_low((float)y[r][k]), v, hot_q, rate);
-                const float score = (left > 0.0f ? left : p) * __builtin_amdgcn_rcpf(e[r][k]);
-                best = max(best, e[r][k] > 0.0f ? draft_code(score, v, left > 0.0f) : 0ull);
+                const float inverse = e[r][k] > 0.0f ? __builtin_amdgcn_rcpf(e[r][k]) : 0.0f;
+                const float score = fmaxf((left > 0.0f ? left : p) * inverse, 0.0f);  // (0 times infinity: 0)
+                best = max(best, draft_code(score, v, left > 0.0f));
             }
         if (first + ROUNDS * kDraftStretch < i1)
             draft_load<VEC, ROUNDS>(noise, first + ROUNDS * kDraftStretch, i1, e);
@@ -403,7 +405,7 @@ __global__ __launch_bounds__(kDraftBlock) void k_draft_race(DraftArgs a)
     if (!s_last || mine > a.G)
         return;
     best = s_best[0];
-    const int token = best ? (int)~(uint32_t)best : -1;
+    const int token = draft_token(best);
     const int64_t o = (int64_t)s * (a.G + 1) + mine;
     if (mine == 0)
         a.n_accepted[s] = j;

@@ -271,3 +271,30 @@ def test_no_sequences_and_refusals(sp):
         sp.head_draft_verify(**args, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError, match="no workspace"):
         sp.head_draft_verify(z(1, 33, 4), None, z(1, 32, t=i32), z(1, 32), z(1, 4), z(1, 33, t=i32), z(1, t=i32))
+
+
+@pytest.mark.parametrize("V", [50, 5000, 30000])
+@pytest.mark.parametrize("dist", [True, False])
+@pytest.mark.parametrize("bad", [0.0, -1.0, float("nan"), float("inf")])
+def test_residual_without_usable_noise(sp, V, dist, bad):
+    """r is max(p - q, 0) as soon as that is positive anywhere: where none of its tokens has noise that
+    can win, nothing else wins in their place.  Sequence 1 has one such token left, sequence 2's draft is
+    accepted (p itself is raced)."""
+    p = problem(3, 1, V, ragged=False, banned=0)
+    p["temperature"][:] = 1.0
+    p["uniform"][:] = [[1.0], [1.0], [0.0]]
+    few = np.arange(V) % 7 == 3  # with a distribution: p > q on these alone
+    for s in range(3):
+        p["draft"][s, 0] = p["target"][s, 0] + np.where(few & (np.arange(V) != p["drafts"][s, 0]), 0.0, 4.0)
+    q = [so.probabilities(p["draft"][s, 0].astype(np.float32), 1.0) if dist else (np.arange(V) == p["drafts"][s, 0]) * 1.0
+         for s in range(3)]
+    for s in range(3):
+        left = so.probabilities(p["target"][s, 0].astype(np.float32), 1.0) - q[s] > 0
+        assert left.any() and not left.all()
+        if s == 1:
+            left[np.argmax(left)] = False  # the lowest keeps its noise
+        p["noise"][s, left] = bad
+    got, want = run(sp, p, dist=dist)
+    assert want[0][0].tolist() == [-1, -1] and want[0][1, 0] >= 0 and want[1].tolist() == [0, 0, 1]
+    assert (got[0] == want[0]).all() and (got[1] == want[1]).all()
+    assert got[3][0, 0] == 0
