@@ -577,7 +577,8 @@ def dense_fused_backward(h: DenseFused, dy: torch.Tensor, dx: torch.Tensor | Non
     if dx is not None:
         xp, ldx = _rows(dx, "dx", B, h.K)
         x_type = _type_of(dx, "dx")
-    ws = _workspace(workspace, int(_lib.dense_fused_workspace_bytes(h.ptr, B, y_type)), dy.device, stream)
+    # (no size: the call refuses its arguments)
+    ws = _workspace(workspace, max(0, int(_lib.dense_fused_workspace_bytes(h.ptr, B, y_type))), dy.device, stream)
     _check(_lib.dense_fused_backward(h.ptr, gp, y_type, ldg, pp, ldp, act, B, xp, x_type, ldx,
                                      _vector(dbias, "dbias", h.M), _dev_ptr(ws, "workspace"),
                                      ws.numel() * ws.element_size(), _stream(stream)), "dense_fused_backward")

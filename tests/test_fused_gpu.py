@@ -543,3 +543,19 @@ def test_residual_in_place_of_every_form(sp, xk, yk, K, M, B):
     torch.cuda.synchronize()
     assert torch.isfinite(y.float()).all() and torch.equal(r, y)
     h.close()
+
+
+def test_refusals_of_the_gradient_name_their_cause(sp):
+    """A closed handle and too many rows have no workspace size: the call itself refuses them."""
+    h = handle(sp, problem(8, 1, 1), backward=True)
+    n = sp.FUSED_MAX_B + 1
+    with pytest.raises(sp.SpikeError, match="B = "):
+        sp.dense_fused_backward(h, torch.empty((n, 1), device="cuda"), dbias=torch.empty(1, device="cuda"))
+    with pytest.raises(sp.SpikeError, match="B = "):
+        sp.dense_fused_forward(h, torch.empty((n, 8), dtype=torch.bfloat16, device="cuda"), torch.empty((n, 1), device="cuda"))
+    h.close()
+    for B in (3, 40):
+        with pytest.raises(sp.SpikeError, match="null handle"):
+            sp.dense_fused_backward(h, torch.empty((B, 1), device="cuda"), dx=torch.empty((B, 8), device="cuda"))
+        with pytest.raises(sp.SpikeError, match="null handle"):
+            sp.dense_fused_forward(h, torch.empty((B, 8), device="cuda"), torch.empty((B, 1), device="cuda"))
