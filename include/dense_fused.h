@@ -95,9 +95,10 @@ int dense_fused_forward(dense_fused_t handle, const void *x, int32_t x_type, int
                         int32_t y_type, int64_t ld_y, void *pre, int64_t ld_pre, void *workspace,
                         int64_t workspace_bytes, void *stream);
 
-/* Workspace of dense_fused_forward for these rows: 0 (it may then be NULL)
- * for up to FUSED_FEW_ROWS rows, and for 16-bit ones that start on 16-byte boundaries with K a
- * multiple of 8; -1 for a null handle or a size or type it refuses. */
+/* Workspace of dense_fused_forward for these rows; where it is 0 the workspace may be NULL:
+ * always for up to FUSED_FEW_ROWS rows, and for 16-bit ones that start on 16-byte boundaries
+ * with K a multiple of 8 unless their sums are split over workgroups, which depends on the
+ * sizes.  -1 for a null handle or a size or type it refuses. */
 int64_t dense_fused_forward_workspace_bytes(dense_fused_t handle, const void *x, int32_t x_type, int64_t ld_x,
                                             int32_t B);
 

@@ -559,3 +559,19 @@ def test_refusals_of_the_gradient_name_their_cause(sp):
             sp.dense_fused_backward(h, torch.empty((B, 1), device="cuda"), dx=torch.empty((B, 8), device="cuda"))
         with pytest.raises(sp.SpikeError, match="null handle"):
             sp.dense_fused_forward(h, torch.empty((B, 8), device="cuda"), torch.empty((B, 1), device="cuda"))
+
+
+def test_forward_workspace_is_what_the_query_says(sp):
+    """Aligned 16-bit rows need none, except where the sums are split; FP32 rows and others need some."""
+    for K, M, B, xk, some in ((192, 1600, 1100, "bf16", False), (6000, 70, 40, "bf16", True), (192, 1600, 1100, "f32", True), (6000, 70, 32, "f32", False)):
+        h = handle(sp, problem(K, M, 1))
+        x, y = torch.zeros((B, K), dtype=TYPES[xk], device="cuda"), torch.empty((B, M), device="cuda")
+        n = sp.dense_fused_forward_workspace_bytes(h, x)
+        assert (n > 0) == some
+        sp.dense_fused_forward(h, x, y, workspace=torch.empty(max(n, 16), dtype=torch.uint8, device="cuda"))
+        if n > 0:
+            with pytest.raises(sp.SpikeError, match="workspace"):
+                sp.dense_fused_forward(h, x, y, workspace=torch.empty(n - 16, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        assert (y == 0).all()
+        h.close()
