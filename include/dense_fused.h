@@ -22,8 +22,9 @@
  * activations of up to FUSED_FEW_ROWS rows are cut into BF16 parts that
  * add up to them exactly (three, and two more below 2^-110); those of more rows are scaled, row by row, by a power
  * of two and rounded to two F16 parts, which keep an element to 2^-23 of itself
- * or 2^-40 of its row's largest finite one, whichever is more.  Each part is
- * multiplied on the matrix cores.  All sums are FP32, in an order that depends
+ * or 2^-39 of its row's largest finite one, whichever is more (a caller that
+ * needs every bit of rows with a wider range passes FUSED_FEW_ROWS at a time).
+ * Each part is multiplied on the matrix cores.  All sums are FP32, in an order that depends
  * on the sizes alone; equal calls give equal bits (a row's bits may depend on
  * B).  z stays FP32 up to y; outputs are rounded once.  In the backward pass
  * g * scale is FP32 and enters the product in two such F16 parts, or of up to

@@ -263,8 +263,10 @@ __device__ inline f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
 
 // Phi(-a) / exp(-a^2 / 2) for a >= 0 (half the scaled complementary error
 // function of a / sqrt 2): a polynomial in t = 1 / (1 + 0.28 a), fitted to
-// relative error 1.7e-7 over all a (least squares with weights raised where
-// the error was largest, in double precision).
+// relative error 1.8e-7 over all a (least squares with weights raised where
+// the error was largest, in double precision).  What it is multiplied with,
+// exp2 of an argument rounded to FP32, adds about a^2 2^-24: the GELU of -3 to -6 is
+// off by 2e-6 of itself, of -12 by 8e-6 (2e-9 and 2e-37), and below -13.2 it is 0.
 __device__ inline float gauss_tail(float a)
 {
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.28f, a, 1.0f));
@@ -972,7 +974,8 @@ __global__ __launch_bounds__(256) void k_fused_align(const uint16_t* __restrict_
 // Cuts FP32 rows of n elements into two scaled F16 planes for the product.  Two
 // roundings to 11 bits keep an element to 2^-23 of itself (one bit less than FP32
 // holds; the sums' own rounding, 2^-24 of a partial sum per step, is larger) down to
-// 2^-17 of the row's largest, and smaller ones to 2^-40 of that.  Three BF16 planes
+// 2^-17 of the row's largest, and smaller ones to 2^-39 of that (F16's smallest step is
+// 2^-24, the largest is scaled to 2^14 or more).  Three BF16 planes
 // would keep every bit at any range, for half as much again in the product
 // (1536 -> 6144, 2500 rows: 126 us, against 98; 500 rows 40 and 30).  The planes' rows
 // have `ld` (n rounded up to 8) elements, zeros past n.  A workgroup walks a row, whose
