@@ -274,15 +274,19 @@ int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 // What g * scale is kept in between the gate and the product: two scaled F16 planes and what
 // undoes the scaling, apart or side by side in a row; or FP32 rows where the product takes few
 // of them, which it cuts itself.  Side by side (a row's planes are whole steps), a tile of one
-// plane walks them one after the other; apart, a tile of two takes them together.  BF16 rows, us,
-// side by side and apart: 6144 -> 1536 inputs, 8192 rows 350 and 329, 64 rows 24.3 and 23.2;
-// 1536 -> 1536, 1000 rows 31 and 33; 1536 -> 6144, 16,384 rows 533 and 543, 500 rows 48 and 33.
+// plane walks them one after the other; apart, a tile of two takes them together, which is
+// faster where sums are long, outputs many and rows fill the tiles.  BF16, us, side by side and
+// apart, M summed over -> K: 6144 -> 1536, 64 rows 23.5 and 23.0, 2500 rows 164 and 126, 8192 rows 357
+// and 334; 1536 -> 6144, 500 rows 46 and 31, 16,384 rows 549 and 560; 1280 -> 1536, 2500 rows 49
+// and 38.  Otherwise: 6000 -> 72, 500 rows 25 and 28; 6000 -> 520, 2500 rows 85 and 93; 72 -> 4104,
+// 500 rows 11 and 13; 456 -> 256, 8192 rows 26 and 31; but 1000 -> 1536, 2500 rows 40 and 32.
 enum GateForm { kGateRows, kGateApart, kGateBeside };
 
-GateForm gate_form(int y_type, int32_t B)
+GateForm gate_form(const dense_fused* h, int y_type, int32_t B)
 {
-    return y_type == SPIKE_TYPE_BF16 ? (B <= kFewRows ? kGateRows : kGateBeside)
-                                     : B <= kFewRows ? kGateRows : kGateApart;
+    if (B <= kFewRows)
+        return kGateRows;
+    return y_type != SPIKE_TYPE_BF16 || (h->M >= 1280 && h->K >= 1024 && B >= 64) ? kGateApart : kGateBeside;
 }
 int gate_width(GateForm form, int32_t M) { return (int)spk::fused_pad(M, form == kGateBeside ? spk::kFusedStep : 8); }
 int64_t gate_plane_bytes(GateForm form, int32_t B, int32_t M)
@@ -451,7 +455,7 @@ int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
 {
     if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(y_type))
         return -1;
-    const GateForm form = gate_form(y_type, B);
+    const GateForm form = gate_form(h, y_type, B);
     const int64_t sums = form == kGateRows ? 0
                                            : split_bytes(tile_plan(gate_planes(form), B, h->K,
                                                                    (h->M + spk::kFusedStep - 1) / spk::kFusedStep),
@@ -491,7 +495,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return rc;
     if (act == DENSE_ACT_NONE)
         pre = nullptr;
-    const GateForm form = gate_form(y_type, B);
+    const GateForm form = gate_form(h, y_type, B);
     const int width = gate_width(form, h->M);
     int parts = 0;
     float* partial = nullptr;

@@ -17,7 +17,8 @@ import pytest
 import torch
 
 from oracle import step_oracle as so
-from tests.test_fused_gpu import TYPES, act_code, dev, handle, host
+from tests.launches import launches
+from tests.test_fused_gpu import TYPES, act_code, dev, handle, host, problem
 
 pytestmark = pytest.mark.gpu
 
@@ -111,4 +112,34 @@ def test_wide_gradients(sp, B):
     lim = limit(want, host(dy) * p["scale"], columns(p["Q"]), B, 1) + 2.0 ** -149 * 127
     got = host(dx)
     assert (np.abs(got - want) <= lim).all(), np.nanmax(np.abs(got - want) / lim)
+    h.close()
+
+
+@pytest.mark.parametrize("B", [33, 63, 64, 200, 700])
+@pytest.mark.parametrize("K,M,pad,offset", [(1024, 1280, 0, 0), (1100, 1300, 3, 1), (1023, 1280, 0, 0), (1024, 1279, 0, 0), (2100, 8300, 0, 0)])
+@pytest.mark.parametrize("xk", ["f32", "bf16"])
+def test_bf16_gradient_in_both_forms(sp, B, K, M, pad, offset, xk):
+    """Planes apart and side by side, at the sizes where one follows the other: integers exactly, each operand's bits."""
+    r = np.random.default_rng([44, B, K, M])
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p, backward=True)
+    dy, dx = dev(p["dy"], "bf16", pad, offset), dev(np.full((B, K), np.nan), xk, pad, offset)
+    db = torch.full((M,), float("nan"), device="cuda")
+    ws = torch.full((sp.dense_fused_workspace_bytes(h, B, torch.bfloat16),), 255, dtype=torch.uint8, device="cuda")  # (NaN)
+    names = [n for n, _, _ in launches(lambda st: sp.dense_fused_backward(h, dy, dx=dx, dbias=db, workspace=ws, stream=st))]
+    planes = 2 if M >= 1280 and K >= 1024 and B >= 64 else 1
+    assert any(f"k_fused_tileIDF16_Li{planes}E" in n for n in names), names
+    sp.dense_fused_backward(h, dy, dx=dx, dbias=db, workspace=ws)
+    torch.cuda.synchronize()
+    want, wb, _ = so.fused_backward(p["Q"], p["scale"], host(dy))
+    assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[xk])) and (db.cpu().numpy() == wb).all()
+    h.close()
+    p = {"Q": columns(one_code(r, K, M)), "scale": r.uniform(0.5, 1.5, M).astype(np.float32)}
+    h = handle(sp, p, backward=True)
+    dy, dx = dev(r.normal(size=(B, M)), "bf16", pad, offset), torch.full((B, K), float("nan"), device="cuda")
+    sp.dense_fused_backward(h, dy, dx=dx)
+    torch.cuda.synchronize()
+    want, _, g = so.fused_backward(p["Q"], np.ones(M), host(dy) * p["scale"].astype(np.float64))
+    lim = limit(want, g, columns(p["Q"]), B, 1)
+    assert (np.abs(host(dx) - want) <= lim).all()
     h.close()
