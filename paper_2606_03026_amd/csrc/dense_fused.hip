@@ -120,9 +120,10 @@ struct TilePlan {
 // The shape, and the workgroups that share a tile's steps, with the least estimated
 // time: the steps of the tiles that come to one compute unit, and for a split the join
 // (a launch, and the FP32 sums written and read at 3.9 MB/us).  What that decides
-// between, BF16, in us: 1536 -> 1536, 64 rows: 7.1 in tiles of 64 x 32 by four teams, 8.2 by one,
-// 26 in 256 x 128; 1536 -> 6144, 2500 rows: 94 in 64 x 32, 48 in 256 x 128; 6144 -> 1536, 33
-// rows: 14.2 in one part, 13.1 in four; with 1024 rows 30.7 by two teams, 43 in four parts.
+// between, BF16 without an activation, in us: 1536 -> 1536, 64 rows: 6.8 in tiles of 64 x 32 by
+// four teams, 9.6 in 64 x 64, 25 in 256 x 128; 1536 -> 6144, 2500 rows: 112 in 64 x 32, 46 in
+// 256 x 128; 6144 -> 1536, 33 rows: 14.6 in one part, 11.6 in four; with 1024 rows 30 by two teams,
+// 42 in four parts.
 TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
 {
     const TileShape* shapes = ns == 1 ? kShapes1 : kShapes2;
@@ -201,9 +202,9 @@ void launch_rows(const FusedArgs& a, hipStream_t st)
 
 // Few rows.  Tiles of outputs that a workgroup takes together share what it does
 // to the activations (the cutting of FP32 ones costs more than a tile's weights),
-// and the 17th to 32nd row share the weights: FP32, 1536 -> 6144, one row 5.9 us
-// one by one and 5.1 by twos; 1536 -> 57,344 41 and 17.4 by fours, 16 rows 55 and
-// 18.2.  Fewer outputs than that leave compute units idle.
+// and the 17th to 32nd row share the weights: FP32, 1536 -> 6144, one row 6.4 us
+// one by one and 5.0 by twos; 1536 -> 57,344 29 and 19 by fours, 16 rows 46 and
+// 20.  Fewer outputs than that leave compute units idle.
 template <typename XT, int NS, bool VECX>
 void launch_few(const FusedArgs& a, hipStream_t st)
 {

@@ -356,7 +356,7 @@ __global__ __launch_bounds__(kEmbedBlock) void k_embed_sum(const TG* __restrict_
 // Joins the partial sums of the rows that several runs share: the wave of the
 // run in which such a row begins adds the following runs' sums to its own.
 // Workgroups from join_wgs on zero rows that no token names.  Bound by the reads that
-// depend on each other (16,384 tokens, with 32 MB written: 10 us).
+// depend on each other (16,384 tokens, with 32 MB written: 8.8 us).
 template <typename TD, int VEC>
 __global__ __launch_bounds__(kEmbedBlock) void k_embed_join(const uint32_t* __restrict__ keys, int T, int D,
                                                             float scale, int accumulate, TD* __restrict__ dtable,

@@ -475,9 +475,9 @@ struct OutputColumns {
 
 // Up to 16 NB rows: a workgroup takes 16 MT outputs and all inputs, its WK
 // waves sharing the 64-input steps; the waves' sums are joined in LDS.  Bound
-// by the weights' bytes (1536 -> 57,344, one FP32 row: 19.6 us, 4.5 TB/s; BF16 16.8, 5.2),
-// where these are few by latency (1536 -> 6144, one FP32 row: 5.1 us; 1536 -> 1536, 7 BF16
-// rows: 3.3).  Asking whether three parts left anything costs 0 to 8% of an FP32 call (6144 ->
+// by the weights' bytes (1536 -> 57,344, one FP32 row: 18.8 us, 4.7 TB/s; BF16 16.8, 5.2),
+// where these are few by latency (1536 -> 6144, one FP32 row: 5.0 us; 1536 -> 1536, 7 BF16
+// rows: 3.0).  Asking whether three parts left anything costs 0 to 8% of an FP32 call (6144 ->
 // 1536, 7 rows: 10.2 us without, 11.3).
 // Rows that are not there cost no loads, only idle columns of the matrix instruction.
 template <typename XT, int NS, int NB, int MT, int WK, bool VECX>
@@ -658,10 +658,10 @@ constexpr int fused_tile_lds()
 // adds up their sums: where there are fewer tiles than compute units, one group leaves
 // most of its unit's issue slots empty.
 // Bound by how densely the waves issue products between their waits: 16,384 BF16 rows
-// of 1536 -> 6144 with GELU and the values before it 318 us, 972 TFLOP/s (the product
-// alone 279 us, 1108 TFLOP/s); 2500 FP32 rows, two planes, 91 us and 1034 TFLOP/s, the
-// matrix units busy 44% of the time, LDS 4%; 8192 rows of 6144 -> 1536, two planes one after
-// the other, 263 us and 1176 TFLOP/s.
+// of 1536 -> 6144 with GELU and the values before it 319 us, 970 TFLOP/s (the product
+// alone 264 us, 1174 TFLOP/s); 2500 FP32 rows, two planes, 91 us and 1034 TFLOP/s, the
+// matrix units busy 45% of the time, LDS 4%; 8192 rows of 6144 -> 1536, two planes, 243 us
+// and 1272 TFLOP/s, 59%.
 // Codes widened by byte moves and packed F16 sums instead of conversions: no change.
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
 __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
