@@ -1,6 +1,6 @@
 /*
- * dense_fused.h -- C ABI of the INT8 projection with bias, activation and
- * residual in its epilogue, and of its gradient.
+ * dense_fused.h -- C ABI of the projection with INT8 or four-bit weights, with
+ * bias, activation and residual in its epilogue, and of its gradient.
  *
  * Operation (paper Sec. 2.3, end of "Quantization and Accumulation": the
  * continuous-input projections, here with what a decoder block does to their
@@ -31,7 +31,19 @@
  * FUSED_FEW_ROWS rows in these BF16 parts.  dbias is summed in FP32 from the
  * unrounded g.
  *
+ * Four-bit weights (dense_fused_create_mx4; quantize.h states what codes and scales stand for) take the
+ * place of scale[m] Q[m][k] in all of this; the same calls take the handle.  Its weights enter the product
+ * as BF16 or F16 operands, each relative to a power of two that brings its output's largest block to
+ * 2^13: exactly where that keeps them above 2^-127 (BF16 x, and FP32 x of up to FUSED_FEW_ROWS rows) or
+ * 2^-24 (F16 x, and more rows of FP32 x: a weight is held to 2^-37 of its output's largest), and in the gradient to 2^-29
+ * of its output's largest.  dense_fused_forward_mx4 takes rows of four-bit codes too, on matrix instructions
+ * that scale the blocks; products are exact, sums FP32.  A block whose scale is 255 is NaN, and so is
+ * every output whose sum has it.  Sums are of x times weights of size up to 2^16, so x above 2^100 may overflow them where z would not.
+ *
  * Data layout (DEVICE pointers):
+ *   codes, scales   of weights [M][K] or rows [B][K], as spike_quantize_mx4 writes them: rows of ceil(K / 2) and
+ *             ceil(K / 32) bytes, ld_codes and ld_scales bytes apart, at any alignment; what lies behind
+ *             element K is not read as part of it.
  *   Q         int8 [M][K] row-major, scale float [M] (as in dense_proj.h); read
  *             by create only, which lays them out for the matrix cores.
  *   x, dx     [B] rows of K elements, ld_x / ld_dx elements apart.
@@ -48,7 +60,7 @@
  * below 2^31; 0 <= B <= FUSED_MAX_B.
  *
  * A handle owns its copies of the weights (1 byte each, twice that with
- * DENSE_FUSED_BACKWARD); calls on it only read them, so it may be used on
+ * DENSE_FUSED_BACKWARD; four-bit ones 17/32 of a byte and one more); calls on it only read them, so it may be used on
  * several streams at once.  forward and backward enqueue kernels on `stream`
  * (a hipStream_t, NULL for the default stream), allocate nothing, do not
  * synchronise and can be captured in a HIP graph.  The workspaces (their sizes
@@ -88,6 +100,10 @@ typedef struct dense_fused *dense_fused_t;
 int dense_fused_create(const int8_t *Q, const float *scale, int32_t K, int32_t M, int32_t flags,
                        dense_fused_t *out_handle);
 
+/* The same of four-bit weights [M][K]. */
+int dense_fused_create_mx4(const uint8_t *codes, int64_t ld_codes, const uint8_t *scales, int64_t ld_scales, int32_t K,
+                           int32_t M, int32_t flags, dense_fused_t *out_handle);
+
 /* Waits for the device and frees the handle (NULL: nothing). */
 int dense_fused_destroy(dense_fused_t handle);
 
@@ -102,6 +118,18 @@ int dense_fused_forward(dense_fused_t handle, const void *x, int32_t x_type, int
  * sizes.  -1 for a null handle or a size or type it refuses. */
 int64_t dense_fused_forward_workspace_bytes(dense_fused_t handle, const void *x, int32_t x_type, int64_t ld_x,
                                             int32_t B);
+
+/* dense_fused_forward of B rows of four-bit codes; the handle's weights are four-bit ones. */
+int dense_fused_forward_mx4(dense_fused_t handle, const uint8_t *codes, int64_t ld_codes, const uint8_t *scales,
+                            int64_t ld_scales, int32_t B, const float *bias, int32_t act, const void *residual,
+                            int64_t ld_residual, void *y, int32_t y_type, int64_t ld_y, void *pre, int64_t ld_pre,
+                            void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Its workspace for these rows, which may be NULL where it is 0: for up to FUSED_FEW_ROWS rows, and
+ * for rows of a multiple of 128 elements whose codes start on 16-byte and scales on 4-byte boundaries unless
+ * their sums are split over workgroups.  -1 for a null handle, one of INT8 weights or a size it refuses. */
+int64_t dense_fused_forward_mx4_workspace_bytes(dense_fused_t handle, const uint8_t *codes, int64_t ld_codes,
+                                                const uint8_t *scales, int64_t ld_scales, int32_t B);
 
 /* Workspace of dense_fused_backward for B rows; -1 for a null handle or a size or type it refuses. */
 int64_t dense_fused_workspace_bytes(dense_fused_t handle, int32_t B, int32_t y_type);

@@ -1,6 +1,7 @@
 """ctypes binding of libspike_proj.so (C ABI in include/spike_proj.h,
 include/dense_proj.h, include/quantize.h, include/head_verify.h,
-include/dense_fused.h, include/spike_embed.h and include/head_draft.h).
+include/dense_fused.h, include/spike_embed.h, include/head_draft.h,
+include/head_logits.h and include/spike_clip.h).
 
 Argument marshalling only: every step of the projection runs in the HIP
 kernels of the library.  Tensors are torch device tensors; their data
@@ -34,6 +35,9 @@ DENSE_FUSED_BACKWARD = 1
 FUSED_MAX_DIM, FUSED_MAX_B, FUSED_FEW_ROWS = 1 << 20, 1 << 22, 32
 EMBED_MAX_V, EMBED_MAX_D, EMBED_MAX_T = 1 << 28, 65536, 1 << 22
 DRAFT_MAX_S, DRAFT_MAX_G, DRAFT_MAX_V = 4096, 31, 1 << 30
+SPIKE_MX4_BLOCK = 32
+LOGITS_MAX_S, LOGITS_MAX_N, LOGITS_MAX_V, LOGITS_MAX_L, LOGITS_MAX_BIAS = 4096, 32, 1 << 30, 1 << 22, 1 << 16
+CLIP_MAX_TENSORS = 1 << 20
 
 
 def SPIKE_SHAPE(V: int, LG: int, U: int, BLOCK: int, NT: bool = False, I16: bool = False) -> int:
@@ -52,6 +56,8 @@ EXPORTED = (
     "dense_fused_create", "dense_fused_destroy", "dense_fused_forward", "dense_fused_workspace_bytes",
     "dense_fused_forward_workspace_bytes", "dense_fused_backward", "spike_embed_forward", "spike_embed_workspace_bytes", "spike_embed_backward",
     "head_draft_workspace_bytes", "head_draft_verify",
+    "spike_quantize_mx4", "dense_fused_create_mx4", "dense_fused_forward_mx4", "dense_fused_forward_mx4_workspace_bytes",
+    "head_logits_adjust", "spike_clip_create", "spike_clip_destroy", "spike_clip_workspace_bytes", "spike_clip_forward",
 )
 
 if not os.path.exists(LIB):
@@ -95,6 +101,16 @@ _sig = {
     "spike_embed_forward": [_p, _i32, _p, _i32, _i32, _i64, _p, _i32, _i32, _f32, _p, _i32, _i64, _p],
     "spike_embed_workspace_bytes": [_i32, _i32],
     "spike_embed_backward": [_p, _i32, _i64, _p, _i32, _i32, _i32, _i32, _f32, _i32, _p, _i32, _i64, _p, _i64, _p],
+    "spike_quantize_mx4": [_p, _i32, _i64, _i32, _i32, _p, _i64, _p, _i64, _p, _i64, _p],
+    "dense_fused_create_mx4": [_p, _i64, _p, _i64, _i32, _i32, _i32, ctypes.POINTER(_p)],
+    "dense_fused_forward_mx4": [_p, _p, _i64, _p, _i64, _i32, _p, _i32, _p, _i64, _p, _i32, _i64, _p, _i64, _p, _i64, _p],
+    "dense_fused_forward_mx4_workspace_bytes": [_p, _p, _i64, _p, _i64, _i32],
+    "head_logits_adjust": [_p, _i64, _i32, _i32, _i32, _i32, _p, _i64, _i32, _p, _p, _p, _p, _p, _p, _p, _p, _i32, _p, _i64, _p,
+                           _i64, _p],
+    "spike_clip_create": [_p, _p, _p, _p, _i32, ctypes.POINTER(_p)],
+    "spike_clip_destroy": [_p],
+    "spike_clip_workspace_bytes": [_p],
+    "spike_clip_forward": [_p, _f32, _p, _p, _i64, _p],
     "head_draft_workspace_bytes": [_i32, _i32, _i32],
     "head_draft_verify": [_p, _i64, _p, _i64, _i32, _p, _p, _p, _p, _i64, _p, _i32, _i32, _i32, _p, _p, _p, _p, _p, _i64, _p],
 }
@@ -104,7 +120,8 @@ for _name, _args in _sig.items():
 _lib.spike_proj_last_error.argtypes = []
 _lib.spike_proj_last_error.restype = ctypes.c_char_p
 for _name in ("head_verify_workspace_bytes", "dense_fused_forward_workspace_bytes", "dense_fused_workspace_bytes",
-              "spike_embed_workspace_bytes", "head_draft_workspace_bytes"):
+              "spike_embed_workspace_bytes", "head_draft_workspace_bytes", "dense_fused_forward_mx4_workspace_bytes",
+              "spike_clip_workspace_bytes"):
     getattr(_lib, _name).restype = ctypes.c_int64
 
 
@@ -441,6 +458,30 @@ def spike_quantize_int8(W: torch.Tensor, layout: int, Q: torch.Tensor, scale: to
                                     _dev_ptr(scale, "scale", M * 4), _stream(stream)), "spike_quantize_int8")
 
 
+def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, values: torch.Tensor | None = None,
+                       stream=None) -> None:
+    """Microscaled four-bit codes of x [M, K] (quantize.h): codes uint8 [M, ceil(K / 2)], two to a byte; scales uint8
+    [M, ceil(K / 32)], exponents of the blocks' powers of two; values: what they stand for, [M, K] of x's type, or None."""
+    M, K = x.shape
+    xp, ldx = _rows(x, "x", M, K)
+    cp, ldc, sp_, lds = _coded_rows(codes, scales, "", M, K)
+    vp, ldv = None, 0
+    if values is not None:
+        vp, ldv = _rows(values, "values", M, K)
+        if values.dtype != x.dtype:
+            raise TypeError("values must have x's type")
+    _check(_lib.spike_quantize_mx4(xp, _type_of(x, "x"), ldx, M, K, cp, ldc, sp_, lds, vp, ldv, _stream(stream)),
+           "spike_quantize_mx4")
+
+
+def _coded_rows(codes: torch.Tensor, scales: torch.Tensor, of: str, rows: int, K: int):
+    """(address, stride) of the codes and of the scales of `rows` rows of K four-bit elements."""
+    if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
+        raise TypeError(f"{of}codes and {of}scales must be uint8")
+    return (*_rows(codes, f"{of}codes", rows, (K + 1) // 2),
+            *_rows(scales, f"{of}scales", rows, (K + SPIKE_MX4_BLOCK - 1) // SPIKE_MX4_BLOCK))
+
+
 def spike_check_scale_shape(M: int, K: int, group: int, scale_rows: int, scale_cols: int) -> None:
     _check(_lib.spike_check_scale_shape(int(M), int(K), int(group), int(scale_rows), int(scale_cols)),
            "spike_check_scale_shape")
@@ -515,6 +556,16 @@ def dense_fused_create(Q: torch.Tensor, scale: torch.Tensor, backward: bool = Fa
     return DenseFused(out.value, int(K), int(M))
 
 
+def dense_fused_create_mx4(codes: torch.Tensor, scales: torch.Tensor, K: int, backward: bool = False) -> DenseFused:
+    """A handle of four-bit weights [M, K], as spike_quantize_mx4 gives them (dense_fused.h); both tensors may be freed
+    afterwards.  Every call that takes a handle takes it."""
+    M, K = codes.shape[0], int(K)
+    out = _p()
+    _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, "", M, K), K, M, DENSE_FUSED_BACKWARD if backward else 0,
+                                       ctypes.byref(out)), "dense_fused_create_mx4")
+    return DenseFused(out.value, K, int(M))
+
+
 def dense_fused_destroy(h: DenseFused) -> None:
     h.close()
 
@@ -550,6 +601,39 @@ def dense_fused_forward_workspace_bytes(h: DenseFused, x: torch.Tensor) -> int:
     """Workspace of dense_fused_forward for these activations [B, K]."""
     xp, ldx = _rows(x, "x", x.shape[0], h.K)
     return int(_lib.dense_fused_forward_workspace_bytes(h.ptr, xp, _type_of(x, "x"), ldx, x.shape[0]))
+
+
+def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Tensor, y: torch.Tensor,
+                            bias: torch.Tensor | None = None, act: int = DENSE_ACT_NONE,
+                            residual: torch.Tensor | None = None, pre: torch.Tensor | None = None,
+                            workspace: torch.Tensor | None = None, stream=None) -> None:
+    """dense_fused_forward of four-bit rows (codes, scales as spike_quantize_mx4 gives them for [B, K]) with a handle of
+    four-bit weights (dense_fused.h)."""
+    B = codes.shape[0]
+    rows = _coded_rows(codes, scales, "", B, h.K)
+    yp, ldy = _rows(y, "y", B, h.M)
+    rp = pp = None
+    ldr = ldp = 0
+    if residual is not None:
+        rp, ldr = _rows(residual, "residual", B, h.M)
+    if pre is not None:
+        pp, ldp = _rows(pre, "pre", B, h.M)
+    if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
+        raise TypeError("residual and pre must have y's type")
+    wp, n_ws = None, 0
+    if B > FUSED_FEW_ROWS:
+        n_ws = _lib.dense_fused_forward_mx4_workspace_bytes(h.ptr, *rows, B)
+    if n_ws > 0:
+        workspace = _workspace(workspace, n_ws, codes.device, stream)
+        wp, n_ws = _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
+    _check(_lib.dense_fused_forward_mx4(h.ptr, *rows, B, _vector(bias, "bias", h.M), act, rp, ldr, yp, _type_of(y, "y"), ldy,
+                                        pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward_mx4")
+
+
+def dense_fused_forward_mx4_workspace_bytes(h: DenseFused, codes: torch.Tensor, scales: torch.Tensor) -> int:
+    """Workspace of dense_fused_forward_mx4 for these rows."""
+    B = codes.shape[0]
+    return int(_lib.dense_fused_forward_mx4_workspace_bytes(h.ptr, *_coded_rows(codes, scales, "", B, h.K), B))
 
 
 def dense_fused_workspace_bytes(h: DenseFused, B: int, dtype: torch.dtype) -> int:
@@ -674,6 +758,102 @@ def head_draft_verify(target: torch.Tensor, draft: torch.Tensor | None, drafts: 
                                   _vector(n_accepted, "n_accepted", S, i32), _vector(accept, "accept", S * G),
                                   _vector(prob, "prob", S * G1), _dev_ptr(ws, "workspace"),
                                   ws.numel() * ws.element_size(), _stream(stream)), "head_draft_verify")
+
+
+def head_logits_adjust(logits: torch.Tensor, out: torch.Tensor, ids: torch.Tensor | None = None,
+                       n_ids: torch.Tensor | None = None, n_prompt: torch.Tensor | None = None,
+                       drafts: torch.Tensor | None = None, repetition: torch.Tensor | None = None,
+                       presence: torch.Tensor | None = None, frequency: torch.Tensor | None = None,
+                       bias_ids: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                       mask: torch.Tensor | None = None, stream=None) -> None:
+    """Penalties, biases and a mask on logits [S, n, V] (head_logits.h); out: the same shape and type, or logits itself.
+    ids: int32 [S, L]; n_ids, n_prompt: int32 [S]; drafts: int32 [S, n - 1]; repetition, presence, frequency: float32 [S];
+    bias_ids int32, bias float32 [S, n_bias]; mask: int32 [S, n, ceil(V / 32)], a bit a token, set where it is allowed."""
+    S, n, V = logits.shape
+    xp, ldx = _logit_rows(logits, "logits", S, n, V)
+    op, ldo = _logit_rows(out, "out", S, n, V)
+    if out.dtype != logits.dtype:
+        raise TypeError("out must have logits' type")
+    i32 = torch.int32
+    ip, ldi, L = None, 0, 0
+    if ids is not None:
+        if ids.dtype != i32 or ids.dim() != 2:
+            raise TypeError("ids must be int32 [S, L]")
+        L = ids.shape[1]
+        ip, ldi = _rows(ids, "ids", S, L)
+    bp, n_bias = None, 0
+    if bias_ids is not None or bias is not None:
+        if bias_ids is None or bias is None or bias_ids.dim() != 2:
+            raise TypeError("bias_ids and bias must both be given, as [S, n_bias]")
+        n_bias = bias_ids.shape[1]
+        bp = _vector(bias_ids, "bias_ids", S * n_bias, i32)
+    mp, ldm = None, 0
+    if mask is not None:
+        if mask.dtype != i32:
+            raise TypeError("mask must be int32 [S, n, ceil(V / 32)]")
+        mp, ldm = _logit_rows(mask, "mask", S, n, (V + 31) // 32)
+    _check(_lib.head_logits_adjust(xp, ldx, _type_of(logits, "logits"), S, n, V, ip, ldi, L, _vector(n_ids, "n_ids", S, i32),
+                                   _vector(n_prompt, "n_prompt", S, i32), _vector(drafts, "drafts", S * (n - 1), i32),
+                                   _vector(repetition, "repetition", S), _vector(presence, "presence", S),
+                                   _vector(frequency, "frequency", S), bp, _vector(bias, "bias", S * n_bias), n_bias, mp, ldm,
+                                   op, ldo, _stream(stream)), "head_logits_adjust")
+
+
+class SpikeClip:
+    """Handle returned by spike_clip_create.  Holds the gradients and outputs, so that they outlive it."""
+
+    def __init__(self, ptr: int, tensors, device):
+        self.ptr, self.tensors, self.device = ptr, tensors, device
+
+    def close(self):
+        if self.ptr:
+            _check(_lib.spike_clip_destroy(self.ptr), "spike_clip_destroy")
+            self.ptr = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def spike_clip_create(grads, outs=None) -> SpikeClip:
+    """A handle for the common norm and the clipping of a list of contiguous gradients (spike_clip.h); outs: where the
+    clipped ones go, of the same sizes and types, an entry None (or no list) for in place."""
+    grads = list(grads)
+    n = len(grads)
+    outs = [None] * n if outs is None else list(outs)
+    if len(outs) != n:
+        raise ValueError(f"{len(outs)} outputs for {n} gradients")
+    in_ptrs, out_ptrs, types, sizes = (_p * n)(), (_p * n)(), (_i32 * n)(), (_i64 * n)()
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        in_ptrs[i] = _dev_ptr(g, f"gradient {i}")
+        types[i], sizes[i] = _type_of(g, f"gradient {i}"), g.numel()
+        if o is not None:
+            if o.dtype != g.dtype or o.numel() != g.numel():
+                raise TypeError(f"output {i} must have its gradient's type and size")
+            out_ptrs[i] = _dev_ptr(o, f"output {i}")
+    out = _p()
+    _check(_lib.spike_clip_create(in_ptrs, out_ptrs, types, sizes, n, ctypes.byref(out)), "spike_clip_create")
+    return SpikeClip(out.value, (grads, outs), grads[0].device if n else torch.device("cuda", torch.cuda.current_device()))
+
+
+def spike_clip_destroy(h: SpikeClip) -> None:
+    h.close()
+
+
+def spike_clip_workspace_bytes(h: SpikeClip) -> int:
+    """Workspace of spike_clip_forward."""
+    return int(_lib.spike_clip_workspace_bytes(h.ptr))
+
+
+def spike_clip_forward(h: SpikeClip, max_norm: float, result: torch.Tensor, workspace: torch.Tensor | None = None,
+                       stream=None) -> None:
+    """Scale the handle's gradients by min(1, max_norm / norm) into its outputs (spike_clip.h); result: float32 [2], the
+    norm and the factor."""
+    ws = _workspace(workspace, max(16, int(_lib.spike_clip_workspace_bytes(h.ptr))), h.device, stream)
+    _check(_lib.spike_clip_forward(h.ptr, max_norm, _vector(result, "result", 2), _dev_ptr(ws, "workspace"),
+                                   ws.numel() * ws.element_size(), _stream(stream)), "spike_clip_forward")
 
 
 def spike_proj_abi_version() -> int:

@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libspike_proj.so")
 SOURCES = [os.path.join(HERE, "csrc", f) for f in (
     "spike_proj.hip", "dense_proj.hip", "quantize.hip", "head_verify.hip",
-    "dense_fused.hip", "spike_embed.hip", "head_draft.hip")]
+    "dense_fused.hip", "spike_embed.hip", "head_draft.hip", "head_logits.hip", "spike_clip.hip")]
 DEPS = sorted(glob.glob(os.path.join(HERE, "csrc", "*"))) + sorted(glob.glob(os.path.join(ROOT, "include", "*.h")))
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,4 +1,4 @@
-// Host side of the fused INT8 projection and its gradient (C ABI in
+// Host side of the fused INT8 or four-bit projection and its gradient (C ABI in
 // include/dense_fused.h): handles, validation, choice of the kernel, launches.
 #include "dense_fused.h"
 
@@ -10,11 +10,14 @@
 
 #include "errors.hpp"
 #include "fused.hpp"
+#include "fused_mx4.hpp"
 
 struct dense_fused {
     int32_t K = 0, M = 0;
     int device = 0;
+    spk::WeightKind kind = spk::kInt8;
     int8_t* P = nullptr;     // rows of Q as outputs; the one allocation, which holds the others too
+    int8_t* S = nullptr;     // exponents of four-bit weights
     int8_t* Pt = nullptr;    // columns of Q as outputs (DENSE_FUSED_BACKWARD)
     float* scale = nullptr;  // [M rounded up to 16], zeros past M
 };
@@ -67,6 +70,32 @@ hipError_t lay_out(const int8_t* Q, const float* scale, bool backward, dense_fus
     return hipDeviceSynchronize();
 }
 
+hipError_t lay_out_mx4(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, bool backward, dense_fused* h)
+{
+    const int64_t bytes = spk::mx4_packed_bytes(h->M, h->K), bytes_s = spk::mx4_scale_bytes(h->M, h->K);
+    const int64_t bytes_t = backward ? spk::fused_packed_bytes(h->K, h->M) : 0;
+    const int padded = (int)spk::fused_pad(h->M, spk::kFusedTile);
+    hipError_t e = hipMalloc(&h->P, (size_t)(bytes + bytes_s + bytes_t + padded * (int64_t)(sizeof(float) + 1)));
+    if (e == hipSuccess)
+        e = hipDeviceSynchronize();  // the codes may still be in flight on any stream
+    if (e != hipSuccess)
+        return e;
+    h->S = h->P + bytes;
+    h->Pt = backward ? h->S + bytes_s : nullptr;
+    h->scale = reinterpret_cast<float*>(h->S + bytes_s + bytes_t);
+    uint8_t* const top = reinterpret_cast<uint8_t*>(h->scale + padded);
+    hipLaunchKernelGGL(spk::k_mx4_top, dim3((unsigned)((padded + 3) / 4)), dim3(256), 0, nullptr, codes, ld_codes, scales, ld_scales,
+                       h->K, h->M, padded, top, h->scale);
+    hipLaunchKernelGGL(spk::k_mx4_pack, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, nullptr, codes, ld_codes, scales,
+                       ld_scales, h->K, h->M, top, reinterpret_cast<uint8_t*>(h->P), reinterpret_cast<uint8_t*>(h->S), bytes / 16);
+    if (backward)
+        hipLaunchKernelGGL(spk::k_mx4_pack_columns, dim3((unsigned)((bytes_t / 16 + 255) / 256)), dim3(256), 0, nullptr, codes,
+                           ld_codes, scales, ld_scales, h->K, h->M, top, h->Pt, bytes_t / 16);
+    if ((e = hipGetLastError()) != hipSuccess)
+        return e;
+    return hipDeviceSynchronize();
+}
+
 int check_device(int want)
 {
     int dev = -1;
@@ -82,16 +111,16 @@ constexpr int kCUs = 256;
 // Up to here a call reads the activations straight from memory.
 constexpr int kFewRows = FUSED_FEW_ROWS;
 
-template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
+template <int W, typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
 void launch_tile(FusedArgs a, hipStream_t st)
 {
     a.out_tiles = (a.n_out + 16 * MT * WM - 1) / (16 * MT * WM);
     a.row_tiles = (a.B + 16 * NT * WN - 1) / (16 * NT * WN);
     const int64_t total = (int64_t)a.out_tiles * a.row_tiles * a.splits;
-    constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D, KS>();
+    constexpr unsigned lds = spk::fused_tile_lds<NS, MT, NT, WM, WN, D, KS, W>();
     static_assert(64 * WM * WN >= 256, "a workgroup can sum a bias gradient too");
     const int64_t sums = a.bias_sums.dbias ? (a.bias_sums.M + 63) / 64 : 0;
-    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D, KS>), dim3((unsigned)((total + 7) / 8 * 8 + sums)),
+    hipLaunchKernelGGL((spk::k_fused_tile<OT, NS, MT, NT, WM, WN, D, KS, W>), dim3((unsigned)((total + 7) / 8 * 8 + sums)),
                        dim3(64 * WM * WN * KS), lds, st, a);
 }
 
@@ -124,10 +153,8 @@ struct TilePlan {
 // four teams, 9.6 in 64 x 64, 25 in 256 x 128; 1536 -> 6144, 2500 rows: 112 in 64 x 32, 46 in
 // 256 x 128; 6144 -> 1536, 33 rows: 14.6 in one part, 11.6 in four; with 1024 rows 30 by two teams,
 // 42 in four parts.
-TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
+TilePlan tile_plan(const TileShape* shapes, int n, int32_t B, int32_t n_out, int32_t steps)
 {
-    const TileShape* shapes = ns == 1 ? kShapes1 : kShapes2;
-    const int n = ns == 1 ? 7 : 5;
     TilePlan best{0, 1};
     float least = 0.0f;
     for (int i = 0; i < n; ++i)
@@ -147,57 +174,74 @@ TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
     return best;
 }
 
+TilePlan tile_plan(int ns, int32_t B, int32_t n_out, int32_t steps)
+{
+    return ns == 1 ? tile_plan(kShapes1, 7, B, n_out, steps) : tile_plan(kShapes2, 5, B, n_out, steps);
+}
+
 // The sums of a split product: rows of n_out rounded up to 8 elements.
 int64_t split_bytes(const TilePlan& p, int32_t B, int32_t n_out)
 {
     return p.splits > 1 ? p.splits * spk::fused_pad(n_out, 8) * B * 4 : 0;
 }
 
+// The steps of a product to p.splits workgroups (`steps`: of the weights), and where there are several their
+// sums, as they are, to `part`.
+void split_product(FusedArgs& a, const TilePlan& p, int steps, float* part)
+{
+    a.splits = p.splits;
+    a.split_steps = (steps + p.splits - 1) / p.splits * (a.steps / steps);
+    if (p.splits > 1) {
+        a.y = part, a.y_type = SPIKE_TYPE_F32, a.ld_y = spk::fused_pad(a.n_out, 8), a.split_stride = a.ld_y * a.B;
+        a.scale = a.row_scale = a.bias = nullptr, a.act = 0, a.residual = a.pre = nullptr, a.vec_out = 1;
+    }
+}
+
+// The sums of a split product to its outputs.
+void join_product(FusedArgs a, const TilePlan& p, const float* part, hipStream_t st)
+{
+    if (p.splits == 1)
+        return;
+    a.splits = p.splits;
+    const int64_t ld = spk::fused_pad(a.n_out, 8);
+    hipLaunchKernelGGL(spk::k_fused_join, spk::row_grid(a.B, ld / 8), dim3(256), 0, st, a, part, ld);
+}
+
 // The product of NS planes of activations; `part`: split_bytes for a split one.
-template <typename OT, int NS>
+template <int W, typename OT, int NS>
 void launch_planes(const FusedArgs& a, float* part, hipStream_t st)
 {
     const TilePlan p = tile_plan(NS, a.B, a.n_out, a.w_steps);
     FusedArgs t = a;
-    t.splits = p.splits;
-    t.split_steps = (a.w_steps + p.splits - 1) / p.splits * (a.steps / a.w_steps);
-    if (p.splits > 1) {
-        t.y = part, t.y_type = SPIKE_TYPE_F32, t.ld_y = spk::fused_pad(a.n_out, 8), t.split_stride = t.ld_y * a.B;
-        t.scale = t.row_scale = t.bias = nullptr, t.act = 0, t.residual = t.pre = nullptr, t.vec_out = 1;
-    }
+    split_product(t, p, a.w_steps, part);
     if constexpr (NS == 1) {
         switch (p.shape) {
-        case 0: launch_tile<OT, NS, 4, 8, 4, 1, 2, 1>(t, st); break;
-        case 1: launch_tile<OT, NS, 2, 8, 4, 1, 2, 1>(t, st); break;
-        case 2: launch_tile<OT, NS, 2, 4, 4, 1, 4, 1>(t, st); break;
-        case 3: launch_tile<OT, NS, 1, 4, 4, 1, 4, 1>(t, st); break;
-        case 4: launch_tile<OT, NS, 2, 4, 4, 1, 4, 2>(t, st); break;
-        case 5: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
-        default: launch_tile<OT, NS, 1, 2, 4, 1, 4, 4>(t, st); break;
+        case 0: launch_tile<W, OT, NS, 4, 8, 4, 1, 2, 1>(t, st); break;
+        case 1: launch_tile<W, OT, NS, 2, 8, 4, 1, 2, 1>(t, st); break;
+        case 2: launch_tile<W, OT, NS, 2, 4, 4, 1, 4, 1>(t, st); break;
+        case 3: launch_tile<W, OT, NS, 1, 4, 4, 1, 4, 1>(t, st); break;
+        case 4: launch_tile<W, OT, NS, 2, 4, 4, 1, 4, 2>(t, st); break;
+        case 5: launch_tile<W, OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
+        default: launch_tile<W, OT, NS, 1, 2, 4, 1, 4, 4>(t, st); break;
         }
     } else {
         switch (p.shape) {
-        case 0: launch_tile<OT, NS, 4, 4, 4, 1, 2, 1>(t, st); break;
-        case 1: launch_tile<OT, NS, 2, 2, 4, 1, 4, 1>(t, st); break;
-        case 2: launch_tile<OT, NS, 1, 2, 4, 1, 4, 1>(t, st); break;
-        case 3: launch_tile<OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
-        default: launch_tile<OT, NS, 2, 4, 4, 1, 2, 1>(t, st); break;
+        case 0: launch_tile<W, OT, NS, 4, 4, 4, 1, 2, 1>(t, st); break;
+        case 1: launch_tile<W, OT, NS, 2, 2, 4, 1, 4, 1>(t, st); break;
+        case 2: launch_tile<W, OT, NS, 1, 2, 4, 1, 4, 1>(t, st); break;
+        case 3: launch_tile<W, OT, NS, 1, 2, 4, 1, 4, 2>(t, st); break;
+        default: launch_tile<W, OT, NS, 2, 4, 4, 1, 2, 1>(t, st); break;
         }
     }
-    if (p.splits > 1) {
-        t = a;
-        t.splits = p.splits;
-        const int64_t ld = spk::fused_pad(a.n_out, 8);
-        hipLaunchKernelGGL(spk::k_fused_join, spk::row_grid(a.B, ld / 8), dim3(256), 0, st, t, part, ld);
-    }
+    join_product(a, p, part, st);
 }
 
-template <typename XT, int NS, int NB, int MT, bool VECX>
+template <int W, typename XT, int NS, int NB, int MT, bool VECX>
 void launch_rows(const FusedArgs& a, hipStream_t st)
 {
     constexpr int WK = 8;
     const dim3 grid((unsigned)((a.n_out + 16 * MT - 1) / (16 * MT)), (unsigned)((a.B + 16 * NB - 1) / (16 * NB)));
-    hipLaunchKernelGGL((spk::k_fused_rows<XT, NS, NB, MT, WK, VECX>), grid, dim3(64 * WK), 0, st, a);
+    hipLaunchKernelGGL((spk::k_fused_rows<XT, NS, NB, MT, WK, VECX, W>), grid, dim3(64 * WK), 0, st, a);
 }
 
 // Few rows.  Tiles of outputs that a workgroup takes together share what it does
@@ -205,18 +249,18 @@ void launch_rows(const FusedArgs& a, hipStream_t st)
 // and the 17th to 32nd row share the weights: FP32, 1536 -> 6144, one row 6.4 us
 // one by one and 5.0 by twos; 1536 -> 57,344 29 and 19 by fours, 16 rows 46 and
 // 20.  Fewer outputs than that leave compute units idle.
-template <typename XT, int NS, bool VECX>
+template <int W, typename XT, int NS, bool VECX>
 void launch_few(const FusedArgs& a, hipStream_t st)
 {
     const int tiles = (a.n_out + 15) / 16;
     if (tiles < kCUs)
-        launch_rows<XT, NS, 1, 1, VECX>(a, st);
+        launch_rows<W, XT, NS, 1, 1, VECX>(a, st);
     else if (tiles < 8 * kCUs)
-        launch_rows<XT, NS, 1, 2, VECX>(a, st);
+        launch_rows<W, XT, NS, 1, 2, VECX>(a, st);
     else if (a.B <= 16)
-        launch_rows<XT, NS, 1, 4, VECX>(a, st);
+        launch_rows<W, XT, NS, 1, 4, VECX>(a, st);
     else
-        launch_rows<XT, NS, 2, 4, VECX>(a, st);
+        launch_rows<W, XT, NS, 2, 4, VECX>(a, st);
 }
 
 // Whether the rows of p start on 16-byte boundaries.
@@ -228,10 +272,10 @@ bool in_chunks(const void* x, int type, int64_t ld, int32_t n)
     return whole(x, type, ld) && n % 8 == 0 && ld < spk::kBufMaxBytes / (256 * (int64_t)type_bytes(type));
 }
 
-template <typename XT, int NS>
+template <int W, typename XT, int NS>
 void few_rows(const FusedArgs& a, bool chunks, hipStream_t st)
 {
-    chunks ? launch_few<XT, NS, true>(a, st) : launch_few<XT, NS, false>(a, st);
+    chunks ? launch_few<W, XT, NS, true>(a, st) : launch_few<W, XT, NS, false>(a, st);
 }
 
 // Planes of cut activations or gradients: their rows are padded to whole chunks.
@@ -327,6 +371,120 @@ int launch_gate(spk::GateArgs a, bool vec, hipStream_t st)
     return (a.B + a.rows - 1) / a.rows;
 }
 
+// The product of forward, x prepared in the workspace where it has to be and the sums of a split product behind that.
+template <int W>
+void launch_forward(FusedArgs& a, int x_type, bool chunks, void* workspace, hipStream_t st)
+{
+    if (a.B <= kFewRows) {
+        switch (x_type) {
+        case SPIKE_TYPE_F32: few_rows<W, float, 3>(a, chunks, st); break;
+        case SPIKE_TYPE_BF16: few_rows<W, spk::bf16, 1>(a, chunks, st); break;
+        default: few_rows<W, spk::f16, 1>(a, chunks, st); break;
+        }
+        return;
+    }
+    float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + prepared_bytes(x_type, chunks, a.B, a.n_in));
+    if (x_type == SPIKE_TYPE_F32)
+        cut_rows(a, workspace, st);
+    else if (!chunks)
+        align_rows(a, workspace, st);
+    switch (x_type) {
+    case SPIKE_TYPE_F32: launch_planes<W, spk::f16, 2>(a, part, st); break;
+    case SPIKE_TYPE_BF16: launch_planes<W, spk::bf16, 1>(a, part, st); break;
+    default: launch_planes<W, spk::f16, 1>(a, part, st); break;
+    }
+}
+
+// The product of backward: rows of g * scale in their form, part: the sums of a split one.
+template <int W>
+void launch_gradient(const FusedArgs& a, GateForm form, float* part, hipStream_t st)
+{
+    switch (form) {
+    case kGateRows: few_rows<W, float, 3>(a, true, st); break;
+    case kGateApart: launch_planes<W, spk::f16, 2>(a, part, st); break;
+    case kGateBeside: launch_planes<W, spk::f16, 1>(a, part, st); break;
+    }
+}
+
+// --- rows of four-bit codes ------------------------------------------------
+
+template <int NB, int MT>
+void launch_mx4_rows(const spk::Mx4Args& m, bool vec, hipStream_t st)
+{
+    constexpr int WK = 8;
+    const dim3 grid((unsigned)((m.f.n_out + 16 * MT - 1) / (16 * MT)), (unsigned)((m.f.B + 16 * NB - 1) / (16 * NB)));
+    if (vec)
+        hipLaunchKernelGGL((spk::k_mx4_rows<NB, MT, WK, true>), grid, dim3(64 * WK), 0, st, m);
+    else
+        hipLaunchKernelGGL((spk::k_mx4_rows<NB, MT, WK, false>), grid, dim3(64 * WK), 0, st, m);
+}
+
+void launch_mx4_few(const spk::Mx4Args& m, bool vec, hipStream_t st)
+{
+    const int tiles = (m.f.n_out + 15) / 16;
+    if (tiles < kCUs)
+        launch_mx4_rows<1, 1>(m, vec, st);
+    else if (tiles < 8 * kCUs)
+        launch_mx4_rows<1, 2>(m, vec, st);
+    else if (m.f.B <= 16)
+        launch_mx4_rows<1, 4>(m, vec, st);
+    else
+        launch_mx4_rows<2, 4>(m, vec, st);
+}
+
+template <int MT, int NT, int WM, int WN, int D>
+void launch_mx4_tile(spk::Mx4Args m, hipStream_t st)
+{
+    FusedArgs& a = m.f;
+    a.out_tiles = (a.n_out + 16 * MT * WM - 1) / (16 * MT * WM);
+    a.row_tiles = (a.B + 16 * NT * WN - 1) / (16 * NT * WN);
+    const int64_t total = (int64_t)a.out_tiles * a.row_tiles * a.splits;
+    hipLaunchKernelGGL((spk::k_mx4_tile<MT, NT, WM, WN, D>), dim3((unsigned)((total + 7) / 8 * 8)), dim3(64 * WM * WN),
+                       (spk::mx4_tile_lds<MT, NT, WM, WN, D>()), st, m);
+}
+
+constexpr TileShape kShapesMx4[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 64, 1, 4.5f, 0.32f, 0.34f}, {64, 64, 1, 3.8f, 0.25f, 0.206f}};
+
+int mx4_steps(int32_t K) { return (K + 127) / 128; }
+
+// Rows of codes that k_mx4_tile takes as they are.
+bool mx4_whole(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, int32_t K)
+{
+    return K % 128 == 0 && aligned_to(codes, 16) && ld_codes % 16 == 0 && ld_codes < spk::kBufMaxBytes / 256 && aligned_to(scales, 4) &&
+           ld_scales % 4 == 0 && ld_scales < spk::kBufMaxBytes / 256;
+}
+
+// Others go through the workspace.
+int64_t mx4_align_bytes(bool whole, int32_t B, int32_t K)
+{
+    const int64_t blocks = 4 * (int64_t)mx4_steps(K);
+    return whole ? 0 : spk::fused_pad(blocks * 17 * B, 16);
+}
+
+void launch_mx4_many(spk::Mx4Args m, bool whole, void* workspace, hipStream_t st)
+{
+    FusedArgs& a = m.f;
+    const TilePlan p = tile_plan(kShapesMx4, 3, a.B, a.n_out, a.steps);
+    float* const part = reinterpret_cast<float*>(static_cast<char*>(workspace) + mx4_align_bytes(whole, a.B, a.n_in));
+    if (!whole) {
+        const int blocks = 4 * a.steps;
+        uint8_t* const codes = static_cast<uint8_t*>(workspace);
+        uint8_t* const scales = codes + (int64_t)blocks * 16 * a.B;
+        const int64_t wgs = ((int64_t)blocks * a.B + 255) / 256;
+        hipLaunchKernelGGL(spk::k_mx4_align, dim3((unsigned)std::min<int64_t>(wgs, 1 << 20)), dim3(256), 0, st,
+                           static_cast<const uint8_t*>(a.x), a.ld_x, m.scales, m.ld_scales, a.B, a.n_in, blocks, codes, scales);
+        a.x = codes, a.ld_x = (int64_t)blocks * 16, m.scales = scales, m.ld_scales = blocks;
+    }
+    const FusedArgs whole_args = a;
+    split_product(a, p, a.steps, part);
+    switch (p.shape) {
+    case 0: launch_mx4_tile<4, 8, 4, 1, 3>(m, st); break;
+    case 1: launch_mx4_tile<2, 4, 4, 1, 4>(m, st); break;
+    default: launch_mx4_tile<1, 4, 4, 1, 4>(m, st); break;
+    }
+    join_product(whole_args, p, part, st);
+}
+
 int check_rows(int32_t B, int32_t act, int x_type, int y_type)
 {
     if (B < 0 || B > FUSED_MAX_B)
@@ -335,6 +493,47 @@ int check_rows(int32_t B, int32_t act, int x_type, int y_type)
         return fail(SPIKE_EINVAL, "activation %d is not a DENSE_ACT_ value", act);
     if (!is_float_type(x_type) || !is_float_type(y_type))
         return fail(SPIKE_EINVAL, "types %d and %d must be F32, BF16 or F16", x_type, y_type);
+    return SPIKE_OK;
+}
+
+int check_weights(int32_t K, int32_t M, int32_t flags)
+{
+    if (K < 1 || K > FUSED_MAX_DIM || M < 1 || M > FUSED_MAX_DIM)
+        return fail(SPIKE_EINVAL, "K = %d, M = %d outside [1, %d]", K, M, FUSED_MAX_DIM);
+    // (rows of K or M elements, 256 of them, also stay within a buffer resource)
+    if (spk::fused_pad(K, 64) * spk::fused_pad(M, 64) >= ((int64_t)1 << 31))
+        return fail(SPIKE_EUNSUPPORTED, "K * M = %lld, each rounded up to 64, reaches 2^31", (long long)K * M);
+    if (flags & ~DENSE_FUSED_BACKWARD)
+        return fail(SPIKE_EINVAL, "unknown flags 0x%x", flags);
+    return SPIKE_OK;
+}
+
+int check_codes(int64_t ld_codes, int64_t ld_scales, int32_t K)
+{
+    if (ld_codes < ((int64_t)K + 1) / 2 || ld_scales < ((int64_t)K + spk::kMxBlock - 1) / spk::kMxBlock)
+        return fail(SPIKE_EINVAL, "row strides %lld and %lld are below the codes or the scales of K = %d", (long long)ld_codes,
+                    (long long)ld_scales, K);
+    return SPIKE_OK;
+}
+
+// A handle whose weights lay_out(handle) lays out on the current device.
+template <typename F>
+int create(int32_t K, int32_t M, spk::WeightKind kind, dense_fused_t* out_handle, F lay_out)
+{
+    dense_fused* h = new (std::nothrow) dense_fused;
+    if (!h)
+        return fail(SPIKE_ENOMEM, "out of host memory");
+    h->K = K, h->M = M, h->kind = kind;
+    hipError_t e = hipGetDevice(&h->device);
+    if (e == hipSuccess)
+        e = lay_out(h);
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        release(h);
+        return e == hipErrorOutOfMemory ? fail(SPIKE_ENOMEM, "out of device memory for the weights' layout")
+                                        : hip_fail(e, "laying out the weights");
+    }
+    *out_handle = h;
     return SPIKE_OK;
 }
 
@@ -352,28 +551,27 @@ int dense_fused_create(const int8_t* Q, const float* scale, int32_t K, int32_t M
         return fail(SPIKE_EINVAL, "null pointer (Q %p, scale %p)", (const void*)Q, (const void*)scale);
     if (!aligned_to(scale, 4))
         return fail(SPIKE_EINVAL, "scale must be 4-byte aligned");
-    if (K < 1 || K > FUSED_MAX_DIM || M < 1 || M > FUSED_MAX_DIM)
-        return fail(SPIKE_EINVAL, "K = %d, M = %d outside [1, %d]", K, M, FUSED_MAX_DIM);
-    // (rows of K or M elements, 256 of them, also stay within a buffer resource)
-    if (spk::fused_pad(K, 64) * spk::fused_pad(M, 64) >= ((int64_t)1 << 31))
-        return fail(SPIKE_EUNSUPPORTED, "K * M = %lld, each rounded up to 64, reaches 2^31", (long long)K * M);
-    if (flags & ~DENSE_FUSED_BACKWARD)
-        return fail(SPIKE_EINVAL, "unknown flags 0x%x", flags);
-    dense_fused* h = new (std::nothrow) dense_fused;
-    if (!h)
-        return fail(SPIKE_ENOMEM, "out of host memory");
-    h->K = K, h->M = M;
-    hipError_t e = hipGetDevice(&h->device);
-    if (e == hipSuccess)
-        e = lay_out(Q, scale, (flags & DENSE_FUSED_BACKWARD) != 0, h);
-    if (e != hipSuccess) {
-        (void)hipGetLastError();
-        release(h);
-        return e == hipErrorOutOfMemory ? fail(SPIKE_ENOMEM, "out of device memory for the weights' layout")
-                                        : hip_fail(e, "laying out the weights");
-    }
-    *out_handle = h;
-    return SPIKE_OK;
+    if (int rc = check_weights(K, M, flags))
+        return rc;
+    return create(K, M, spk::kInt8, out_handle, [&](dense_fused* h) { return lay_out(Q, scale, (flags & DENSE_FUSED_BACKWARD) != 0, h); });
+}
+
+int dense_fused_create_mx4(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, int32_t K, int32_t M,
+                           int32_t flags, dense_fused_t* out_handle)
+{
+    spk::last_error.clear();
+    if (!out_handle)
+        return fail(SPIKE_EINVAL, "null output handle");
+    *out_handle = nullptr;
+    if (!codes || !scales)
+        return fail(SPIKE_EINVAL, "null pointer (codes %p, scales %p)", (const void*)codes, (const void*)scales);
+    if (int rc = check_weights(K, M, flags))
+        return rc;
+    if (int rc = check_codes(ld_codes, ld_scales, K))
+        return rc;
+    return create(K, M, spk::kMx4, out_handle, [&](dense_fused* h) {
+        return lay_out_mx4(codes, ld_codes, scales, ld_scales, (flags & DENSE_FUSED_BACKWARD) != 0, h);
+    });
 }
 
 int dense_fused_destroy(dense_fused_t h)
@@ -422,34 +620,75 @@ int dense_fused_forward(dense_fused_t h, const void* x, int32_t x_type, int64_t 
     if (int rc = check_device(h->device))
         return rc;
     FusedArgs a{};
-    a.P = h->P, a.n_out = h->M, a.n_in = h->K, a.steps = a.w_steps = (h->K + spk::kFusedStep - 1) / spk::kFusedStep;
+    a.P = h->P, a.S = h->S, a.n_out = h->M, a.n_in = h->K, a.steps = a.w_steps = (h->K + spk::kFusedStep - 1) / spk::kFusedStep;
     a.x = x, a.ld_x = ld_x, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
     a.residual = residual, a.ld_residual = ld_residual, a.y = y, a.y_type = y_type, a.ld_y = ld_y;
     a.pre = pre, a.ld_pre = ld_pre;
     a.vec_out = whole(y, y_type, ld_y) && whole(residual, y_type, ld_residual) && whole(pre, y_type, ld_pre);
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const bool chunks = in_chunks(x, x_type, ld_x, h->K);
-    if (B <= kFewRows) {
-        switch (x_type) {
-        case SPIKE_TYPE_F32: few_rows<float, 3>(a, chunks, st); break;
-        case SPIKE_TYPE_BF16: few_rows<spk::bf16, 1>(a, chunks, st); break;
-        default: few_rows<spk::f16, 1>(a, chunks, st); break;
-        }
-    } else {
-        // the workspace: x prepared where it has to be, then the sums of a split product
-        float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + prepared_bytes(x_type, chunks, B, h->K));
-        if (x_type == SPIKE_TYPE_F32)
-            cut_rows(a, workspace, st);
-        else if (!chunks)
-            align_rows(a, workspace, st);
-        switch (x_type) {
-        case SPIKE_TYPE_F32: launch_planes<spk::f16, 2>(a, part, st); break;
-        case SPIKE_TYPE_BF16: launch_planes<spk::bf16, 1>(a, part, st); break;
-        default: launch_planes<spk::f16, 1>(a, part, st); break;
-        }
-    }
+    if (h->kind == spk::kMx4)
+        launch_forward<spk::kMx4>(a, x_type, chunks, workspace, st);
+    else
+        launch_forward<spk::kInt8>(a, x_type, chunks, workspace, st);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "fused projection launch");
+}
+
+int64_t dense_fused_forward_mx4_workspace_bytes(dense_fused_t h, const uint8_t* codes, int64_t ld_codes, const uint8_t* scales,
+                                                int64_t ld_scales, int32_t B)
+{
+    if (!h || h->kind != spk::kMx4 || B < 0 || B > FUSED_MAX_B)
+        return -1;
+    if (B <= kFewRows)
+        return 0;
+    const int64_t sums = split_bytes(tile_plan(kShapesMx4, 3, B, h->M, mx4_steps(h->K)), B, h->M);
+    return sums + mx4_align_bytes(mx4_whole(codes, ld_codes, scales, ld_scales, h->K), B, h->K);
+}
+
+int dense_fused_forward_mx4(dense_fused_t h, const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
+                            int32_t B, const float* bias, int32_t act, const void* residual, int64_t ld_residual, void* y,
+                            int32_t y_type, int64_t ld_y, void* pre, int64_t ld_pre, void* workspace, int64_t workspace_bytes,
+                            void* stream)
+{
+    spk::last_error.clear();
+    if (!h)
+        return fail(SPIKE_EINVAL, "null handle");
+    if (h->kind != spk::kMx4)
+        return fail(SPIKE_EINVAL, "the handle's weights are not four-bit ones");
+    if (int rc = check_rows(B, act, y_type, y_type))
+        return rc;
+    if (int rc = check_codes(ld_codes, ld_scales, h->K))
+        return rc;
+    if (ld_y < h->M || (residual && ld_residual < h->M) || (pre && ld_pre < h->M))
+        return fail(SPIKE_EINVAL, "a row stride is below M = %d", h->M);
+    if (B == 0)
+        return SPIKE_OK;
+    if (!codes || !scales || !y)
+        return fail(SPIKE_EINVAL, "null pointer (codes %p, scales %p, y %p)", (const void*)codes, (const void*)scales, y);
+    if (!aligned_to(y, type_bytes(y_type)) || !aligned_to(bias, 4) || !aligned_to(residual, type_bytes(y_type)) ||
+        !aligned_to(pre, type_bytes(y_type)))
+        return fail(SPIKE_EINVAL, "a pointer is not aligned to its element");
+    const int64_t need = dense_fused_forward_mx4_workspace_bytes(h, codes, ld_codes, scales, ld_scales, B);
+    if (need > 0 && (!workspace || workspace_bytes < need || !aligned_to(workspace, 16)))
+        return fail(SPIKE_EINVAL, "workspace of %lld bytes at %p, needs %lld, 16-byte aligned",
+                    (long long)workspace_bytes, workspace, (long long)need);
+    if (int rc = check_device(h->device))
+        return rc;
+    spk::Mx4Args m{};
+    FusedArgs& a = m.f;
+    a.P = h->P, a.S = h->S, a.n_out = h->M, a.n_in = h->K, a.steps = a.w_steps = mx4_steps(h->K);
+    a.x = codes, a.ld_x = ld_codes, m.scales = scales, m.ld_scales = ld_scales, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
+    a.residual = residual, a.ld_residual = ld_residual, a.y = y, a.y_type = y_type, a.ld_y = ld_y;
+    a.pre = pre, a.ld_pre = ld_pre;
+    a.vec_out = whole(y, y_type, ld_y) && whole(residual, y_type, ld_residual) && whole(pre, y_type, ld_pre);
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (B <= kFewRows)
+        launch_mx4_few(m, h->K % spk::kMxBlock == 0 && aligned_to(codes, 16) && ld_codes % 16 == 0, st);
+    else
+        launch_mx4_many(m, mx4_whole(codes, ld_codes, scales, ld_scales, h->K), workspace, st);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SPIKE_OK : hip_fail(e, "four-bit projection launch");
 }
 
 int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
@@ -539,11 +778,10 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         // the workspace: g * scale (and its rows' scalings), the parts of the bias gradient, the sums of a split product
         float* part = reinterpret_cast<float*>(static_cast<char*>(workspace) + gate_bytes(form, B, h->M) +
                                                spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16));
-        switch (form) {
-        case kGateRows: few_rows<float, 3>(a, true, st); break;
-        case kGateApart: launch_planes<spk::f16, 2>(a, part, st); break;
-        case kGateBeside: launch_planes<spk::f16, 1>(a, part, st); break;
-        }
+        if (h->kind == spk::kMx4)
+            launch_gradient<spk::kFloat8>(a, form, part, st);
+        else
+            launch_gradient<spk::kInt8>(a, form, part, st);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SPIKE_OK : hip_fail(e, "fused projection gradient launch");

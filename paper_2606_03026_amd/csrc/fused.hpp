@@ -8,10 +8,17 @@
 // widened to the activations' type, whatever K and M are (zeros past them).
 // The activations are the B operand, so a lane's four results are four
 // neighbouring outputs of one row.
+//
+// Four-bit weights (quantize.h) lie as [16 outputs][block of 32 inputs][output][16 B], blocks
+// filled up to fours, so that lane 16 g + c finds a whole block of output c in one 16-byte load where a step
+// is 128 inputs, and half of one (inputs 16 g .. 16 g + 15 of 64) in 8 bytes; the blocks' exponents as
+// [16 outputs][four blocks][output][4 B].  The gradient's copy of them, whose sums run across the blocks, is
+// one E5M2 byte a weight (a level times a power of two is one) in the order of the codes.
 #pragma once
 
 #include <type_traits>
 
+#include "mx4.hpp"
 #include "types.hpp"
 
 namespace spk {
@@ -19,11 +26,18 @@ namespace spk {
 constexpr int kFusedTile = 16;  // outputs and rows of one matrix instruction
 constexpr int kFusedStep = 64;  // inputs of one weight load
 
+// What a handle's weights are laid out as.
+enum WeightKind { kInt8, kFloat8, kMx4 };
+
 inline int64_t fused_pad(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 inline int64_t fused_packed_bytes(int64_t n_out, int64_t n_in)
 {
     return fused_pad(n_out, kFusedTile) * fused_pad(n_in, kFusedStep);
 }
+
+// Of four-bit weights: codes, and exponents.
+inline int64_t mx4_packed_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / 2; }
+inline int64_t mx4_scale_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / kMxBlock; }
 
 // Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns; once per
 // handle.  `eights`: rows start on 8-byte boundaries and K is a multiple of 8 (1536 ->
@@ -88,10 +102,51 @@ __device__ inline uint32_t widen_pair(uint32_t w, int i)
     }
 }
 
+// The same of a register of E5M2 bytes, which are F16's upper halves.
 template <typename OT>
-__device__ inline u32x4 widen_codes(uint32_t w0, uint32_t w1)
+__device__ inline uint32_t widen_float8(uint32_t w, int i)
 {
-    return u32x4{widen_pair<OT>(w0, 0), widen_pair<OT>(w0, 1), widen_pair<OT>(w1, 0), widen_pair<OT>(w1, 1)};
+    if constexpr (__is_same(OT, f16)) {
+        return __builtin_amdgcn_perm(w, w, i == 0 ? 0x010c000cu : 0x030c020cu);
+    } else {
+        return __builtin_bit_cast(uint32_t, i == 0 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, false)
+                                                   : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w, 1.0f, true));
+    }
+}
+
+// A lane's 16 codes of a step of 64 inputs, and register j (of four, two values each) of the operand that
+// their half h makes.  `shift`: where a block's exponent lies among the four of a register.
+template <int W> struct StepCodes {
+    u32x4 v;
+
+    template <typename OT>
+    __device__ inline uint32_t widen(int h, int j, int) const
+    {
+        return W == kInt8 ? widen_pair<OT>(v[2 * h + j / 2], j % 2) : widen_float8<OT>(v[2 * h + j / 2], j % 2);
+    }
+};
+template <> struct StepCodes<kMx4> {
+    u32x2 v;
+    uint32_t exponents;
+
+    template <typename OT>
+    __device__ inline uint32_t widen(int h, int j, int shift) const
+    {
+        const float scale = mx_scale(exponents >> shift & 0xffu);
+        switch (j) {
+        case 0: return mx_pair<OT, 0>(v[h], scale);
+        case 1: return mx_pair<OT, 1>(v[h], scale);
+        case 2: return mx_pair<OT, 2>(v[h], scale);
+        default: return mx_pair<OT, 3>(v[h], scale);
+        }
+    }
+};
+
+template <typename OT, int W>
+__device__ inline u32x4 widen_half(const StepCodes<W>& r, int h, int shift)
+{
+    return u32x4{r.template widen<OT>(h, 0, shift), r.template widen<OT>(h, 1, shift), r.template widen<OT>(h, 2, shift),
+                 r.template widen<OT>(h, 3, shift)};
 }
 
 // What of x is left after its upper 16 bits are taken off as a BF16 part; FIRST:
@@ -349,6 +404,7 @@ struct BiasArgs {
 
 struct FusedArgs {
     const int8_t* P;     // weights, laid out
+    const int8_t* S;     // exponents of four-bit ones
     int n_out, n_in, steps;
     int w_steps;         // k_fused_tile: steps of an output's weights; walked again by the steps past them
     const void* x;
@@ -480,11 +536,15 @@ struct OutputColumns {
 // rows: 3.0).  Asking whether three parts left anything costs 0 to 8% of an FP32 call (6144 ->
 // 1536, 7 rows: 10.2 us without, 11.3).
 // Rows that are not there cost no loads, only idle columns of the matrix instruction.
-template <typename XT, int NS, int NB, int MT, int WK, bool VECX>
+// Four-bit weights go in steps of 128 inputs, a lane group's quarter of a step being one block.
+template <typename XT, int NS, int NB, int MT, int WK, bool VECX, int W>
 __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 {
     typedef typename Operand<XT>::type OT;
-    constexpr int U = MT * NB >= 4 ? 1 : MT * NB >= 2 ? 2 : 4;  // steps in flight
+    constexpr bool kFour = W == kMx4;
+    constexpr int U = (MT * NB >= 4 ? 1 : MT * NB >= 2 ? 2 : 4) / (kFour && MT * NB < 4 ? 2 : 1);  // steps in flight
+    constexpr int kStep = kFour ? 128 : kFusedStep, kParts = kStep / 32;
+    const int n_steps = kFour ? (a.steps + 1) / 2 : a.steps;
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, c = lane % 16;
     const int tile0 = blockIdx.x * MT;
@@ -492,6 +552,7 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
     const XT* const x0 = static_cast<const XT*>(a.x) + b0 * a.ld_x;
     const __amdgpu_buffer_rsrc_t xr = rows_resource(x0), wr = weight_resource(a.P, kBufMaxBytes);
+    const __amdgpu_buffer_rsrc_t er = weight_resource(kFour ? a.S : a.P, kBufMaxBytes);
     static_assert(MT * NB <= WK, "a wave joins one tile's sums");
     // the waves that join sums ask for their columns first: these are back when the sums are
     OutputColumns<4> columns;
@@ -503,40 +564,46 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
 #pragma unroll
         for (int n = 0; n < NB; ++n)
             acc[t][n] = f32x4{};
-    for (int s0 = w; s0 < a.steps; s0 += WK * U) {
+    for (int s0 = w; s0 < n_steps; s0 += WK * U) {
         u32x4 wt[U][MT];
-        Raw<XT> x[U][NB][2];
+        uint32_t exponent[U][MT];
+        Raw<XT> x[U][NB][kParts];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int s = s0 + u * WK;
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 // (the vector offset is the one that the range check sees first)
-                const bool live = s < a.steps && tile0 + t < tiles;
-                const uint32_t piece = live ? ((uint32_t)(tile0 + t) * a.steps + s) * 1024u : 0u;
+                const bool live = s < n_steps && tile0 + t < tiles;
+                const uint32_t at = live ? (uint32_t)(tile0 + t) * n_steps + s : 0u, piece = at * 1024u;
                 wt[u][t] = __builtin_bit_cast(
                     u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, piece, 0));
+                if constexpr (kFour)
+                    exponent[u][t] = __builtin_amdgcn_raw_buffer_load_b8(er, live ? c * 4u + g : kOutOfRange, at * 64u, 0);
             }
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 const int b = 16 * n + c;
-                const bool live = b0 + b < a.B && s < a.steps;
+                const bool live = b0 + b < a.B && s < n_steps;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < kParts; ++h)
                     x[u][n][h] = load_raw<XT, VECX>(x0, xr, min((int64_t)b, a.B - 1 - b0) * a.ld_x,
-                                                    live ? s * kFusedStep + 32 * h + 8 * g : a.n_in, a.n_in);
+                                                    live ? s * kStep + (kFour ? 32 * g + 8 * h : 32 * h + 8 * g) : a.n_in, a.n_in);
             }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (s0 + u * WK >= a.steps)
+            if (s0 + u * WK >= n_steps)
                 break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < kParts; ++h) {
                 u32x4 wo[MT];
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
-                    wo[t] = widen_codes<OT>(wt[u][t][2 * h], wt[u][t][2 * h + 1]);
+                    if constexpr (kFour)
+                        wo[t] = mx_eight<OT>(wt[u][t][h], mx_scale(exponent[u][t]));
+                    else
+                        wo[t] = widen_half<OT, W>(StepCodes<W>{wt[u][t]}, h, 0);
 #pragma unroll
                 for (int n = 0; n < NB; ++n) {
                     u32x4 part[NS];
@@ -618,6 +685,14 @@ __device__ inline void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, ui
                  : "memory");
 }
 
+// The same of 4 bytes a lane.
+__device__ inline void load_words_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint32_t off, uint32_t at, uint32_t to)
+{
+    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dword %0, %1, %3 offen lds" ::"v"(off), "s"(rsrc),
+                 "s"(__builtin_amdgcn_readfirstlane(to)), "s"(__builtin_amdgcn_readfirstlane(at))
+                 : "memory");
+}
+
 // All but the wave's N newest loads have landed.
 template <int N>
 __device__ inline void wait_loads()
@@ -630,15 +705,58 @@ __device__ inline uint32_t lds_address(const void* p)
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
 }
 
-template <int NS, int MT, int NT, int WM, int WN>
-constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * MT * 1024; }
+// Loads, and bytes, of a wave's weights of a step: four-bit ones of two tiles a load, and their exponents.
+template <int MT, int W>
+constexpr int fused_weight_loads() { return W == kMx4 ? (MT + 1) / 2 + 1 : MT; }
+template <int MT, int W>
+constexpr int fused_weight_bytes() { return W == kMx4 ? (MT + 1) / 2 * 1024 + 256 : MT * 1024; }
 
-template <int NS, int MT, int NT, int WM, int WN, int D, int KS>
+template <int NS, int MT, int NT, int WM, int WN, int W>
+constexpr int fused_stage_bytes() { return NS * 16 * NT * WN * 128 + WM * WN * fused_weight_bytes<MT, W>(); }
+
+template <int NS, int MT, int NT, int WM, int WN, int D, int KS, int W>
 constexpr int fused_tile_lds()
 {
-    constexpr int rings = KS * D * fused_stage_bytes<NS, MT, NT, WM, WN>();
+    constexpr int rings = KS * D * fused_stage_bytes<NS, MT, NT, WM, WN, W>();
     constexpr int joining = (KS - 1) * WM * WN * MT * NT * 1024, turning = WM * WN * 2 * 16 * 16 * MT * 4;
     return rings > joining + turning ? rings : joining + turning;
+}
+
+// A wave's sums of 16 MT outputs (from tile tile0 on) x 16 NT rows (from b0 on) to memory: 32 rows at a time
+// through this wave's own part of LDS, where the 16-byte chunk q of row r lies at q ^ (r % (4 MT)).
+// UNDO: rows may have been scaled.  y_at: elements from y's start to the rows.
+template <int MT, int NT, bool UNDO>
+__device__ inline void put_tile(const FusedArgs& a, const f32x4 (&acc)[MT][NT], f32x4* s_out, int tile0, int64_t b0, int64_t y_at)
+{
+    const int lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
+    float undo[NT];  // a lane's results belong to one row of each tile
+    if constexpr (UNDO) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+            undo[n] = a.row_scale ? a.row_scale[min(b0 + n * 16 + c, (int64_t)a.B - 1)] : 1.0f;
+    }
+    constexpr int kVecs = 2 * MT;  // of 8 outputs, in a row
+    static_assert(64 % kVecs == 0, "a lane keeps its outputs");
+    const int q = lane % kVecs * 2;
+    OutputColumns<8> columns;
+    columns.load(a, tile0 * 16 + 4 * q);
+#pragma unroll
+    for (int n0 = 0; n0 < NT; n0 += 2) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] = UNDO ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
+            const f32x4 lo = s_out[r * 4 * MT + (q ^ (r % 16 % (4 * MT)))];
+            const f32x4 hi = s_out[r * 4 * MT + ((q + 1) ^ (r % 16 % (4 * MT)))];
+            float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            columns.template store<true>(a, b0 + n0 * 16 + r, z, y_at);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
@@ -663,13 +781,15 @@ constexpr int fused_tile_lds()
 // matrix units busy 45% of the time, LDS 4%; 8192 rows of 6144 -> 1536, two planes, 243 us
 // and 1272 TFLOP/s, 59%.
 // Codes widened by byte moves and packed F16 sums instead of conversions: no change.
-template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS>
+template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS, int W>
 __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
 {
+    constexpr bool kFour = W == kMx4;
     constexpr int kThreads = 64 * WM * WN, kRows = 16 * NT * WN;  // threads of a group
     constexpr int kChunks = kRows * 8 / kThreads;  // 16-byte chunks of a plane that a thread fetches per step
-    constexpr int kStage = fused_stage_bytes<NS, MT, NT, WM, WN>();
-    constexpr int kLoads = NS * kChunks + MT;      // of a wave and step
+    constexpr int kStage = fused_stage_bytes<NS, MT, NT, WM, WN, W>();
+    constexpr int kWaveWeights = fused_weight_bytes<MT, W>();
+    constexpr int kLoads = NS * kChunks + fused_weight_loads<MT, W>();  // of a wave and step
     static_assert(kChunks >= 1 && kRows * 8 % kThreads == 0, "every thread fetches whole chunks");
     static_assert(NT % 2 == 0, "sums are turned around in pairs of row tiles");
     // From three stages on, the next step's is there one step early, and is read into
@@ -707,10 +827,22 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     const int64_t b0 = (int64_t)row_tile * kRows;
 
     const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes);
-    uint32_t w_at[MT];
+    const __amdgpu_buffer_rsrc_t er = weight_resource(kFour ? a.S : a.P, kBufMaxBytes);
+    uint32_t w_at[MT], e_at = 0;
+    // tiles past the outputs repeat the last one; their results are not stored
+    if constexpr (kFour) {
+        const uint32_t pairs = (a.w_steps + 1) / 2;
 #pragma unroll
-    for (int t = 0; t < MT; ++t)  // tiles past the outputs repeat the last one; their results are not stored
-        w_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * a.w_steps * 1024u;
+        for (int t = 0; t < MT; t += 2) {
+            const int half = t + 1 < MT ? lane / 32 : 0;
+            w_at[t] = (uint32_t)min(tile0 + t + half, tiles - 1) * pairs * 1024u + lane % 32 * 16u;
+        }
+        e_at = (uint32_t)min(tile0 + min(g, MT - 1), tiles - 1) * pairs * 64u + c * 4u;
+    } else {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            w_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * a.w_steps * 1024u;
+    }
     __amdgpu_buffer_rsrc_t xr[NS];
 #pragma unroll
     for (int p = 0; p < NS; ++p)
@@ -731,10 +863,17 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
         const uint32_t at = s < steps ? s : 0, to = lds + buf * kStage;
         const uint32_t step = first + at, w_step = step - (step >= (uint32_t)a.w_steps ? a.w_steps : 0);
         auto weights = [&]() __attribute__((always_inline)) {
+            const uint32_t mine = to + kWeights + w * kWaveWeights;
+            if constexpr (kFour) {
+#pragma unroll
+                for (int t = 0; t < MT; t += 2)
+                    load_to_lds(wr, s < steps ? w_at[t] : kOutOfRange, w_step * 512u, mine + t * 512);
+                load_words_to_lds(er, s < steps ? e_at : kOutOfRange, w_step / 2 * 64u, mine + (MT + 1) / 2 * 1024);
+                return;
+            }
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + w_step * 1024u,
-                            to + kWeights + (w * MT + t) * 1024);
+                load_to_lds(wr, s < steps ? lane * 16u : kOutOfRange, w_at[t] + w_step * 1024u, mine + t * 1024);
         };
         if (kWeightsFirst)
             weights();
@@ -753,16 +892,31 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             acc[t][n] = f32x4{};
-    u32x4 wt[MT], wo[2][MT];  // a step's codes; the operands of its two halves
-    const u32x4* const s_w = s_ring + kWeights / 16 + w * MT * 64 + lane;
+    StepCodes<W> wt[MT];
+    u32x4 wo[2][MT];  // a step's codes; the operands of its two halves
+    // a lane's codes of tile t in a stage (of its own wave's weights)
+    const char* const s_w = reinterpret_cast<const char*>(s_ring) + kWeights + w * kWaveWeights;
+    auto codes = [&](int stage, int t) __attribute__((always_inline)) {
+        const char* const p = s_w + stage * kStage;
+        StepCodes<W> r;
+        if constexpr (kFour) {
+            r.v = *reinterpret_cast<const u32x2*>(p + t * 512 + g / 2 * 256 + c * 16 + g % 2 * 8);
+            r.exponents = *reinterpret_cast<const uint32_t*>(p + (MT + 1) / 2 * 1024 + t * 64 + c * 4);
+        } else {
+            r.v = *reinterpret_cast<const u32x4*>(p + t * 1024 + lane * 16);
+        }
+        return r;
+    };
+    // where the exponent of the lane's block in step s lies among those of its pair of steps
+    auto shift_of = [&](int s) __attribute__((always_inline)) { return kFour ? ((first + s) & 1) * 16 + g / 2 * 8 : 0; };
 #pragma unroll
     for (int s = 0; s < D - 1; ++s)
         fetch(s, s);
     wait_loads<kBehind>();
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        wt[t] = s_w[t * 64];
-        wo[0][t] = widen_codes<OT>(wt[t][0], wt[t][1]);
+        wt[t] = codes(0, t);
+        wo[0][t] = widen_half<OT, W>(wt[t], 0, shift_of(0));
     }
     __syncthreads();
     // One step, in items of one operand of activations times MT of weights.  While an
@@ -773,14 +927,15 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     // (waves that multiply go before the waves of another workgroup that store)
     __builtin_amdgcn_s_setprio(1);
     int cur = 0;
-    const int c0 = g ^ (c % 8), c1 = (4 + g) ^ (c % 8);
+    const int c0 = (kFour ? 2 * g : g) ^ (c % 8), c1 = (kFour ? 2 * g + 1 : 4 + g) ^ (c % 8);
     auto read = [&](int stage, int item) __attribute__((always_inline)) {
         const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
         return s_ring[stage * (kStage / 16) + ((p * kRows + (wn * NT + n) * 16 + c) * 8 + (h == 0 ? c0 : c1))];
     };
     if constexpr (kEarly) {
         // all of the next step's operands and codes are read while this step's are multiplied
-        u32x4 xs[2][kItems], ws[2][MT];
+        u32x4 xs[2][kItems];
+        StepCodes<W> ws[2][MT];
 #pragma unroll
         for (int item = 0; item < kItems; ++item)
             xs[0][item] = read(0, item);
@@ -792,7 +947,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
             const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                ws[1 - q][t] = s_w[next * (kStage / 16) + t * 64];
+                ws[1 - q][t] = codes(next, t);
+            const int shift = shift_of(s), shift_next = shift_of(s + 1);
 #pragma unroll
             for (int item = 0; item < kItems; ++item)
                 xs[1 - q][item] = read(next, item);
@@ -807,7 +963,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
 #pragma unroll
                     for (int v = 0; v < 4 * MT; ++v)
                         if (v * kHalf / 4 == in_half * MT + t)
-                            wo[1 - h][v / 4][v % 4] = widen_pair<OT>(h == 0 ? ws[q][v / 4][2 + v % 4 / 2] : ws[1 - q][v / 4][v % 4 / 2], v % 2);
+                            wo[1 - h][v / 4][v % 4] = h == 0 ? ws[q][v / 4].template widen<OT>(1, v % 4, shift)
+                                                             : ws[1 - q][v / 4].template widen<OT>(0, v % 4, shift_next);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -822,6 +979,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     } else {
         for (int s = 0; s < walk; ++s) {
             const int next = cur + 1 == D ? 0 : cur + 1, last = cur == 0 ? D - 1 : cur - 1;
+            const int shift = shift_of(s), shift_next = shift_of(s + 1);
             u32x4 xo[3];
             xo[0] = read(cur, 0);
             xo[1] = read(cur, 1);
@@ -837,7 +995,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                     wait_loads<kWeightsFirst ? NS * kChunks : 0>();
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
-                        wt[t] = s_w[next * (kStage / 16) + t * 64];
+                        wt[t] = codes(next, t);
                 }
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
@@ -847,7 +1005,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                     for (int v = 0; v < 4 * MT; ++v) {
                         const int slot = h == 0 ? v * kHalf / 4 : MT + v * (kHalf - 1) / 4;
                         if (slot == in_half * MT + t)
-                            wo[1 - h][v / 4][v % 4] = widen_pair<OT>(wt[v / 4][(h == 0 ? 2 : 0) + v % 4 / 2], v % 2);
+                            wo[1 - h][v / 4][v % 4] = wt[v / 4].template widen<OT>(1 - h, v % 4, h == 0 ? shift : shift_next);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -883,40 +1041,9 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                 for (int n = 0; n < NT; ++n)
                     acc[t][n] += s_join[k * kTeam + (t * NT + n) * 64];
     }
-    float undo[NT];  // a lane's results belong to one row of each tile
-    if constexpr (__is_same(OT, f16)) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-            undo[n] = a.row_scale ? a.row_scale[min(b0 + (wn * NT + n) * 16 + c, (int64_t)a.B - 1)] : 1.0f;
-    }
-    // 32 rows x 16 MT outputs at a time, in this wave's own part of LDS; the
-    // 16-byte chunk q of row r lies at q ^ (r % (4 MT))
     // (behind the other teams' sums)
     f32x4* const s_out = reinterpret_cast<f32x4*>(s_fused) + (KS - 1) * WM * WN * MT * NT * 64 + w * 2 * 16 * 4 * MT;
-    constexpr int kVecs = 2 * MT;  // of 8 outputs, in a row
-    static_assert(64 % kVecs == 0, "a lane keeps its outputs");
-    const int q = lane % kVecs * 2;
-    OutputColumns<8> columns;
-    columns.load(a, tile0 * 16 + 4 * q);
-    const int64_t y_at = split * a.split_stride;
-#pragma unroll
-    for (int n0 = 0; n0 < NT; n0 += 2) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] =
-                    __is_same(OT, f16) ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-        for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
-            const f32x4 lo = s_out[r * 4 * MT + (q ^ (r % 16 % (4 * MT)))];
-            const f32x4 hi = s_out[r * 4 * MT + ((q + 1) ^ (r % 16 % (4 * MT)))];
-            float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-            columns.template store<true>(a, b0 + (wn * NT + n0) * 16 + r, z, y_at);
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
+    put_tile<MT, NT, __is_same(OT, f16)>(a, acc, s_out, tile0, b0 + wn * NT * 16, split * a.split_stride);
 }
 
 // The join, and the copy below, walk rows of vectors of 8: a wave along a row, the four waves

@@ -1,4 +1,4 @@
-// Host side of the INT8 quantizer/exporter (C ABI in include/quantize.h):
+// Host side of the quantizers (C ABI in include/quantize.h):
 // validation and the launches.  No allocation, no synchronisation.
 #include "quantize.h"
 
@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "errors.hpp"
+#include "mx4.hpp"
 #include "quantize.hpp"
 
 namespace {
@@ -26,6 +27,17 @@ void launch_tile(bool vec, dim3 grid, hipStream_t st, const float* W, const floa
     else
         hipLaunchKernelGGL((spk::k_quant_tile<COL, false>), grid, dim3(spk::kQuantBlock), 0, st, W, scale, M, K, Q,
                            tiles_k);
+}
+
+template <typename T>
+void launch_mx4(const spk::QuantMx4Args& a, bool vec, hipStream_t st)
+{
+    constexpr uint32_t per = 256 * spk::kQuantMx4Unroll;
+    const dim3 grid((a.units + per - 1) / per);
+    if (vec)
+        hipLaunchKernelGGL((spk::k_quant_mx4<T, true>), grid, dim3(256), 0, st, a);
+    else
+        hipLaunchKernelGGL((spk::k_quant_mx4<T, false>), grid, dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -111,6 +123,43 @@ int spike_quantize_int8(const float* W, int32_t M, int32_t K, int32_t layout, in
     if (e != hipSuccess)
         return hip_fail(e, "quantizer launch");
     return SPIKE_OK;
+}
+
+int spike_quantize_mx4(const void* x, int32_t x_type, int64_t ld_x, int32_t M, int32_t K, uint8_t* codes, int64_t ld_codes,
+                       uint8_t* scales, int64_t ld_scales, void* values, int64_t ld_values, void* stream)
+{
+    spk::last_error.clear();
+    if (M < 0 || M > (1 << 24) || K < 1 || K > (1 << 24))
+        return fail(SPIKE_EINVAL, "M = %d, K = %d outside [0, 2^24], [1, 2^24]", M, K);
+    if ((int64_t)M * K > (int64_t)1 << 31)
+        return fail(SPIKE_EINVAL, "M * K = %lld exceeds 2^31", (long long)M * K);
+    if (!spk::is_float_type(x_type))
+        return fail(SPIKE_EINVAL, "type %d is not F32, BF16 or F16", x_type);
+    const int64_t blocks = ((int64_t)K + spk::kMxBlock - 1) / spk::kMxBlock;
+    if (ld_x < K || ld_codes < ((int64_t)K + 1) / 2 || ld_scales < blocks || (values && ld_values < K))
+        return fail(SPIKE_EINVAL, "a row stride is below K = %d elements, their codes or their scales", K);
+    if (M == 0)
+        return SPIKE_OK;
+    if (!x || !codes || !scales)
+        return fail(SPIKE_EINVAL, "null pointer (x %p, codes %p, scales %p)", x, (void*)codes, (void*)scales);
+    if (values == x && ld_values != ld_x)
+        return fail(SPIKE_EINVAL, "values is x with another row stride");
+    const int b = spk::type_bytes(x_type);
+    if (!aligned(x, b) || !aligned(values, b))
+        return fail(SPIKE_EINVAL, "a pointer is not aligned to its element");
+    spk::QuantMx4Args a{};
+    a.x = x, a.ld_x = ld_x, a.M = M, a.K = K, a.eights = (uint32_t)(blocks * (spk::kMxBlock / 8)), a.units = (uint32_t)(M * blocks * (spk::kMxBlock / 8));
+    a.codes = codes, a.ld_codes = ld_codes, a.scales = scales, a.ld_scales = ld_scales, a.values = values, a.ld_values = ld_values;
+    const bool vec = K % 8 == 0 && aligned(x, 16) && ld_x * b % 16 == 0 && aligned(codes, 4) && ld_codes % 4 == 0 &&
+                     (!values || (aligned(values, 16) && ld_values * b % 16 == 0));
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    switch (x_type) {
+    case SPIKE_TYPE_F32: launch_mx4<float>(a, vec, st); break;
+    case SPIKE_TYPE_BF16: launch_mx4<spk::bf16>(a, vec, st); break;
+    default: launch_mx4<spk::f16>(a, vec, st); break;
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SPIKE_OK : hip_fail(e, "quantizer launch");
 }
 
 int spike_check_scale_shape(int32_t M, int32_t K, int32_t group, int32_t scale_rows, int32_t scale_cols)
