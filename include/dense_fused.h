@@ -60,7 +60,7 @@
  * below 2^31; 0 <= B <= FUSED_MAX_B.
  *
  * A handle owns its copies of the weights (1 byte each, twice that with
- * DENSE_FUSED_BACKWARD; four-bit ones 17/32 of a byte and one more); calls on it only read them, so it may be used on
+ * DENSE_FUSED_BACKWARD; four-bit ones 9/16 of a byte and one more); calls on it only read them, so it may be used on
  * several streams at once.  forward and backward enqueue kernels on `stream`
  * (a hipStream_t, NULL for the default stream), allocate nothing, do not
  * synchronise and can be captured in a HIP graph.  The workspaces (their sizes

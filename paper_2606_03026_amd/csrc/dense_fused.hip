@@ -18,6 +18,7 @@ struct dense_fused {
     spk::WeightKind kind = spk::kInt8;
     int8_t* P = nullptr;     // rows of Q as outputs; the one allocation, which holds the others too
     int8_t* S = nullptr;     // exponents of four-bit weights
+    int8_t* E = nullptr;     // the same in k_mx4_tile's order
     int8_t* Pt = nullptr;    // columns of Q as outputs (DENSE_FUSED_BACKWARD)
     float* scale = nullptr;  // [M rounded up to 16], zeros past M
 };
@@ -73,21 +74,24 @@ hipError_t lay_out(const int8_t* Q, const float* scale, bool backward, dense_fus
 hipError_t lay_out_mx4(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales, bool backward, dense_fused* h)
 {
     const int64_t bytes = spk::mx4_packed_bytes(h->M, h->K), bytes_s = spk::mx4_scale_bytes(h->M, h->K);
-    const int64_t bytes_t = backward ? spk::fused_packed_bytes(h->K, h->M) : 0;
+    const int64_t bytes_e = spk::mx4_scale_bytes(h->M, spk::fused_pad(h->K, 512));
+    const int64_t bytes_t = backward ? spk::mx4_gradient_bytes(h->K, h->M) : 0;
     const int padded = (int)spk::fused_pad(h->M, spk::kFusedTile);
-    hipError_t e = hipMalloc(&h->P, (size_t)(bytes + bytes_s + bytes_t + padded * (int64_t)(sizeof(float) + 1)));
+    hipError_t e = hipMalloc(&h->P, (size_t)(bytes + bytes_s + bytes_e + bytes_t + padded * (int64_t)(sizeof(float) + 1)));
     if (e == hipSuccess)
         e = hipDeviceSynchronize();  // the codes may still be in flight on any stream
     if (e != hipSuccess)
         return e;
     h->S = h->P + bytes;
-    h->Pt = backward ? h->S + bytes_s : nullptr;
-    h->scale = reinterpret_cast<float*>(h->S + bytes_s + bytes_t);
+    h->E = h->S + bytes_s;
+    h->Pt = backward ? h->E + bytes_e : nullptr;
+    h->scale = reinterpret_cast<float*>(h->E + bytes_e + bytes_t);
     uint8_t* const top = reinterpret_cast<uint8_t*>(h->scale + padded);
     hipLaunchKernelGGL(spk::k_mx4_top, dim3((unsigned)((padded + 3) / 4)), dim3(256), 0, nullptr, codes, ld_codes, scales, ld_scales,
                        h->K, h->M, padded, top, h->scale);
     hipLaunchKernelGGL(spk::k_mx4_pack, dim3((unsigned)((bytes / 16 + 255) / 256)), dim3(256), 0, nullptr, codes, ld_codes, scales,
-                       ld_scales, h->K, h->M, top, reinterpret_cast<uint8_t*>(h->P), reinterpret_cast<uint8_t*>(h->S), bytes / 16);
+                       ld_scales, h->K, h->M, top, reinterpret_cast<uint8_t*>(h->P), reinterpret_cast<uint8_t*>(h->S),
+                       reinterpret_cast<uint8_t*>(h->E), bytes / 16);
     if (backward)
         hipLaunchKernelGGL(spk::k_mx4_pack_columns, dim3((unsigned)((bytes_t / 16 + 255) / 256)), dim3(256), 0, nullptr, codes,
                            ld_codes, scales, ld_scales, h->K, h->M, top, h->Pt, bytes_t / 16);
@@ -240,7 +244,8 @@ template <int W, typename XT, int NS, int NB, int MT, bool VECX>
 void launch_rows(const FusedArgs& a, hipStream_t st)
 {
     constexpr int WK = 8;
-    const dim3 grid((unsigned)((a.n_out + 16 * MT - 1) / (16 * MT)), (unsigned)((a.B + 16 * NB - 1) / (16 * NB)));
+    const int64_t outs = spk::fused_pad(a.n_out, W == spk::kInt8 ? 16 : 32);
+    const dim3 grid((unsigned)((outs + 16 * MT - 1) / (16 * MT)), (unsigned)((a.B + 16 * NB - 1) / (16 * NB)));
     hipLaunchKernelGGL((spk::k_fused_rows<XT, NS, NB, MT, WK, VECX, W>), grid, dim3(64 * WK), 0, st, a);
 }
 
@@ -412,7 +417,7 @@ template <int NB, int MT>
 void launch_mx4_rows(const spk::Mx4Args& m, bool vec, hipStream_t st)
 {
     constexpr int WK = 8;
-    const dim3 grid((unsigned)((m.f.n_out + 16 * MT - 1) / (16 * MT)), (unsigned)((m.f.B + 16 * NB - 1) / (16 * NB)));
+    const dim3 grid((unsigned)((spk::fused_pad(m.f.n_out, 32) + 16 * MT - 1) / (16 * MT)), (unsigned)((m.f.B + 16 * NB - 1) / (16 * NB)));
     if (vec)
         hipLaunchKernelGGL((spk::k_mx4_rows<NB, MT, WK, true>), grid, dim3(64 * WK), 0, st, m);
     else
@@ -678,7 +683,7 @@ int dense_fused_forward_mx4(dense_fused_t h, const uint8_t* codes, int64_t ld_co
     spk::Mx4Args m{};
     FusedArgs& a = m.f;
     a.P = h->P, a.S = h->S, a.n_out = h->M, a.n_in = h->K, a.steps = a.w_steps = mx4_steps(h->K);
-    a.x = codes, a.ld_x = ld_codes, m.scales = scales, m.ld_scales = ld_scales, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
+    a.x = codes, a.ld_x = ld_codes, m.scales = scales, m.ld_scales = ld_scales, m.E = h->E, a.B = B, a.scale = h->scale, a.bias = bias, a.act = act;
     a.residual = residual, a.ld_residual = ld_residual, a.y = y, a.y_type = y_type, a.ld_y = ld_y;
     a.pre = pre, a.ld_pre = ld_pre;
     a.vec_out = whole(y, y_type, ld_y) && whole(residual, y_type, ld_residual) && whole(pre, y_type, ld_pre);

@@ -10,10 +10,12 @@
 // neighbouring outputs of one row.
 //
 // Four-bit weights (quantize.h) lie as [16 outputs][block of 32 inputs][output][16 B], blocks
-// filled up to fours, so that lane 16 g + c finds a whole block of output c in one 16-byte load where a step
+// filled up to fours and outputs to 32, so that lane 16 g + c finds a whole block of output c in one 16-byte load where a step
 // is 128 inputs, and half of one (inputs 16 g .. 16 g + 15 of 64) in 8 bytes; the blocks' exponents as
 // [16 outputs][four blocks][output][4 B].  The gradient's copy of them, whose sums run across the blocks, is
-// one E5M2 byte a weight (a level times a power of two is one) in the order of the codes.
+// one E5M2 byte a weight (a level times a power of two is one) in the order of INT8 codes.  In both, two tiles
+// share 32 outputs so that a lane's results of them are eight neighbours (mx4_output), which it stores
+// without going through LDS.
 #pragma once
 
 #include <type_traits>
@@ -35,9 +37,20 @@ inline int64_t fused_packed_bytes(int64_t n_out, int64_t n_in)
     return fused_pad(n_out, kFusedTile) * fused_pad(n_in, kFusedStep);
 }
 
-// Of four-bit weights: codes, and exponents.
-inline int64_t mx4_packed_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / 2; }
-inline int64_t mx4_scale_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / kMxBlock; }
+// Of four-bit weights: codes, exponents, and the gradient's copy.
+inline int64_t mx4_packed_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, 2 * kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / 2; }
+inline int64_t mx4_scale_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, 2 * kFusedTile) * fused_pad(n_in, 4 * kMxBlock) / kMxBlock; }
+inline int64_t mx4_gradient_bytes(int64_t n_out, int64_t n_in) { return fused_pad(n_out, 2 * kFusedTile) * fused_pad(n_in, kFusedStep); }
+
+// The output in row i of a tile: rows 4 g .. 4 g + 3 of an even tile and of the odd one after it are
+// outputs 8 g .. 8 g + 7 of their 32.
+__host__ __device__ inline int64_t mx4_output(int64_t tile, int i) { return tile / 2 * 32 + i / 4 * 8 + tile % 2 * 4 + i % 4; }
+
+// Tiles of weights, and the first of a lane group's four outputs in one.
+template <int W>
+__device__ inline int fused_tiles(int n_out) { return W == kInt8 ? (n_out + kFusedTile - 1) / kFusedTile : (n_out + 2 * kFusedTile - 1) / (2 * kFusedTile) * 2; }
+template <int W>
+__device__ inline int fused_output(int tile, int g) { return W == kInt8 ? tile * kFusedTile + 4 * g : (int)mx4_output(tile, 4 * g); }
 
 // Lays out Q [M][K] with its rows as outputs, or (TRANSPOSE) its columns; once per
 // handle.  `eights`: rows start on 8-byte boundaries and K is a multiple of 8 (1536 ->
@@ -549,7 +562,7 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     const int g = lane / 16, c = lane % 16;
     const int tile0 = blockIdx.x * MT;
     const int64_t b0 = (int64_t)blockIdx.y * 16 * NB;
-    const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
+    const int tiles = fused_tiles<W>(a.n_out);
     const XT* const x0 = static_cast<const XT*>(a.x) + b0 * a.ld_x;
     const __amdgpu_buffer_rsrc_t xr = rows_resource(x0), wr = weight_resource(a.P, kBufMaxBytes);
     const __amdgpu_buffer_rsrc_t er = weight_resource(kFour ? a.S : a.P, kBufMaxBytes);
@@ -557,7 +570,7 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     // the waves that join sums ask for their columns first: these are back when the sums are
     OutputColumns<4> columns;
     if (w < MT * NB)
-        columns.load(a, (tile0 + w / NB) * 16 + 4 * g);
+        columns.load(a, fused_output<W>(tile0 + w / NB, g));
     f32x4 acc[MT][NB];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -724,8 +737,8 @@ constexpr int fused_tile_lds()
 
 // A wave's sums of 16 MT outputs (from tile tile0 on) x 16 NT rows (from b0 on) to memory: 32 rows at a time
 // through this wave's own part of LDS, where the 16-byte chunk q of row r lies at q ^ (r % (4 MT)).
-// UNDO: rows may have been scaled.  y_at: elements from y's start to the rows.
-template <int MT, int NT, bool UNDO>
+// UNDO: rows may have been scaled.  PAIRS: the outputs are in mx4_output's order.  y_at: elements from y's start to the rows.
+template <int MT, int NT, bool UNDO, bool PAIRS>
 __device__ inline void put_tile(const FusedArgs& a, const f32x4 (&acc)[MT][NT], f32x4* s_out, int tile0, int64_t b0, int64_t y_at)
 {
     const int lane = threadIdx.x % 64, g = lane / 16, c = lane % 16;
@@ -735,28 +748,142 @@ __device__ inline void put_tile(const FusedArgs& a, const f32x4 (&acc)[MT][NT], 
         for (int n = 0; n < NT; ++n)
             undo[n] = a.row_scale ? a.row_scale[min(b0 + n * 16 + c, (int64_t)a.B - 1)] : 1.0f;
     }
-    constexpr int kVecs = 2 * MT;  // of 8 outputs, in a row
+    constexpr int V = PAIRS && MT == 1 ? 4 : 8;  // neighbouring outputs
+    constexpr int kVecs = 16 * MT / V;           // in a row
     static_assert(64 % kVecs == 0, "a lane keeps its outputs");
-    const int q = lane % kVecs * 2;
-    OutputColumns<8> columns;
-    columns.load(a, tile0 * 16 + 4 * q);
+    const int q = lane % kVecs * (V / 4);
+    OutputColumns<V> columns;
+    columns.load(a, PAIRS && MT == 1 ? (int)mx4_output(tile0, 4 * q) : tile0 * 16 + 4 * q);  // (an even tile begins its 32 outputs)
 #pragma unroll
     for (int n0 = 0; n0 < NT; n0 += 2) {
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                s_out[(n * 16 + c) * 4 * MT + ((4 * t + g) ^ (c % (4 * MT)))] = UNDO ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
+                s_out[(n * 16 + c) * 4 * MT + ((PAIRS && MT > 1 ? t / 2 * 8 + 2 * g + t % 2 : 4 * t + g) ^ (c % (4 * MT)))] = UNDO ? acc[t][n0 + n] * undo[n0 + n] : acc[t][n0 + n];
         __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
         for (int r = lane / kVecs; r < 32; r += 64 / kVecs) {
-            const f32x4 lo = s_out[r * 4 * MT + (q ^ (r % 16 % (4 * MT)))];
-            const f32x4 hi = s_out[r * 4 * MT + ((q + 1) ^ (r % 16 % (4 * MT)))];
-            float z[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            float z[V];
+#pragma unroll
+            for (int e = 0; e < V; e += 4) {
+                const f32x4 v = s_out[r * 4 * MT + ((q + e / 4) ^ (r % 16 % (4 * MT)))];
+                z[e] = v[0], z[e + 1] = v[1], z[e + 2] = v[2], z[e + 3] = v[3];
+            }
             columns.template store<true>(a, b0 + n0 * 16 + r, z, y_at);
         }
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+// The same of tiles in mx4_output's order that lie within the outputs, where rows go in whole vectors: a lane
+// has 8 neighbouring outputs a row and stores them as they are, without LDS.  The sums turn into outputs in place.
+// (One pass over all of them at a time, with barriers for the scheduler: it would begin more at once than registers hold.)
+template <typename T, int MT, int NT, bool RESIDUAL>
+__device__ __forceinline__ void put_vectors(const f32x4 (&acc)[MT][NT], T* y, int64_t ld, const T* residual, int64_t ld_residual, int rows)
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t b = n * 16;
+        if (b < rows) {
+#pragma unroll
+            for (int t = 0; t < MT; t += 2) {
+                float z[8] = {acc[t][n][0],     acc[t][n][1],     acc[t][n][2],     acc[t][n][3],
+                              acc[t + 1][n][0], acc[t + 1][n][1], acc[t + 1][n][2], acc[t + 1][n][3]};
+                if (RESIDUAL) {
+                    float r[8];
+                    read_w<T, 8>(residual + b * ld_residual + t * 16, r, true, 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        z[e] += r[e];
+                }
+                write_w<T, 8, true>(y + b * ld + t * 16, z, true, 8);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// From row b0 (this lane's) and output m0 on, to y or pre.
+template <bool RESIDUAL, int MT, int NT>
+__device__ __forceinline__ void put_typed(const FusedArgs& a, const f32x4 (&acc)[MT][NT], void* y, int64_t at, int64_t ld, int64_t b0, int m0)
+{
+    const int rows = (int)min((int64_t)(16 * NT), a.B - b0);
+    auto put = [&](auto zero) __attribute__((always_inline)) {
+        typedef decltype(zero) T;
+        put_vectors<T, MT, NT, RESIDUAL>(acc, static_cast<T*>(y) + at + b0 * ld + m0, ld,
+                                         RESIDUAL ? static_cast<const T*>(a.residual) + b0 * a.ld_residual + m0 : nullptr, a.ld_residual, rows);
+    };
+    switch (a.y_type) {
+    case SPIKE_TYPE_F32: put(0.0f); break;
+    case SPIKE_TYPE_BF16: put(bf16{}); break;
+    default: put(f16{}); break;
+    }
+}
+
+template <int ACT, int MT, int NT>
+__device__ __forceinline__ void act_tile(f32x4 (&acc)[MT][NT])
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            float z[4] = {acc[t][n][0], acc[t][n][1], acc[t][n][2], acc[t][n][3]};
+            act_values<4>(z, ACT);
+            acc[t][n] = f32x4{z[0], z[1], z[2], z[3]};
+            __builtin_amdgcn_sched_barrier(0);
+        }
+}
+
+// Whether a wave's tiles go this way.
+template <int MT>
+__device__ inline bool straight_tile(const FusedArgs& a, int tile0) { return MT % 2 == 0 && a.vec_out && (tile0 + MT) * kFusedTile <= a.n_out; }
+
+template <int MT, int NT, bool UNDO>
+__device__ __forceinline__ void put_tile_straight(const FusedArgs& a, f32x4 (&acc)[MT][NT], int tile0, int64_t b0, int64_t y_at)
+{
+    static_assert(MT % 2 == 0, "pairs of tiles");
+    const int lane = threadIdx.x % 64, g = lane / 16;
+    b0 += lane % 16;
+    const int m0 = fused_output<kMx4>(tile0, g);
+    if (UNDO && a.row_scale) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float undo = a.row_scale[min(b0 + n * 16, (int64_t)a.B - 1)];
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                acc[t][n] *= undo;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int m = m0 + t / 2 * 32 + t % 2 * 4;
+        if (a.scale) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(a.scale + m);  // (the handle's: aligned)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                acc[t][n] *= v;
+        }
+        if (a.bias) {
+            const f32x4 v = {a.bias[m], a.bias[m + 1], a.bias[m + 2], a.bias[m + 3]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                acc[t][n] += v;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (a.pre)
+        put_typed<false>(a, acc, a.pre, 0, a.ld_pre, b0, m0);
+    switch (a.act) {
+    case 1: act_tile<1>(acc); break;
+    case 2: act_tile<2>(acc); break;
+    case 3: act_tile<3>(acc); break;
+    default: break;
+    }
+    if (a.residual)
+        put_typed<true>(a, acc, a.y, y_at, a.ld_y, b0, m0);
+    else
+        put_typed<false>(a, acc, a.y, y_at, a.ld_y, b0, m0);
 }
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves.  The
@@ -822,7 +949,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     const int first = min(split * a.split_steps + team * walk, a.steps - 1), steps = min(walk, mine - team * walk);
     const int g = lane / 16, c = lane % 16;
     const int wm = w % WM, wn = w / WM;
-    const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
+    const int tiles = fused_tiles<W>(a.n_out);
     const int tile0 = (out_tile * WM + wm) * MT;
     const int64_t b0 = (int64_t)row_tile * kRows;
 
@@ -1041,9 +1168,13 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
                 for (int n = 0; n < NT; ++n)
                     acc[t][n] += s_join[k * kTeam + (t * NT + n) * 64];
     }
+    if constexpr (W != kInt8 && MT % 2 == 0) {
+        if (straight_tile<MT>(a, tile0))
+            return put_tile_straight<MT, NT, __is_same(OT, f16)>(a, acc, tile0, b0 + wn * NT * 16, split * a.split_stride);
+    }
     // (behind the other teams' sums)
     f32x4* const s_out = reinterpret_cast<f32x4*>(s_fused) + (KS - 1) * WM * WN * MT * NT * 64 + w * 2 * 16 * 4 * MT;
-    put_tile<MT, NT, __is_same(OT, f16)>(a, acc, s_out, tile0, b0 + wn * NT * 16, split * a.split_stride);
+    put_tile<MT, NT, __is_same(OT, f16), W != kInt8>(a, acc, s_out, tile0, b0 + wn * NT * 16, split * a.split_stride);
 }
 
 // The join, and the copy below, walk rows of vectors of 8: a wave along a row, the four waves

@@ -57,16 +57,17 @@ __global__ __launch_bounds__(256) void k_mx4_top(const uint8_t* codes, int64_t l
 // A block's exponent relative to its output's largest; -1: it and its codes count as zero (smaller than the largest by 2^-140).
 __device__ inline int mx_relative(int byte, int top, bool any) { return byte == 255 ? 255 : any ? max(byte - top + kMxTop, -1) : -1; }
 
-// [tiles][blocks, rounded up to 4][16 outputs][16 B] and [tiles][blocks / 4][16 outputs][4 B]; a thread a block.
+// [tiles][blocks, rounded up to 4][16 outputs][16 B] and [tiles][blocks / 4][16 outputs][4 B]; and the exponents once more in
+// k_mx4_tile's order, [tiles][fours of 128 inputs][block of 128][16 outputs][4 B, one for each of the four].  A thread a block.
 __global__ __launch_bounds__(256) void k_mx4_pack(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales, int64_t ld_scales,
-                                                  int K, int M, const uint8_t* top, uint8_t* P, uint8_t* S, int64_t total)
+                                                  int K, int M, const uint8_t* top, uint8_t* P, uint8_t* S, uint8_t* E, int64_t total)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= total)
         return;
     const int64_t blocks = ((int64_t)K + 4 * kMxBlock - 1) / (4 * kMxBlock) * 4;
     const int c = i % 16;
-    const int64_t block = i / 16 % blocks, tile = i / 16 / blocks, m = tile * 16 + c;
+    const int64_t block = i / 16 % blocks, tile = i / 16 / blocks, m = mx4_output(tile, c);
     uint32_t w[4] = {};
     int byte = -1;
     if (m < M && block * kMxBlock < K) {
@@ -77,10 +78,12 @@ __global__ __launch_bounds__(256) void k_mx4_pack(const uint8_t* codes, int64_t 
         w[0] = w[1] = w[2] = w[3] = 0, byte = 127;
     *reinterpret_cast<u32x4*>(P + i * 16) = u32x4{w[0], w[1], w[2], w[3]};
     S[(tile * (blocks / 4) + block / 4) * 64 + c * 4 + block % 4] = (uint8_t)byte;
+    E[(tile * ((blocks + 15) / 16) + block / 16) * 256 + (block % 4 * 16 + c) * 4 + block / 4 % 4] = (uint8_t)byte;
 }
 
 // The gradient's: columns as outputs, a weight times its output's kMxTop-relative scale as one E5M2 byte (exact
-// where its block is within 2^-28 of the output's largest, else to 2^-29 of that), in k_fused_pack's order.
+// where its block is within 2^-28 of the output's largest, else to 2^-29 of that), in k_fused_pack's order but for
+// the outputs'.
 __global__ __launch_bounds__(256) void k_mx4_pack_columns(const uint8_t* codes, int64_t ld_codes, const uint8_t* scales,
                                                           int64_t ld_scales, int K, int M, const uint8_t* top, int8_t* P, int64_t chunks)
 {
@@ -90,7 +93,7 @@ __global__ __launch_bounds__(256) void k_mx4_pack_columns(const uint8_t* codes, 
     const int steps = (M + kFusedStep - 1) / kFusedStep;
     const int lane = i % 64;
     const int64_t piece = i / 64;
-    const int64_t k = piece / steps * kFusedTile + lane % 16, m0 = piece % steps * kFusedStep + lane / 16 * 8;
+    const int64_t k = mx4_output(piece / steps, lane % 16), m0 = piece % steps * kFusedStep + lane / 16 * 8;
     uint32_t w[4];
     for (int r = 0; r < 4; ++r) {
         float v[4];
@@ -115,6 +118,7 @@ struct Mx4Args {
     FusedArgs f;  // (steps: of 128 inputs; x: the rows' codes, ld_x: bytes)
     const uint8_t* scales;
     int64_t ld_scales;
+    const int8_t* E;  // the weights' exponents in k_mx4_tile's order
 };
 
 typedef int32_t i32x8 __attribute__((ext_vector_type(8)));
@@ -138,13 +142,13 @@ __global__ __launch_bounds__(64 * WK) void k_mx4_rows(Mx4Args m)
     const int g = lane / 16, c = lane % 16;
     const int tile0 = blockIdx.x * MT;
     const int64_t b0 = (int64_t)blockIdx.y * 16 * NB;
-    const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile, blocks = (a.n_in + kMxBlock - 1) / kMxBlock;
+    const int tiles = fused_tiles<kMx4>(a.n_out), blocks = (a.n_in + kMxBlock - 1) / kMxBlock;
     const uint8_t* const x0 = static_cast<const uint8_t*>(a.x);
     const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes), er = weight_resource(a.S, kBufMaxBytes);
     static_assert(MT * NB <= WK, "a wave joins one tile's sums");
     OutputColumns<4> columns;
     if (w < MT * NB)
-        columns.load(a, (tile0 + w / NB) * 16 + 4 * g);
+        columns.load(a, fused_output<kMx4>(tile0 + w / NB, g));
     f32x4 acc[MT][NB];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -228,20 +232,22 @@ __global__ __launch_bounds__(256) void k_mx4_align(const uint8_t* codes, int64_t
     }
 }
 
-template <int MT, int NT, int WM, int WN>
-constexpr int mx4_stage_bytes() { return 16 * NT * WN * 64 + WM * WN * (256 + MT * 1024 + 256); }
+template <int NT, int WM, int WN>
+constexpr int mx4_stage_bytes() { return 16 * NT * WN * 64 + WM * WN * 256; }
 
 template <int MT, int NT, int WM, int WN, int D>
 constexpr int mx4_tile_lds()
 {
-    constexpr int ring = D * mx4_stage_bytes<MT, NT, WM, WN>(), turning = WM * WN * 2 * 16 * 16 * MT * 4;
+    constexpr int ring = D * mx4_stage_bytes<NT, WM, WN>(), turning = WM * WN * 2 * 16 * 16 * MT * 4;
     return ring > turning ? ring : turning;
 }
 
-// 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves, 128 inputs a step, from a ring of D stages in
-// LDS that loads fill without registers.  A stage has the rows' codes (64 bytes a row; chunk q of row r at
-// q ^ (r / 4 % 4), so that 16 rows' chunks fall into different banks), their exponents, and for each wave its
-// weights and their exponents.  Rows: codes at 16-byte, exponents at 4-byte boundaries, K in whole steps.
+// 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves, 128 inputs a step.  The rows' codes (64 bytes a
+// row; chunk q of row r at q ^ (r / 4 % 4), so that 16 rows' chunks fall into different banks) and their exponents come
+// through a ring of D stages in LDS that loads fill without registers; a wave's weights are its own, so they go
+// straight to registers, two steps ahead, each register refilled as soon as its products are issued.
+// (Weights through LDS too: its bandwidth bounds, 107 us for 16,384 rows of 6144 -> 1536.)
+// Rows: codes at 16-byte, exponents at 4-byte boundaries, K in whole steps.
 template <int MT, int NT, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
 {
@@ -249,11 +255,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
     constexpr int kThreads = 64 * WM * WN, kRows = 16 * NT * WN, kWaves = WM * WN;
     constexpr int kChunks = kRows * 4 / kThreads;       // 16-byte chunks of rows that a thread fetches per step
     constexpr int kOwnRows = kRows / kWaves;            // rows whose exponents a wave fetches
-    constexpr int kStage = mx4_stage_bytes<MT, NT, WM, WN>();
-    constexpr int kExponents = kRows * 64, kWeights = kExponents + kWaves * 256, kWave = MT * 1024 + 256;  // places in a stage
-    constexpr int kLoads = kChunks + 1 + MT + 1;        // of a wave and step
+    constexpr int kStage = mx4_stage_bytes<NT, WM, WN>();
+    constexpr int kExponents = kRows * 64;              // where they begin in a stage
     static_assert(kChunks >= 1 && kRows * 4 % kThreads == 0, "every thread fetches whole chunks");
-    static_assert(kOwnRows >= 1 && kOwnRows <= 64 && MT <= 4 && NT % 2 == 0 && D >= 2 && (D - 2) * kLoads < 64, "what a load covers");
+    static_assert(kOwnRows >= 1 && kOwnRows <= 64 && MT <= 4 && NT % 2 == 0 && D >= 3, "what a load covers");
     extern __shared__ u32x4 s_fused[];
     const int plane_tiles = a.out_tiles * a.row_tiles, total = plane_tiles * a.splits, per_xcd = (total + 7) / 8;
     const int place = (int)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -266,18 +271,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int g = lane / 16, c = lane % 16, wm = w % WM, wn = w / WM;
     const int first = split * a.split_steps, steps = min(a.split_steps, a.steps - first);
-    const int tiles = (a.n_out + kFusedTile - 1) / kFusedTile;
+    const int tiles = fused_tiles<kMx4>(a.n_out);
     const int tile0 = (out_tile * WM + wm) * MT;
     const int64_t b0 = (int64_t)row_tile * kRows;
 
-    const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes), er = weight_resource(a.S, kBufMaxBytes);
+    const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes), er = weight_resource(m.E, kBufMaxBytes);
     const __amdgpu_buffer_rsrc_t xr = weight_resource(static_cast<const int8_t*>(a.x) + b0 * a.ld_x, kBufMaxBytes);
     const __amdgpu_buffer_rsrc_t sr = weight_resource(reinterpret_cast<const int8_t*>(m.scales) + b0 * m.ld_scales, kBufMaxBytes);
-    uint32_t w_at[MT], x_off[kChunks];
+    const uint32_t fours = (a.steps + 3) / 4;
+    uint32_t tile_at[MT], e_at[MT], x_off[kChunks];
 #pragma unroll
-    for (int t = 0; t < MT; ++t)  // tiles past the outputs repeat the last one; their results are not stored
-        w_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * a.steps * 1024u;
-    const uint32_t e_at = (uint32_t)min(tile0 + min(g, MT - 1), tiles - 1) * a.steps * 64u + c * 4u;
+    for (int t = 0; t < MT; ++t) {  // tiles past the outputs repeat the last one; their results are not stored
+        tile_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * a.steps + first;
+        e_at[t] = (uint32_t)min(tile0 + t, tiles - 1) * fours;
+    }
     const int last_row = (int)min((int64_t)kRows, a.B - b0) - 1;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
@@ -286,18 +293,28 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
     }
     const uint32_t s_off = (uint32_t)(min(w * kOwnRows + min(lane, kOwnRows - 1), last_row) * m.ld_scales);
     const uint32_t lds = lds_address(s_fused);
-    // Step s of this workgroup's to stage `buf`; past the last, zeros.
+    // Step s of this workgroup's to stage `buf`; past the last, the last again.
     auto fetch = [&](int buf, int s) __attribute__((always_inline)) {
-        const bool live = s < steps;
-        const uint32_t at = first + (live ? s : 0), to = lds + buf * kStage;
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-            load_to_lds(wr, live ? lane * 16u : kOutOfRange, w_at[t] + at * 1024u, to + kWeights + w * kWave + t * 1024);
-        load_words_to_lds(er, live ? e_at : kOutOfRange, at * 64u, to + kWeights + w * kWave + MT * 1024);
-        load_words_to_lds(sr, live ? s_off : kOutOfRange, at * 4u, to + kExponents + w * 256);
+        const uint32_t at = first + min(s, steps - 1), to = lds + buf * kStage;
+        load_words_to_lds(sr, s_off, at * 4u, to + kExponents + w * 256);
 #pragma unroll
         for (int i = 0; i < kChunks; ++i)
-            load_to_lds(xr, live ? x_off[i] : kOutOfRange, at * 64u, to + (i * (kThreads / 4) + w * 16) * 64);
+            load_to_lds(xr, x_off[i], at * 64u, to + (i * (kThreads / 4) + w * 16) * 64);
+    };
+    u32x4 wt[2][MT];
+    uint32_t we[2][MT];
+    constexpr int kWeightLoads = 2 * MT;
+    auto weights = [&](auto parity, int s) __attribute__((always_inline)) {
+        constexpr int q = decltype(parity)::value;
+        // (past the last step: zeros)
+        const bool live = s < steps;
+        const uint32_t at = live ? s : 0;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            wt[q][t] = __builtin_bit_cast(
+                u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, (tile_at[t] + at) * 1024u, 0));
+            we[q][t] = __builtin_amdgcn_raw_buffer_load_b32(er, live ? lane * 4u : kOutOfRange, (e_at[t] + (first + at) / 4) * 256u, 0);
+        }
     };
     f32x4 acc[MT][NT];
 #pragma unroll
@@ -305,42 +322,59 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
             acc[t][n] = f32x4{};
+    // (in the order in which a step asks: rows of D - 1 steps ahead, then weights of two ahead)
 #pragma unroll
-    for (int s = 0; s < D - 1; ++s)
+    for (int s = 0; s < D - 1; ++s) {
         fetch(s, s);
+        if (s == D - 3)
+            weights(std::integral_constant<int, 0>{}, 0);
+        if (s == D - 2)
+            weights(std::integral_constant<int, 1>{}, 1);
+    }
     int cur = 0;
     const char* const ring = reinterpret_cast<const char*>(s_fused);
-    for (int s = 0; s < steps; ++s) {
-        // this stage has landed for this wave, then for all; and all are done with the stage before it
-        wait_loads<(D - 2) * kLoads>();
+    auto step = [&](auto parity, int s) __attribute__((always_inline)) {
+        constexpr int p = decltype(parity)::value;
+        // all but the newest weights have landed for this wave, this stage's rows among it, then for all; and all are done with the stage before it
+        wait_loads<kWeightLoads>();
         __syncthreads();
         const char* const stage = ring + cur * kStage;
-        const char* const mine = stage + kWeights + w * kWave;
-        u32x4 wt[MT], x[NT];
-        uint32_t we[MT], xe[NT];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            wt[t] = *reinterpret_cast<const u32x4*>(mine + t * 1024 + lane * 16);
-            we[t] = *reinterpret_cast<const uint32_t*>(mine + MT * 1024 + t * 64 + c * 4) >> (8 * g);
-        }
+        u32x4 x[NT];
+        uint32_t xe[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = (wn * NT + n) * 16 + c;
             x[n] = *reinterpret_cast<const u32x4*>(stage + r * 64 + (g ^ c / 4) * 16);
-            xe[n] = *reinterpret_cast<const uint32_t*>(stage + kExponents + r / kOwnRows * 256 + r % kOwnRows * 4) >> (8 * g);
+            xe[n] = *reinterpret_cast<const uint32_t*>(stage + kExponents + r / kOwnRows * 256 + r % kOwnRows * 4);
         }
         fetch(cur == 0 ? D - 1 : cur - 1, s + D - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        uint32_t e[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            e[t] = we[p][t] >> ((first + s) % 4 * 8);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-                acc[t][n] = mfma_mx4(wt[t], we[t], x[n], xe[n], acc[t][n]);
+                acc[t][n] = mfma_mx4(wt[p][t], e[t], x[n], xe[n] >> (8 * g), acc[t][n]);
+        __builtin_amdgcn_sched_barrier(0);
+        weights(parity, s + 2);
         cur = cur + 1 == D ? 0 : cur + 1;
+    };
+    for (int s = 0; s < steps; s += 2) {  // (a step past the last multiplies zeros)
+        step(std::integral_constant<int, 0>{}, s);
+        step(std::integral_constant<int, 1>{}, s + 1);
     }
-    // the zeros fetched past the last step have landed everywhere before LDS is used anew
+    // what was fetched past the last step has landed everywhere before LDS is used anew
     wait_loads<0>();
     __syncthreads();
-    put_tile<MT, NT, false>(a, acc, reinterpret_cast<f32x4*>(s_fused) + w * 2 * 16 * 4 * MT, tile0, b0 + wn * NT * 16, split * a.split_stride);
+    const int64_t row0 = b0 + wn * NT * 16, y_at = split * a.split_stride;
+    if constexpr (MT % 2 == 0) {
+        if (straight_tile<MT>(a, tile0))
+            return put_tile_straight<MT, NT, false>(a, acc, tile0, row0, y_at);
+    }
+    put_tile<MT, NT, false, true>(a, acc, reinterpret_cast<f32x4*>(s_fused) + w * 2 * 16 * 4 * MT, tile0, row0, y_at);
 }
 
 }  // namespace spk
