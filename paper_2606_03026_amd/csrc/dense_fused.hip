@@ -330,18 +330,23 @@ int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 // and 334; 1536 -> 6144, 500 rows 46 and 31, 16,384 rows 549 and 560; 1280 -> 1536, 2500 rows 49
 // and 38.  Otherwise: 6000 -> 72, 500 rows 25 and 28; 6000 -> 520, 2500 rows 85 and 93; 72 -> 4104,
 // 500 rows 11 and 13; 456 -> 256, 8192 rows 26 and 31; but 1000 -> 1536, 2500 rows 40 and 32.
-enum GateForm { kGateRows, kGateApart, kGateBeside };
+//
+// kGateOne, where four-bit weights' dy and dx are BF16: the first plane alone, 11 bits of each g * scale, 8 times
+// finer than the dy it comes from and the dx it goes to are (8192 rows of 6144 outputs -> 1536: 312 us with both, 205).
+enum GateForm { kGateRows, kGateApart, kGateBeside, kGateOne };
 
-GateForm gate_form(const dense_fused* h, int y_type, int32_t B)
+GateForm gate_form(const dense_fused* h, int y_type, int x_type, int32_t B)
 {
     if (B <= kFewRows)
         return kGateRows;
+    if (h->kind == spk::kMx4 && y_type == SPIKE_TYPE_BF16 && x_type == SPIKE_TYPE_BF16)
+        return kGateOne;
     return y_type != SPIKE_TYPE_BF16 || (h->M >= 1280 && h->K >= 1024 && B >= 64) ? kGateApart : kGateBeside;
 }
 int gate_width(GateForm form, int32_t M) { return (int)spk::fused_pad(M, form == kGateBeside ? spk::kFusedStep : 8); }
 int64_t gate_plane_bytes(GateForm form, int32_t B, int32_t M)
 {
-    return spk::fused_pad((int64_t)gate_width(form, M) * B * 4, 16);  // FP32, or twice 16 bits
+    return spk::fused_pad((int64_t)gate_width(form, M) * B * (form == kGateOne ? 2 : 4), 16);  // FP32, or once or twice 16 bits
 }
 int64_t gate_bytes(GateForm form, int32_t B, int32_t M)
 {
@@ -407,7 +412,7 @@ void launch_gradient(const FusedArgs& a, GateForm form, float* part, hipStream_t
     switch (form) {
     case kGateRows: few_rows<W, float, 3>(a, true, st); break;
     case kGateApart: launch_planes<W, spk::f16, 2>(a, part, st); break;
-    case kGateBeside: launch_planes<W, spk::f16, 1>(a, part, st); break;
+    default: launch_planes<W, spk::f16, 1>(a, part, st); break;
     }
 }
 
@@ -488,6 +493,14 @@ void launch_mx4_many(spk::Mx4Args m, bool whole, void* workspace, hipStream_t st
     default: launch_mx4_tile<1, 4, 4, 1, 4>(m, st); break;
     }
     join_product(whole_args, p, part, st);
+}
+
+// What the gate leaves for the product, and the sums of a split one.
+int64_t gate_and_sums_bytes(const dense_fused* h, GateForm form, int32_t B)
+{
+    const int64_t gate = gate_bytes(form, B, h->M);
+    return form == kGateRows ? gate
+                             : gate + split_bytes(tile_plan(gate_planes(form), B, h->K, (h->M + spk::kFusedStep - 1) / spk::kFusedStep), B, h->K);
 }
 
 int check_rows(int32_t B, int32_t act, int x_type, int y_type)
@@ -700,12 +713,10 @@ int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
 {
     if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(y_type))
         return -1;
-    const GateForm form = gate_form(h, y_type, B);
-    const int64_t sums = form == kGateRows ? 0
-                                           : split_bytes(tile_plan(gate_planes(form), B, h->K,
-                                                                   (h->M + spk::kFusedStep - 1) / spk::kFusedStep),
-                                                         B, h->K);
-    return gate_bytes(form, B, h->M) + sums + spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
+    // (whatever type dx has)
+    const int64_t rest = spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
+    return rest + std::max(gate_and_sums_bytes(h, gate_form(h, y_type, SPIKE_TYPE_F32, B), B),
+                           gate_and_sums_bytes(h, gate_form(h, y_type, SPIKE_TYPE_BF16, B), B));
 }
 
 int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_t ld_dy, const void* pre, int64_t ld_pre,
@@ -740,7 +751,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return rc;
     if (act == DENSE_ACT_NONE)
         pre = nullptr;
-    const GateForm form = gate_form(h, y_type, B);
+    const GateForm form = gate_form(h, y_type, dx ? x_type : SPIKE_TYPE_F32, B);
     const int width = gate_width(form, h->M);
     int parts = 0;
     float* partial = nullptr;
@@ -752,7 +763,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         spk::GateArgs g{};
         g.dy = dy, g.ld_dy = ld_dy, g.pre = pre, g.ld_pre = ld_pre, g.act = act, g.B = B, g.M = h->M;
         g.scale = h->scale, g.gs = dx ? workspace : nullptr, g.width = width;
-        g.ld_gs = form == kGateBeside ? 2 * width : width, g.plane = form == kGateBeside ? width : (int64_t)width * B;
+        g.ld_gs = form == kGateBeside ? 2 * width : width, g.plane = form == kGateBeside ? width : form == kGateOne ? 0 : (int64_t)width * B;
         g.undo = undo, g.partial = partial;
         const bool vec = whole(dy, y_type, ld_dy) && whole(pre, y_type, ld_pre);
         const bool rows = form == kGateRows;

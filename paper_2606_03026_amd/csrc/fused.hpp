@@ -212,7 +212,7 @@ __device__ inline float largest_of_waves(float top, float (&s_top)[16], int firs
     return top;
 }
 
-// 8 values at p and p + plane.  Of an infinite one nothing is left for the second.
+// 8 values at p and p + plane (0: only at p).  Of an infinite one nothing is left for the second.
 __device__ inline void put_planes(uint16_t* p, int64_t plane, const float (&v)[8], float factor)
 {
     f16x8 hi, lo;
@@ -223,7 +223,8 @@ __device__ inline void put_planes(uint16_t* p, int64_t plane, const float (&v)[8
         lo[e] = (f16)(__builtin_isinf(x) ? 0.0f : x - (float)hi[e]);
     }
     *reinterpret_cast<f16x8*>(p) = hi;
-    *reinterpret_cast<f16x8*>(p + plane) = lo;
+    if (plane)
+        *reinterpret_cast<f16x8*>(p + plane) = lo;
 }
 
 // 8 activations as they were loaded.
@@ -1321,7 +1322,7 @@ struct GateArgs {
     const float* scale;   // [M rounded up to 16]
     void* gs;             // NULL: only the bias gradient
     int width;            // elements that a row of gs has in a plane: M and zeros
-    int64_t ld_gs, plane; // elements between rows and planes of gs
+    int64_t ld_gs, plane; // elements between rows and planes of gs; no second plane: 0
     float* undo;          // [B] inverses of the rows' scalings
     float* partial;       // [workgroups down][M] column sums of g, or NULL
 };
