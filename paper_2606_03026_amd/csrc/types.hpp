@@ -42,12 +42,17 @@ __device__ inline float in_fp32(float v)
     return v;
 }
 
-template <typename T>
+// (STREAM: past the caches)
+template <typename T, bool STREAM = false>
 __device__ inline void store8(T* p, f32x8 v)
 {
     for (int e = 0; e < 8; ++e)
         v[e] = in_fp32<T>(v[e]);
-    *reinterpret_cast<typename Vec8<T>::type*>(p) = __builtin_convertvector(v, typename Vec8<T>::type);
+    const typename Vec8<T>::type r = __builtin_convertvector(v, typename Vec8<T>::type);
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(r, reinterpret_cast<typename Vec8<T>::type*>(p));
+    else
+        *reinterpret_cast<typename Vec8<T>::type*>(p) = r;
 }
 
 inline int type_bytes(int type)
