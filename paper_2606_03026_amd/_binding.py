@@ -464,7 +464,7 @@ def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     [M, ceil(K / 32)], exponents of the blocks' powers of two; values: what they stand for, [M, K] of x's type, or None."""
     M, K = x.shape
     xp, ldx = _rows(x, "x", M, K)
-    cp, ldc, sp_, lds = _coded_rows(codes, scales, "", M, K)
+    cp, ldc, sp_, lds = _coded_rows(codes, scales, M, K)
     vp, ldv = None, 0
     if values is not None:
         vp, ldv = _rows(values, "values", M, K)
@@ -474,12 +474,11 @@ def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
            "spike_quantize_mx4")
 
 
-def _coded_rows(codes: torch.Tensor, scales: torch.Tensor, of: str, rows: int, K: int):
+def _coded_rows(codes: torch.Tensor, scales: torch.Tensor, rows: int, K: int):
     """(address, stride) of the codes and of the scales of `rows` rows of K four-bit elements."""
     if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
-        raise TypeError(f"{of}codes and {of}scales must be uint8")
-    return (*_rows(codes, f"{of}codes", rows, (K + 1) // 2),
-            *_rows(scales, f"{of}scales", rows, (K + SPIKE_MX4_BLOCK - 1) // SPIKE_MX4_BLOCK))
+        raise TypeError("codes and scales must be uint8")
+    return _rows(codes, "codes", rows, (K + 1) // 2) + _rows(scales, "scales", rows, (K + SPIKE_MX4_BLOCK - 1) // SPIKE_MX4_BLOCK)
 
 
 def spike_check_scale_shape(M: int, K: int, group: int, scale_rows: int, scale_cols: int) -> None:
@@ -561,7 +560,7 @@ def dense_fused_create_mx4(codes: torch.Tensor, scales: torch.Tensor, K: int, ba
     afterwards.  Every call that takes a handle takes it."""
     M, K = codes.shape[0], int(K)
     out = _p()
-    _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, "", M, K), K, M, DENSE_FUSED_BACKWARD if backward else 0,
+    _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, M, K), K, M, DENSE_FUSED_BACKWARD if backward else 0,
                                        ctypes.byref(out)), "dense_fused_create_mx4")
     return DenseFused(out.value, K, int(M))
 
@@ -610,7 +609,7 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
     """dense_fused_forward of four-bit rows (codes, scales as spike_quantize_mx4 gives them for [B, K]) with a handle of
     four-bit weights (dense_fused.h)."""
     B = codes.shape[0]
-    rows = _coded_rows(codes, scales, "", B, h.K)
+    rows = _coded_rows(codes, scales, B, h.K)
     yp, ldy = _rows(y, "y", B, h.M)
     rp = pp = None
     ldr = ldp = 0
@@ -633,7 +632,7 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
 def dense_fused_forward_mx4_workspace_bytes(h: DenseFused, codes: torch.Tensor, scales: torch.Tensor) -> int:
     """Workspace of dense_fused_forward_mx4 for these rows."""
     B = codes.shape[0]
-    return int(_lib.dense_fused_forward_mx4_workspace_bytes(h.ptr, *_coded_rows(codes, scales, "", B, h.K), B))
+    return int(_lib.dense_fused_forward_mx4_workspace_bytes(h.ptr, *_coded_rows(codes, scales, B, h.K), B))
 
 
 def dense_fused_workspace_bytes(h: DenseFused, B: int, dtype: torch.dtype) -> int:
@@ -804,6 +803,7 @@ class SpikeClip:
 
     def __init__(self, ptr: int, tensors, device):
         self.ptr, self.tensors, self.device = ptr, tensors, device
+        self.workspace_bytes = int(_lib.spike_clip_workspace_bytes(ptr))
 
     def close(self):
         if self.ptr:
@@ -826,7 +826,11 @@ def spike_clip_create(grads, outs=None) -> SpikeClip:
     if len(outs) != n:
         raise ValueError(f"{len(outs)} outputs for {n} gradients")
     in_ptrs, out_ptrs, types, sizes = (_p * n)(), (_p * n)(), (_i32 * n)(), (_i64 * n)()
+    device = torch.device("cuda", torch.cuda.current_device())
     for i, (g, o) in enumerate(zip(grads, outs)):
+        for t in (g, o):
+            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != device:
+                raise ValueError(f"tensor {i} is on {t.device}, the current device is {device}")
         in_ptrs[i] = _dev_ptr(g, f"gradient {i}")
         types[i], sizes[i] = _type_of(g, f"gradient {i}"), g.numel()
         if o is not None:
@@ -835,7 +839,7 @@ def spike_clip_create(grads, outs=None) -> SpikeClip:
             out_ptrs[i] = _dev_ptr(o, f"output {i}")
     out = _p()
     _check(_lib.spike_clip_create(in_ptrs, out_ptrs, types, sizes, n, ctypes.byref(out)), "spike_clip_create")
-    return SpikeClip(out.value, (grads, outs), grads[0].device if n else torch.device("cuda", torch.cuda.current_device()))
+    return SpikeClip(out.value, (grads, outs), device)
 
 
 def spike_clip_destroy(h: SpikeClip) -> None:
@@ -844,14 +848,14 @@ def spike_clip_destroy(h: SpikeClip) -> None:
 
 def spike_clip_workspace_bytes(h: SpikeClip) -> int:
     """Workspace of spike_clip_forward."""
-    return int(_lib.spike_clip_workspace_bytes(h.ptr))
+    return h.workspace_bytes
 
 
 def spike_clip_forward(h: SpikeClip, max_norm: float, result: torch.Tensor, workspace: torch.Tensor | None = None,
                        stream=None) -> None:
     """Scale the handle's gradients by min(1, max_norm / norm) into its outputs (spike_clip.h); result: float32 [2], the
     norm and the factor."""
-    ws = _workspace(workspace, max(16, int(_lib.spike_clip_workspace_bytes(h.ptr))), h.device, stream)
+    ws = _workspace(workspace, h.workspace_bytes, h.device, stream)
     _check(_lib.spike_clip_forward(h.ptr, max_norm, _vector(result, "result", 2), _dev_ptr(ws, "workspace"),
                                    ws.numel() * ws.element_size(), _stream(stream)), "spike_clip_forward")
 

@@ -277,9 +277,29 @@ bool in_chunks(const void* x, int type, int64_t ld, int32_t n)
     return whole(x, type, ld) && n % 8 == 0 && ld < spk::kBufMaxBytes / (256 * (int64_t)type_bytes(type));
 }
 
+// Four tiles of outputs a workgroup where there are many, in four waves, so that all workgroups of a head are resident at once
+// (57,344 outputs 12.5 us; eight waves 14.9).
+template <int W, int MT>
+void launch_spread(const FusedArgs& a, bool chunks, hipStream_t st)
+{
+    constexpr int WK = MT == 4 ? 4 : 8;
+    const dim3 grid((unsigned)((spk::fused_pad(a.n_out, 32) + 16 * MT - 1) / (16 * MT)));
+    const unsigned lds = (unsigned)spk::spread_lds<W>(a.B, a.n_in);
+    if (chunks)
+        hipLaunchKernelGGL((spk::k_fused_spread<MT, WK, true, W>), grid, dim3(64 * WK), lds, st, a);
+    else
+        hipLaunchKernelGGL((spk::k_fused_spread<MT, WK, false, W>), grid, dim3(64 * WK), lds, st, a);
+}
+
 template <int W, typename XT, int NS>
 void few_rows(const FusedArgs& a, bool chunks, hipStream_t st)
 {
+    if constexpr (W != spk::kInt8 && sizeof(XT) == 4) {
+        if (a.B <= spk::kSpreadRows && spk::spread_lds<W>(a.B, a.n_in) <= spk::kSpreadLds) {
+            const int tiles = (a.n_out + 15) / 16;
+            return tiles < kCUs ? launch_spread<W, 1>(a, chunks, st) : tiles < 4 * kCUs ? launch_spread<W, 2>(a, chunks, st) : launch_spread<W, 4>(a, chunks, st);
+        }
+    }
     chunks ? launch_few<W, XT, NS, true>(a, st) : launch_few<W, XT, NS, false>(a, st);
 }
 
@@ -453,7 +473,10 @@ void launch_mx4_tile(spk::Mx4Args m, hipStream_t st)
                        (spk::mx4_tile_lds<MT, NT, WM, WN, D>()), st, m);
 }
 
-constexpr TileShape kShapesMx4[] = {{256, 128, 1, 5.8f, 0.79f, 0.95f}, {128, 64, 1, 4.5f, 0.32f, 0.34f}, {64, 64, 1, 3.8f, 0.25f, 0.206f}};
+// Measured over 512 -> 512, 1536 -> 1536, 1536 -> 6144 and 6144 -> 1536 with 40 to 4096 rows (steps of 128 inputs).  What
+// that decides between, in us: 1536 -> 1536, 320 rows 15.4 in tiles of 256 x 128, 8.1 in 128 x 64, 7.8 in 64 x 64; 1536 -> 6144, 4096 rows
+// 41, 45 and 63; 6144 -> 1536, 40 rows 16.2 in one part, 12.6 in four.
+constexpr TileShape kShapesMx4[] = {{256, 128, 1, 5.9f, 0.70f, 0.88f}, {128, 64, 1, 3.9f, 0.36f, 0.29f}, {64, 64, 1, 4.0f, 0.29f, 0.21f}};
 
 int mx4_steps(int32_t K) { return (K + 127) / 128; }
 

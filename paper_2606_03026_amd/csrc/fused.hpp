@@ -658,6 +658,140 @@ __global__ __launch_bounds__(64 * WK) void k_fused_rows(FusedArgs a)
     columns.store(a, b, z);
 }
 
+// FP32 rows so few that their three BF16 parts fit the 16 columns of the matrix instruction (part p of row b is column 3 b +
+// p; the columns of a row are added up at the end): one product where k_fused_rows takes three, and the parts are
+// made once a workgroup, in LDS.  What three parts leave (values below 2^-110) is asked once a workgroup and
+// added by a loop of its own.  Four-bit weights, and the gradient's copy of them.  One row of FP32, four-bit weights, here and
+// in k_fused_rows: 1536 -> 1536 3.9 and 4.5 us, 6144 -> 1536 5.5 and 9.7, 1536 -> 57,344 12.5 (47 MB, 3.8 TB/s) and 15.3.
+constexpr int kSpreadRows = 5;
+constexpr int kSpreadLds = 49152;  // bytes of parts
+
+__host__ __device__ inline int spread_step(int W) { return W == kMx4 ? 128 : kFusedStep; }
+template <int W>
+__host__ __device__ inline int64_t spread_lds(int64_t B, int64_t n_in) { return (n_in + spread_step(W) - 1) / spread_step(W) * spread_step(W) * B * 6; }
+
+template <int MT, int WK, bool VECX, int W>
+__global__ __launch_bounds__(64 * WK) void k_fused_spread(FusedArgs a)
+{
+    constexpr bool kFour = W == kMx4;
+    constexpr int U = MT >= 4 ? 2 : 4;  // steps in flight
+    constexpr int kStep = kFour ? 128 : kFusedStep, kParts = kStep / 32;
+    const int n_steps = (a.n_in + kStep - 1) / kStep;
+    const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int g = lane / 16, c = lane % 16;
+    const int tile0 = blockIdx.x * MT, tiles = fused_tiles<W>(a.n_out), cols = 3 * a.B;
+    const __amdgpu_buffer_rsrc_t wr = weight_resource(a.P, kBufMaxBytes), er = weight_resource(kFour ? a.S : a.P, kBufMaxBytes);
+    extern __shared__ u32x4 s_fused[];
+    __shared__ f32x4 s_sum[WK][MT][64];
+    __shared__ uint32_t s_left;
+    static_assert(MT <= WK, "a wave joins one tile's sums");
+    u32x4 wt[U][MT];
+    uint32_t exponent[U][MT];
+    auto fetch = [&](int u, int s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const bool live = s < n_steps && tile0 + t < tiles;
+            const uint32_t at = live ? (uint32_t)(tile0 + t) * n_steps + s : 0u;
+            wt[u][t] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, at * 1024u, 0));
+            if constexpr (kFour)
+                exponent[u][t] = __builtin_amdgcn_raw_buffer_load_b8(er, live ? c * 4u + g : kOutOfRange, at * 64u, 0);
+        }
+    };
+    auto operand = [&](int u, int t, int h) __attribute__((always_inline)) {
+        if constexpr (kFour)
+            return mx_eight<bf16>(wt[u][t][h], mx_scale(exponent[u][t]));
+        else
+            return widen_half<bf16, W>(StepCodes<W>{wt[u][t]}, h, 0);
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        fetch(u, w + u * WK);
+    // the waves that join sums ask for their columns now: these are back when the sums are
+    OutputColumns<4> columns;
+    if (w < MT)
+        columns.load(a, fused_output<W>(tile0 + w, g));
+    if (threadIdx.x == 0)
+        s_left = 0;
+    __syncthreads();
+    const float* const x0 = static_cast<const float*>(a.x);
+    const __amdgpu_buffer_rsrc_t xr = rows_resource(x0);
+    const int groups = n_steps * kStep / 8;
+    for (int i = threadIdx.x; i < groups * a.B; i += 64 * WK) {
+        const int b = i / groups, k8 = i % groups;
+        u32x4 part[3];
+        if (split_raw<float, 3>(load_raw<float, VECX>(x0, xr, b * a.ld_x, k8 * 8, a.n_in), part))
+            s_left = 1;
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+            s_fused[k8 * cols + 3 * b + p] = part[p];
+    }
+    __syncthreads();
+    // a lane's column of slice h of step s (columns past the last repeat it)
+    const int col = min(c, cols - 1);
+    auto column = [&](int s, int h) __attribute__((always_inline)) {
+        return (s * (kStep / 8) + (kFour ? 4 * g + h : 4 * h + g)) * cols + col;
+    };
+    f32x4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        acc[t] = f32x4{};
+    for (int s0 = w; s0 < n_steps; s0 += WK * U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int s = s0 + u * WK;
+            if (s >= n_steps)
+                break;
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+                const u32x4 x = s_fused[column(s, h)];
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    acc[t] = mfma16<bf16>(operand(u, t, h), x, acc[t]);
+            }
+            fetch(u, s + WK * U);
+        }
+    }
+    if (__builtin_expect(s_left != 0, 0)) {
+        f32x4 rest_sum[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            rest_sum[t] = f32x4{};
+#pragma unroll 1
+        for (int s = w; s < n_steps; s += WK) {
+            fetch(0, s);
+#pragma unroll
+            for (int h = 0; h < kParts; ++h) {
+                u32x4 rest[2];
+                const int b = min(c / 3, a.B - 1), k = s * kStep + (kFour ? 32 * g + 8 * h : 32 * h + 8 * g);
+                split_rest(load_raw<float, VECX>(x0, xr, b * a.ld_x, k, a.n_in), rest);
+                if (c % 3 != 0)
+                    rest[0] = rest[1] = u32x4{};
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+                    rest_sum[t] = mfma16<bf16>(operand(0, t, h), rest[0], mfma16<bf16>(operand(0, t, h), rest[1], rest_sum[t]));
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+            acc[t] += rest_sum[t] * 0x1p-149f;
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        s_sum[w][t][lane] = acc[t];
+    __syncthreads();
+    if (w >= MT)
+        return;
+    f32x4 sum = s_sum[0][w][lane];
+#pragma unroll
+    for (int v = 1; v < WK; ++v)
+        sum += s_sum[v][w][lane];
+    float z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        z[e] = sum[e] + (__shfl_down(sum[e], 1) + __shfl_down(sum[e], 2));
+    columns.store(a, c % 3 == 0 ? c / 3 : a.B, z);  // (a row past the last is not stored)
+}
+
 // dbias from its parts (the first 256 threads of a workgroup: 64 outputs, a quarter of
 // the parts per wave; s_sum: 256 floats of LDS).  Beside a product it is hidden; alone
 // 16 parts of 6144 take 2.8 us, 157 of 12,000 (7.5 MB) 5.2.

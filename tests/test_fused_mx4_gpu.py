@@ -409,3 +409,93 @@ def test_forward_workspace_is_what_the_query_says(sp):
         torch.cuda.synchronize()
         assert (y == 0).all()
         h.close()
+
+
+# sizes that take each kernel form: few rows by 1, 2 and 4 tiles of outputs (and two of rows), FP32 rows as columns
+# and in parts, every tile shape of four-bit rows with the steps in one part and in several
+@pytest.mark.parametrize("xk,K,M,B,name", [("f32", 200, 100, 5, "k_fused_spread"), ("f32", 100, 4200, 1, "k_fused_spread"),
+                                           ("f32", 72, 17000, 4, "k_fused_spread"), ("f32", 72, 17000, 6, "k_fused_rows"),
+                                           ("f32", 9000, 40, 2, "k_fused_rows"), ("bf16", 72, 33000, 20, "k_fused_rows"),
+                                           ("mx4", 200, 100, 9, "k_mx4_rows"), ("mx4", 100, 4200, 9, "k_mx4_rows"),
+                                           ("mx4", 72, 33000, 16, "k_mx4_rows"), ("mx4", 72, 33000, 20, "k_mx4_rows"),
+                                           ("mx4", 1100, 4100, 3000, "k_mx4_tileILi4ELi8E"), ("mx4", 1100, 2100, 1500, "k_mx4_tileILi2ELi4E"),
+                                           ("mx4", 520, 200, 100, "k_mx4_tileILi1ELi4E"), ("mx4", 6200, 200, 100, "k_fused_join")])
+def test_every_form(sp, xk, K, M, B, name):
+    p = problem(K, M, B, integer=True)
+    h = handle(sp, p)
+    names = kernel_names(sp, h, p, xk, B, M)
+    assert any(name in n for n in names), names
+    for pad, offset in ((0, 0), (1, 1)):
+        (y, z), want, want_z, _ = forward(sp, h, p, xk, "f32", act="relu", pre=True, pad=pad, offset=offset)
+        assert torch.equal(y.cpu(), torch.from_numpy(want.astype(np.float32))) and torch.equal(z.cpu(), torch.from_numpy(want_z.astype(np.float32)))
+    h.close()
+
+
+@pytest.mark.parametrize("B", [1, 5])
+@pytest.mark.parametrize("K", [130, 1536])
+def test_columns_of_few_fp32_rows(sp, K, B):
+    """Rows as parts in columns: subnormals, values whose lowest bits lie below BF16's steps, infinities, beside ordinary rows."""
+    M = 70
+    p = problem(K, M, B)
+    r = np.random.default_rng([26, K, B])
+    p["scales"] = r.integers(125, 129, p["scales"].shape).astype(np.uint8)
+    p["W"] = so.mx4_values(p["codes"], p["scales"])
+    p["x"] = (r.normal(size=(B, K)) * 10.0 ** r.uniform(-44, -34, (B, K))).astype(np.float32)
+    h = handle(sp, p)
+    (y, _), want, _, x64 = forward(sp, h, p, "f32", "f32", bias=False, residual=False)
+    # a sum of multiples of 2^-150 (weights of 1/8 at least times steps of 2^-149), each addition off by u, stored to 2^-149
+    lim = 6 * U * np.sqrt(3 * K + 32) * (np.abs(x64) @ np.abs(p["W"]).T) + 2.0 ** -149
+    assert (np.abs(host(y) - want) <= lim).all(), np.max(np.abs(host(y) - want) / lim)
+    p["x"] = r.normal(size=(B, K)).astype(np.float32)
+    p["x"][0, 3] = np.inf
+    p["codes"][:, 3] = np.where(np.arange(M) % 2, 2, 10)
+    p["W"] = so.mx4_values(p["codes"], p["scales"])
+    h2 = handle(sp, p)
+    with np.errstate(invalid="ignore"):
+        (y, _), want, _, x64 = forward(sp, h2, p, "f32", "f32", bias=False, residual=False)
+    got = host(y)
+    assert (got[0] == np.where(np.arange(M) % 2, np.inf, -np.inf)).all()
+    lim = 6 * U * np.sqrt(3 * K + 32) * (np.abs(x64[1:]) @ np.abs(p["W"]).T)
+    assert (np.abs(got[1:] - want[1:]) <= lim).all()
+    h.close()
+    h2.close()
+
+
+@pytest.mark.parametrize("B", [3, 40, 600])
+def test_nothing_is_left_from_the_call_before(sp, B):
+    """A call whose rows are all NaN, then one of integers: nothing of the first is in the second."""
+    p = problem(136, 520, B, integer=True)
+    h = handle(sp, p)
+    nan = torch.full((B, 5), 255, dtype=torch.uint8, device="cuda")
+    y = torch.empty((B, 520), device="cuda")
+    sp.dense_fused_forward_mx4(h, torch.full((B, 68), 0x77, dtype=torch.uint8, device="cuda"), nan, y)
+    sp.dense_fused_forward_mx4(h, bytes_dev(packed(p["x_codes"])), bytes_dev(p["x_scales"]), y)
+    torch.cuda.synchronize()
+    assert torch.equal(y.cpu(), torch.from_numpy((rows_of(p) @ p["W"].T).astype(np.float32)))
+    h.close()
+
+
+def test_quantised_weights_give_the_product_of_their_values(sp):
+    """Export, product with rows in BF16 and in four bits, gradient: each as with the values that the export returns."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    W, x, dy = (torch.randn(s, device="cuda", generator=g) for s in ((300, 200), (90, 200), (90, 300)))
+    codes, scales = torch.empty((300, 100), dtype=torch.uint8, device="cuda"), torch.empty((300, 7), dtype=torch.uint8, device="cuda")
+    values = torch.empty_like(W)
+    sp.spike_quantize_mx4(W, codes, scales, values=values)
+    h = sp.dense_fused_create_mx4(codes, scales, 200, backward=True)
+    xb = x.bfloat16()
+    xc, xs = torch.empty((90, 100), dtype=torch.uint8, device="cuda"), torch.empty((90, 7), dtype=torch.uint8, device="cuda")
+    xv = torch.empty_like(xb)
+    sp.spike_quantize_mx4(xb, xc, xs, values=xv)
+    y, y4, dx = torch.empty((90, 300), device="cuda"), torch.empty((90, 300), device="cuda"), torch.empty((90, 200), device="cuda")
+    sp.dense_fused_forward(h, xb, y)
+    sp.dense_fused_forward_mx4(h, xc, xs, y4)
+    sp.dense_fused_backward(h, dy, dx=dx)
+    torch.cuda.synchronize()
+    v64 = host(values)
+    for got, rows, K in ((y, host(xb) @ v64.T, 200), (y4, host(xv) @ v64.T, 200), (dx, host(dy) @ v64, 300)):
+        mass = np.sqrt((host(dy if K == 300 else xb) ** 2).sum(axis=1, keepdims=True) * (v64 ** 2).sum(axis=0 if K == 300 else 1))
+        # (mass bounds the sum of the products' sizes by no less than its K-th root of K: Cauchy; four-bit rows may be a quarter larger)
+        assert (np.abs(host(got) - rows) <= 6 * U * np.sqrt(2 * K + 32) * 1.25 * np.sqrt(K) * mass + 2.0 ** -23 * mass).all()
+    h.close()
