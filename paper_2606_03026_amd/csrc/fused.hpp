@@ -11,7 +11,7 @@
 //
 // Four-bit weights (quantize.h) lie as [16 outputs][block of 32 inputs][output][16 B], blocks
 // filled up to fours and outputs to 32, so that lane 16 g + c finds a whole block of output c in one 16-byte load where a step
-// is 128 inputs, and half of one (inputs 16 g .. 16 g + 15 of 64) in 8 bytes; the blocks' exponents as
+// is 128 inputs, and two eights of one in 4 bytes each where it is 64; the blocks' exponents as
 // [16 outputs][four blocks][output][4 B].  The gradient's copy of them, whose sums run across the blocks, is
 // one E5M2 byte a weight (a level times a power of two is one) in the order of INT8 codes.  In both, two tiles
 // share 32 outputs so that a lane's results of them are eight neighbours (mx4_output), which it stores
@@ -1162,7 +1162,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
         const char* const p = s_w + stage * kStage;
         StepCodes<W> r;
         if constexpr (kFour) {
-            r.v = *reinterpret_cast<const u32x2*>(p + t * 512 + g / 2 * 256 + c * 16 + g % 2 * 8);
+            const uint32_t* const block = reinterpret_cast<const uint32_t*>(p + t * 512 + g / 2 * 256 + c * 16) + g % 2;
+            r.v = u32x2{block[0], block[2]};
             r.exponents = *reinterpret_cast<const uint32_t*>(p + (MT + 1) / 2 * 1024 + t * 64 + c * 4);
         } else {
             r.v = *reinterpret_cast<const u32x4*>(p + t * 1024 + lane * 16);
@@ -1189,7 +1190,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_t
     // (waves that multiply go before the waves of another workgroup that store)
     __builtin_amdgcn_s_setprio(1);
     int cur = 0;
-    const int c0 = (kFour ? 2 * g : g) ^ (c % 8), c1 = (kFour ? 2 * g + 1 : 4 + g) ^ (c % 8);
+    // (an odd and an even chunk are read together: their rows' places differ)
+    const int c0 = (kFour ? g / 2 * 4 + g % 2 : g) ^ (c % 8), c1 = (kFour ? g / 2 * 4 + g % 2 + 2 : 4 + g) ^ (c % 8);
     auto read = [&](int stage, int item) __attribute__((always_inline)) {
         const int h = item / kHalf, n = item % kHalf / NS, p = item % NS;
         return s_ring[stage * (kStage / 16) + ((p * kRows + (wn * NT + n) * 16 + c) * 8 + (h == 0 ? c0 : c1))];

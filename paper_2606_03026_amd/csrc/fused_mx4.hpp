@@ -232,6 +232,11 @@ __global__ __launch_bounds__(256) void k_mx4_align(const uint8_t* codes, int64_t
     }
 }
 
+// A read of 16 bytes a lane takes 16 lanes at a time: rows 0 to 3 and 12 to 15 of one group of lanes with rows 4 to 11 of the
+// next, and the others.  This order gives each of them a place of its own among the 256 bytes that lie in different banks
+// (r / 4 % 4 itself: 4.7 million cycles of conflicts in 16,384 rows of 1536 -> 6144; the time was the same).
+__device__ inline int mx4_turn(int r) { return -(r / 4) & 3; }
+
 template <int NT, int WM, int WN>
 constexpr int mx4_stage_bytes() { return 16 * NT * WN * 64 + WM * WN * 256; }
 
@@ -243,10 +248,12 @@ constexpr int mx4_tile_lds()
 }
 
 // 16 MT WM outputs x 16 NT WN rows per workgroup of WM x WN waves, 128 inputs a step.  The rows' codes (64 bytes a
-// row; chunk q of row r at q ^ (r / 4 % 4), so that 16 rows' chunks fall into different banks) and their exponents come
+// row; chunk q of row r at q ^ mx4_turn(r), so that what is read at a time falls into different banks) and their exponents come
 // through a ring of D stages in LDS that loads fill without registers; a wave's weights are its own, so they go
 // straight to registers, two steps ahead, each register refilled as soon as its products are issued.
-// (Weights through LDS too: its bandwidth bounds, 107 us for 16,384 rows of 6144 -> 1536.)
+// Bound by the latency of those loads, which one step in flight does not cover, and by the outputs: 16,384 rows 6144 -> 1536 100 us, 3.1
+// PFLOP/s (79 without any load, 44 at the rate that these instructions reach from registers), 1536 -> 6144 125, with GELU 152 to 165.
+// Slower or no faster: weights through LDS too (107), four and five stages, priorities by workgroup.
 // Rows: codes at 16-byte, exponents at 4-byte boundaries, K in whole steps.
 template <int MT, int NT, int WM, int WN, int D>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
@@ -288,7 +295,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
     const int last_row = (int)min((int64_t)kRows, a.B - b0) - 1;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
-        const int r = i * (kThreads / 4) + threadIdx.x / 4, q = threadIdx.x % 4 ^ r / 4 % 4;
+        const int r = i * (kThreads / 4) + threadIdx.x / 4, q = threadIdx.x % 4 ^ mx4_turn(r);
         x_off[i] = (uint32_t)(min(r, last_row) * a.ld_x) + q * 16u;
     }
     const uint32_t s_off = (uint32_t)(min(w * kOwnRows + min(lane, kOwnRows - 1), last_row) * m.ld_scales);
@@ -304,17 +311,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
     u32x4 wt[2][MT];
     uint32_t we[2][MT];
     constexpr int kWeightLoads = 2 * MT;
-    auto weights = [&](auto parity, int s) __attribute__((always_inline)) {
+    auto weights = [&](auto parity, int t, int s) __attribute__((always_inline)) {
         constexpr int q = decltype(parity)::value;
         // (past the last step: zeros)
         const bool live = s < steps;
         const uint32_t at = live ? s : 0;
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            wt[q][t] = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, (tile_at[t] + at) * 1024u, 0));
-            we[q][t] = __builtin_amdgcn_raw_buffer_load_b32(er, live ? lane * 4u : kOutOfRange, (e_at[t] + (first + at) / 4) * 256u, 0);
-        }
+        wt[q][t] = __builtin_bit_cast(
+            u32x4, __builtin_amdgcn_raw_buffer_load_b128(wr, live ? lane * 16u : kOutOfRange, (tile_at[t] + at) * 1024u, 0));
+        we[q][t] = __builtin_amdgcn_raw_buffer_load_b32(er, live ? lane * 4u : kOutOfRange, (e_at[t] + (first + at) / 4) * 256u, 0);
     };
     f32x4 acc[MT][NT];
 #pragma unroll
@@ -326,10 +330,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
 #pragma unroll
     for (int s = 0; s < D - 1; ++s) {
         fetch(s, s);
-        if (s == D - 3)
-            weights(std::integral_constant<int, 0>{}, 0);
-        if (s == D - 2)
-            weights(std::integral_constant<int, 1>{}, 1);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            if (s == D - 3)
+                weights(std::integral_constant<int, 0>{}, t, 0);
+            if (s == D - 2)
+                weights(std::integral_constant<int, 1>{}, t, 1);
+        }
     }
     int cur = 0;
     const char* const ring = reinterpret_cast<const char*>(s_fused);
@@ -344,7 +351,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int r = (wn * NT + n) * 16 + c;
-            x[n] = *reinterpret_cast<const u32x4*>(stage + r * 64 + (g ^ c / 4) * 16);
+            x[n] = *reinterpret_cast<const u32x4*>(stage + r * 64 + (g ^ mx4_turn(c)) * 16);
             xe[n] = *reinterpret_cast<const uint32_t*>(stage + kExponents + r / kOwnRows * 256 + r % kOwnRows * 4);
         }
         fetch(cur == 0 ? D - 1 : cur - 1, s + D - 1);
@@ -355,11 +362,17 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mx4_tile(Mx4Args m)
             e[t] = we[p][t] >> ((first + s) % 4 * 8);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
+            xe[n] >>= 8 * g;
+        // tile by tile, its weights of two steps ahead behind its products
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-                acc[t][n] = mfma_mx4(wt[p][t], e[t], x[n], xe[n] >> (8 * g), acc[t][n]);
-        __builtin_amdgcn_sched_barrier(0);
-        weights(parity, s + 2);
+        for (int t = 0; t < MT; ++t) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                acc[t][n] = mfma_mx4(wt[p][t], e[t], x[n], xe[n], acc[t][n]);
+            __builtin_amdgcn_sched_barrier(0);
+            weights(parity, t, s + 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
         cur = cur + 1 == D ? 0 : cur + 1;
     };
     for (int s = 0; s < steps; s += 2) {  // (a step past the last multiplies zeros)
