@@ -193,6 +193,12 @@ def _vector(t: torch.Tensor | None, name: str, n: int, dtype=torch.float32):
     return t.data_ptr() if t.is_cuda and t.is_contiguous() else _dev_ptr(t, name)
 
 
+def _on_current(t: torch.Tensor, name: str) -> None:
+    """A tensor of another device than the current one would be read through the wrong device's stream."""
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on {t.device}, the current device is {torch._C._cuda_getDevice()}")
+
+
 def _workspace(given: torch.Tensor | None, nbytes: int, device, stream) -> torch.Tensor:
     """`given`, or fresh memory that belongs to the stream of the call."""
     if given is not None:
@@ -463,6 +469,7 @@ def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     """Microscaled four-bit codes of x [M, K] (quantize.h): codes uint8 [M, ceil(K / 2)], two to a byte; scales uint8
     [M, ceil(K / 32)], exponents of the blocks' powers of two; values: what they stand for, [M, K] of x's type, or None."""
     M, K = x.shape
+    _on_current(x, "x")
     xp, ldx = _rows(x, "x", M, K)
     cp, ldc, sp_, lds = _coded_rows(codes, scales, M, K)
     vp, ldv = None, 0
@@ -559,6 +566,7 @@ def dense_fused_create_mx4(codes: torch.Tensor, scales: torch.Tensor, K: int, ba
     """A handle of four-bit weights [M, K], as spike_quantize_mx4 gives them (dense_fused.h); both tensors may be freed
     afterwards.  Every call that takes a handle takes it."""
     M, K = codes.shape[0], int(K)
+    _on_current(codes, "codes")
     out = _p()
     _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, M, K), K, M, DENSE_FUSED_BACKWARD if backward else 0,
                                        ctypes.byref(out)), "dense_fused_create_mx4")
@@ -609,6 +617,7 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
     """dense_fused_forward of four-bit rows (codes, scales as spike_quantize_mx4 gives them for [B, K]) with a handle of
     four-bit weights (dense_fused.h)."""
     B = codes.shape[0]
+    _on_current(codes, "codes")
     rows = _coded_rows(codes, scales, B, h.K)
     yp, ldy = _rows(y, "y", B, h.M)
     rp = pp = None
@@ -769,6 +778,7 @@ def head_logits_adjust(logits: torch.Tensor, out: torch.Tensor, ids: torch.Tenso
     ids: int32 [S, L]; n_ids, n_prompt: int32 [S]; drafts: int32 [S, n - 1]; repetition, presence, frequency: float32 [S];
     bias_ids int32, bias float32 [S, n_bias]; mask: int32 [S, n, ceil(V / 32)], a bit a token, set where it is allowed."""
     S, n, V = logits.shape
+    _on_current(logits, "logits")
     xp, ldx = _logit_rows(logits, "logits", S, n, V)
     op, ldo = _logit_rows(out, "out", S, n, V)
     if out.dtype != logits.dtype:
@@ -829,8 +839,8 @@ def spike_clip_create(grads, outs=None) -> SpikeClip:
     device = torch.device("cuda", torch.cuda.current_device())
     for i, (g, o) in enumerate(zip(grads, outs)):
         for t in (g, o):
-            if isinstance(t, torch.Tensor) and t.is_cuda and t.device != device:
-                raise ValueError(f"tensor {i} is on {t.device}, the current device is {device}")
+            if isinstance(t, torch.Tensor):
+                _on_current(t, f"tensor {i}")
         in_ptrs[i] = _dev_ptr(g, f"gradient {i}")
         types[i], sizes[i] = _type_of(g, f"gradient {i}"), g.numel()
         if o is not None:

@@ -295,6 +295,23 @@ def test_backward(sp, K, M, B, xk, yk, act):
     h.close()
 
 
+@pytest.mark.parametrize("K,M,B", [(70, 60, 40), (300, 700, 90), (520, 2100, 700)])
+@pytest.mark.parametrize("xk,entry", [("bf16", 2.0 ** -12), ("f32", 2.0 ** -23)])
+def test_gradient_of_bf16_outputs_keeps_its_digits(sp, K, M, B, xk, entry):
+    """A BF16 dy whose slopes give it more digits: to a BF16 dx they enter with 11 bits (2^-12 of an element), to an FP32 one
+    with 2^-23 of it; the slope is off by 1e-6, and dx is rounded to its type."""
+    p = problem(K, M, B)
+    z = np.random.default_rng([27, K, M, B]).normal(size=(B, M)).astype(np.float32)
+    h = handle(sp, p, backward=True)
+    dx, _, (want, _, g) = backward(sp, h, p, xk, "bf16", "silu", z=z, want_bias=False)
+    w = np.abs(p["W"])
+    g_err = np.abs(host(torch.from_numpy(p["dy"]).bfloat16())) * 1e-6
+    lim = (6 * U * np.sqrt(2 * M + 32) * (np.abs(g) @ w) + 6 * entry * np.sqrt((g * g) @ (w * w)) + g_err @ w
+           + HALF_UNIT[xk] * np.abs(want) * 1.01 + 2.0 ** -25)
+    assert (np.abs(host(dx) - want) <= lim).all(), np.max(np.abs(host(dx) - want) / lim)
+    h.close()
+
+
 @pytest.mark.parametrize("act", ["gelu", "silu"])
 def test_gradient_against_differences(sp, act):
     """dx and dbias along a direction against central differences of the definition in 64 bits."""
@@ -414,7 +431,8 @@ def test_forward_workspace_is_what_the_query_says(sp):
 # sizes that take each kernel form: few rows by 1, 2 and 4 tiles of outputs (and two of rows), FP32 rows as columns
 # and in parts, every tile shape of four-bit rows with the steps in one part and in several
 @pytest.mark.parametrize("xk,K,M,B,name", [("f32", 200, 100, 5, "k_fused_spread"), ("f32", 100, 4200, 1, "k_fused_spread"),
-                                           ("f32", 72, 17000, 4, "k_fused_spread"), ("f32", 72, 17000, 6, "k_fused_rows"),
+                                           ("f32", 72, 17000, 4, "k_fused_spread"), ("f32", 8192, 4200, 1, "k_fused_spread"),
+                                           ("f32", 4096, 17000, 2, "k_fused_spread"), ("f32", 72, 17000, 6, "k_fused_rows"),
                                            ("f32", 9000, 40, 2, "k_fused_rows"), ("bf16", 72, 33000, 20, "k_fused_rows"),
                                            ("mx4", 200, 100, 9, "k_mx4_rows"), ("mx4", 100, 4200, 9, "k_mx4_rows"),
                                            ("mx4", 72, 33000, 16, "k_mx4_rows"), ("mx4", 72, 33000, 20, "k_mx4_rows"),
