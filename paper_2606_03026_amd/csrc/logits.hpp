@@ -67,10 +67,13 @@ struct LogitsRaw {
 };
 
 // x / r where x > 0 (inverse: 1 / r, rounded), else x * r.  The quotient is the rounded one: a product with the inverse, off by
-// little more than a unit, and one step that adds what is left over times the inverse.  Where that is not a number (x or the
-// inverse infinite, r infinite) the product is what a division gives.
+// little more than a unit, and one step that adds what is left over times the inverse.  Where that is not a number (x infinite, or the
+// quotient) the product is what a division gives; an r so far from 1 that the inverse loses digits is divided by (r is the same
+// for all lanes).
 __device__ inline float penalized(float x, float r, float inverse)
 {
+    if (!(r > 0x1p-64f && r < 0x1p64f))
+        return x > 0.0f ? x / r : x * r;
     const float q = x * inverse, step = __builtin_fmaf(__builtin_fmaf(-q, r, x), inverse, q);
     return x > 0.0f ? (step == step ? step : q) : x * r;
 }

@@ -175,6 +175,26 @@ def test_streams_graphs_and_no_sequences(sp):
     sp.head_logits_adjust(x[:0], out[:0])
 
 
+def test_quotients_are_rounded_once(sp):
+    """Every token seen once in the prompt: x / r and x * r bit for bit as FP32 gives them, for penalties near 1 and far from it."""
+    r = torch.cat([torch.rand(60) * 1.5 + 0.5, torch.tensor([1.0, 0.0, 1e-40, 1e-20, 3.0, 1e20, 1e38, float("inf")])]).cuda()
+    S, V = r.numel(), 3000
+    x = (torch.randn((S, 1, V), device="cuda") * torch.exp(torch.randn((S, 1, V), device="cuda") * 8)).clamp(-1e30, 1e30)
+    x[:, 0, :4] = torch.tensor([float("inf"), -float("inf"), 3e38, 1e-30], device="cuda")
+    ids = torch.arange(V, dtype=torch.int32, device="cuda").repeat(S, 1)
+    out = torch.empty_like(x)
+    sp.head_logits_adjust(x, out, ids=ids, n_prompt=torch.full((S,), V, dtype=torch.int32, device="cuda"), repetition=r)
+    torch.cuda.synchronize()
+    rc, xc = r.cpu().numpy()[:, None, None], x.cpu().numpy()
+    with np.errstate(all="ignore"):
+        want = np.where(xc > 0, xc / rc, xc * rc)
+    got = out.cpu().numpy()
+    # (a quotient below 2^-126 may be a step of 2^-149 off)
+    small = np.abs(want) < 2.0 ** -120
+    assert ((got == want) | (np.isnan(got) & np.isnan(want)))[~small].all()
+    assert (np.abs(got.astype(np.float64) - want) <= 2.0 ** -149)[small].all()
+
+
 def test_refusals_of_the_binding(sp):
     x = torch.zeros((2, 3, 50), device="cuda")
     i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
