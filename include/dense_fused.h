@@ -28,8 +28,7 @@
  * on the sizes alone; equal calls give equal bits (a row's bits may depend on
  * B).  z stays FP32 up to y; outputs are rounded once.  In the backward pass
  * g * scale is FP32 and enters the product in two such F16 parts, or of up to
- * FUSED_FEW_ROWS rows in these BF16 parts; with four-bit weights and BF16 for both dy and dx, of more rows
- * in the first F16 part alone (2^-12 of an element, where dy and dx are held to 2^-9).  dbias is summed in FP32 from the
+ * FUSED_FEW_ROWS rows in these BF16 parts.  dbias is summed in FP32 from the
  * unrounded g.
  *
  * Four-bit weights (dense_fused_create_mx4; quantize.h states what codes and scales stand for) take the

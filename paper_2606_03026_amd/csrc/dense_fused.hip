@@ -351,15 +351,17 @@ int gate_parts(int32_t B) { return (B + gate_rows(B) - 1) / gate_rows(B); }
 // and 38.  Otherwise: 6000 -> 72, 500 rows 25 and 28; 6000 -> 520, 2500 rows 85 and 93; 72 -> 4104,
 // 500 rows 11 and 13; 456 -> 256, 8192 rows 26 and 31; but 1000 -> 1536, 2500 rows 40 and 32.
 //
-// kGateOne, where four-bit weights' dy and dx are BF16: the first plane alone, 11 bits of each g * scale, 8 times
-// finer than the dy it comes from and the dx it goes to are (8192 rows of 6144 outputs -> 1536: 312 us with both, 205).
+// kGateOne: the first plane alone, where the second would hold zeros.  Without a slope g is dy or 0, and four-bit weights' scales
+// are powers of two, so that g * scale of a BF16 dy has 8 bits: F16 holds them from 2^-32 of the row's largest on, and what it drops
+// below that is at most half of F16's smallest step, which the second plane rounds to 0 as well (8192 rows of 6144 outputs ->
+// 1536, no activation: 277 us with both, 168).
 enum GateForm { kGateRows, kGateApart, kGateBeside, kGateOne };
 
-GateForm gate_form(const dense_fused* h, int y_type, int x_type, int32_t B)
+GateForm gate_form(const dense_fused* h, int y_type, int act, int32_t B)
 {
     if (B <= kFewRows)
         return kGateRows;
-    if (h->kind == spk::kMx4 && y_type == SPIKE_TYPE_BF16 && x_type == SPIKE_TYPE_BF16)
+    if (h->kind == spk::kMx4 && y_type == SPIKE_TYPE_BF16 && (act == DENSE_ACT_NONE || act == DENSE_ACT_RELU))
         return kGateOne;
     return y_type != SPIKE_TYPE_BF16 || (h->M >= 1280 && h->K >= 1024 && B >= 64) ? kGateApart : kGateBeside;
 }
@@ -736,10 +738,10 @@ int64_t dense_fused_workspace_bytes(dense_fused_t h, int32_t B, int32_t y_type)
 {
     if (!h || B < 0 || B > FUSED_MAX_B || !is_float_type(y_type))
         return -1;
-    // (whatever type dx has)
+    // (whatever the activation is)
     const int64_t rest = spk::fused_pad((int64_t)gate_parts(B) * h->M * 4, 16);
-    return rest + std::max(gate_and_sums_bytes(h, gate_form(h, y_type, SPIKE_TYPE_F32, B), B),
-                           gate_and_sums_bytes(h, gate_form(h, y_type, SPIKE_TYPE_BF16, B), B));
+    return rest + std::max(gate_and_sums_bytes(h, gate_form(h, y_type, DENSE_ACT_NONE, B), B),
+                           gate_and_sums_bytes(h, gate_form(h, y_type, DENSE_ACT_GELU, B), B));
 }
 
 int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_t ld_dy, const void* pre, int64_t ld_pre,
@@ -774,7 +776,7 @@ int dense_fused_backward(dense_fused_t h, const void* dy, int32_t y_type, int64_
         return rc;
     if (act == DENSE_ACT_NONE)
         pre = nullptr;
-    const GateForm form = gate_form(h, y_type, dx ? x_type : SPIKE_TYPE_F32, B);
+    const GateForm form = gate_form(h, y_type, act, B);
     const int width = gate_width(form, h->M);
     int parts = 0;
     float* partial = nullptr;

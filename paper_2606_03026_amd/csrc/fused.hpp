@@ -1467,8 +1467,8 @@ struct GateArgs {
 
 // Rows of up to 8,192 outputs in whole vectors: a workgroup walks `rows` of them, `groups`
 // at a time, g * scale of a row staying in registers until the row's largest is known, and
-// goes to gs in two scaled F16 planes (PLANES; else as FP32 rows): g * scale is an FP32
-// value whatever the type of dy, and dx may be FP32 (one plane, 11 bits, left 2e-4 of its
+// goes to gs in two scaled F16 planes (PLANES; else as FP32 rows; one where the second would be zeros):
+// g * scale is an FP32 value whatever the type of dy, and dx may be FP32 (one plane, 11 bits, left 2e-4 of its
 // size there).  A thread has one vector of outputs and their sums over the rows, which the groups join in LDS and leave in
 // partial[workgroup]; the next row's loads are on their way while this one's largest is
 // found.  Bound by memory, and about as much by the slope's arithmetic (8192 rows of
