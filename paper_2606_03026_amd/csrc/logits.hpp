@@ -66,17 +66,9 @@ struct LogitsRaw {
     }
 };
 
-// x / r where x > 0 (inverse: 1 / r, rounded), else x * r.  The quotient is the rounded one: a product with the inverse, off by
-// little more than a unit, and one step that adds what is left over times the inverse.  Where that is not a number (x infinite, or the
-// quotient) the product is what a division gives; an r so far from 1 that the inverse loses digits is divided by (r is the same
-// for all lanes).
-__device__ inline float penalized(float x, float r, float inverse)
-{
-    if (!(r > 0x1p-64f && r < 0x1p64f))
-        return x > 0.0f ? x / r : x * r;
-    const float q = x * inverse, step = __builtin_fmaf(__builtin_fmaf(-q, r, x), inverse, q);
-    return x > 0.0f ? (step == step ? step : q) : x * r;
-}
+// (A quotient by the inverse and the remainder is as fast, 64 sequences of 5 rows 42.6 us either way, but off where the
+// remainder is subnormal or the product overflows.)
+__device__ inline float penalized(float x, float r) { return x > 0.0f ? x / r : x * r; }
 
 // A workgroup takes 2,048 tokens of the n rows of a sequence.  It counts in LDS which of them the
 // history names (whole numbers, so the order of the atomics does not matter) and where the list of biases names them last; then a
@@ -145,7 +137,6 @@ __global__ __launch_bounds__(256) void k_logits(LogitsArgs a)
             if (v < here && id >= 0)
                 atomicMax(&s_bias[v], i + 1);
         }
-        const float inverse = 1.0f / repetition;
         __syncthreads();
         auto at = [](int e) { return VEC ? (int)threadIdx.x * 8 + e : e * 256 + (int)threadIdx.x; };
         uint32_t count[8], any = 0, biased = 0;
@@ -178,7 +169,7 @@ __global__ __launch_bounds__(256) void k_logits(LogitsArgs a)
             if (any != 0) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float less = penalized(x[e], repetition, inverse);
+                    const float less = penalized(x[e], repetition);
                     x[e] = count[e] != 0 ? less : x[e];
                     const uint32_t said = count[e] & ~kLogitsPrompt;
                     const float told = (x[e] - frequency * (float)said) - presence;
