@@ -142,9 +142,19 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _dev_ptr(t: torch.Tensor, name: str, nbytes: int | None = None) -> int:
+def _placed(t, name: str, device: int | None) -> None:
+    """Refuses what is no device tensor, and one of another device than `device` (where that is given): the current device's
+    kernels would read it."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current device is {device}")
+
+
+def _dev_ptr(t: torch.Tensor, name: str, nbytes: int | None = None, device: int | None = None) -> int:
+    """Address of a contiguous device tensor."""
+    if not isinstance(t, torch.Tensor) or not (t.is_cuda if device is None else t.get_device() == device):
+        _placed(t, name, device)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     if nbytes is not None and t.numel() * t.element_size() < nbytes:
@@ -163,19 +173,18 @@ def _type_of(t: torch.Tensor, name: str) -> int:
     return code
 
 
-def _rows(t: torch.Tensor, name: str, rows: int, cols: int):
+def _rows(t: torch.Tensor, name: str, rows: int, cols: int, device: int | None = None):
     """(address, elements between rows) of a device tensor [rows, cols] whose rows are contiguous."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.shape == (rows, cols):
+    if isinstance(t, torch.Tensor) and (t.is_cuda if device is None else t.get_device() == device) and t.shape == (rows, cols):
         step, one = t.stride()
         if one == 1 and step >= cols:
             return t.data_ptr(), step
-    return _other_rows(t, name, rows, cols)
+    return _other_rows(t, name, rows, cols, device)
 
 
-def _other_rows(t, name: str, rows: int, cols: int):
+def _other_rows(t, name: str, rows: int, cols: int, device: int | None = None):
     """_rows of a tensor with one column or one row of any stride; what else there is, is refused."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
+    _placed(t, name, device)
     if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
         raise ValueError(f"{name} must be [{rows}, {cols}], is {list(t.shape)}")
     step, one = t.stride()
@@ -184,19 +193,14 @@ def _other_rows(t, name: str, rows: int, cols: int):
     return t.data_ptr(), max(step, cols)
 
 
-def _vector(t: torch.Tensor | None, name: str, n: int, dtype=torch.float32):
+def _vector(t: torch.Tensor | None, name: str, n: int, dtype=torch.float32, device: int | None = None):
     """Address of a contiguous device tensor of n elements; None stays None."""
     if t is None:
         return None
     if t.dtype is not dtype or t.numel() != n:
         raise TypeError(f"{name} must be {dtype} with {n} entries")
-    return t.data_ptr() if t.is_cuda and t.is_contiguous() else _dev_ptr(t, name)
-
-
-def _on_current(t: torch.Tensor, name: str) -> None:
-    """A tensor of another device than the current one would be read through the wrong device's stream."""
-    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"{name} is on {t.device}, the current device is {torch._C._cuda_getDevice()}")
+    here = t.is_cuda if device is None else t.get_device() == device
+    return t.data_ptr() if here and t.is_contiguous() else _dev_ptr(t, name, device=device)
 
 
 def _workspace(given: torch.Tensor | None, nbytes: int, device, stream) -> torch.Tensor:
@@ -469,23 +473,24 @@ def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
     """Microscaled four-bit codes of x [M, K] (quantize.h): codes uint8 [M, ceil(K / 2)], two to a byte; scales uint8
     [M, ceil(K / 32)], exponents of the blocks' powers of two; values: what they stand for, [M, K] of x's type, or None."""
     M, K = x.shape
-    _on_current(x, "x")
-    xp, ldx = _rows(x, "x", M, K)
-    cp, ldc, sp_, lds = _coded_rows(codes, scales, M, K)
+    dev = torch._C._cuda_getDevice()
+    xp, ldx = _rows(x, "x", M, K, dev)
+    cp, ldc, sp_, lds = _coded_rows(codes, scales, M, K, dev)
     vp, ldv = None, 0
     if values is not None:
-        vp, ldv = _rows(values, "values", M, K)
+        vp, ldv = _rows(values, "values", M, K, dev)
         if values.dtype != x.dtype:
             raise TypeError("values must have x's type")
     _check(_lib.spike_quantize_mx4(xp, _type_of(x, "x"), ldx, M, K, cp, ldc, sp_, lds, vp, ldv, _stream(stream)),
            "spike_quantize_mx4")
 
 
-def _coded_rows(codes: torch.Tensor, scales: torch.Tensor, rows: int, K: int):
+def _coded_rows(codes: torch.Tensor, scales: torch.Tensor, rows: int, K: int, device: int | None = None):
     """(address, stride) of the codes and of the scales of `rows` rows of K four-bit elements."""
     if codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8:
         raise TypeError("codes and scales must be uint8")
-    return _rows(codes, "codes", rows, (K + 1) // 2) + _rows(scales, "scales", rows, (K + SPIKE_MX4_BLOCK - 1) // SPIKE_MX4_BLOCK)
+    return (_rows(codes, "codes", rows, (K + 1) // 2, device) +
+            _rows(scales, "scales", rows, (K + SPIKE_MX4_BLOCK - 1) // SPIKE_MX4_BLOCK, device))
 
 
 def spike_check_scale_shape(M: int, K: int, group: int, scale_rows: int, scale_cols: int) -> None:
@@ -566,10 +571,9 @@ def dense_fused_create_mx4(codes: torch.Tensor, scales: torch.Tensor, K: int, ba
     """A handle of four-bit weights [M, K], as spike_quantize_mx4 gives them (dense_fused.h); both tensors may be freed
     afterwards.  Every call that takes a handle takes it."""
     M, K = codes.shape[0], int(K)
-    _on_current(codes, "codes")
     out = _p()
-    _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, M, K), K, M, DENSE_FUSED_BACKWARD if backward else 0,
-                                       ctypes.byref(out)), "dense_fused_create_mx4")
+    _check(_lib.dense_fused_create_mx4(*_coded_rows(codes, scales, M, K, torch._C._cuda_getDevice()), K, M,
+                                       DENSE_FUSED_BACKWARD if backward else 0, ctypes.byref(out)), "dense_fused_create_mx4")
     return DenseFused(out.value, K, int(M))
 
 
@@ -583,14 +587,15 @@ def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: t
     """y = act(z) + residual, z = scale * (x @ float(Q).T) + bias (dense_fused.h); z also to `pre`.
     x: [B, K]; y, residual, pre: [B, M] of one type; rows may be strided."""
     B = x.shape[0]
-    xp, ldx = _rows(x, "x", B, h.K)
-    yp, ldy = _rows(y, "y", B, h.M)
+    dev = torch._C._cuda_getDevice()
+    xp, ldx = _rows(x, "x", B, h.K, dev)
+    yp, ldy = _rows(y, "y", B, h.M, dev)
     rp = pp = None
     ldr = ldp = 0
     if residual is not None:
-        rp, ldr = _rows(residual, "residual", B, h.M)
+        rp, ldr = _rows(residual, "residual", B, h.M, dev)
     if pre is not None:
-        pp, ldp = _rows(pre, "pre", B, h.M)
+        pp, ldp = _rows(pre, "pre", B, h.M, dev)
     if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
         raise TypeError("residual and pre must have y's type")
     x_type = _type_of(x, "x")
@@ -599,8 +604,8 @@ def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: t
         n_ws = _lib.dense_fused_forward_workspace_bytes(h.ptr, xp, x_type, ldx, B)
     if n_ws > 0:
         workspace = _workspace(workspace, n_ws, x.device, stream)
-        wp, n_ws = _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
-    _check(_lib.dense_fused_forward(h.ptr, xp, x_type, ldx, B, _vector(bias, "bias", h.M), act, rp, ldr, yp,
+        wp, n_ws = _dev_ptr(workspace, "workspace", device=dev), workspace.numel() * workspace.element_size()
+    _check(_lib.dense_fused_forward(h.ptr, xp, x_type, ldx, B, _vector(bias, "bias", h.M, device=dev), act, rp, ldr, yp,
                                     _type_of(y, "y"), ldy, pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward")
 
 
@@ -617,15 +622,15 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
     """dense_fused_forward of four-bit rows (codes, scales as spike_quantize_mx4 gives them for [B, K]) with a handle of
     four-bit weights (dense_fused.h)."""
     B = codes.shape[0]
-    _on_current(codes, "codes")
-    rows = _coded_rows(codes, scales, B, h.K)
-    yp, ldy = _rows(y, "y", B, h.M)
+    dev = torch._C._cuda_getDevice()
+    rows = _coded_rows(codes, scales, B, h.K, dev)
+    yp, ldy = _rows(y, "y", B, h.M, dev)
     rp = pp = None
     ldr = ldp = 0
     if residual is not None:
-        rp, ldr = _rows(residual, "residual", B, h.M)
+        rp, ldr = _rows(residual, "residual", B, h.M, dev)
     if pre is not None:
-        pp, ldp = _rows(pre, "pre", B, h.M)
+        pp, ldp = _rows(pre, "pre", B, h.M, dev)
     if (residual is not None and residual.dtype != y.dtype) or (pre is not None and pre.dtype != y.dtype):
         raise TypeError("residual and pre must have y's type")
     wp, n_ws = None, 0
@@ -633,8 +638,8 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
         n_ws = _lib.dense_fused_forward_mx4_workspace_bytes(h.ptr, *rows, B)
     if n_ws > 0:
         workspace = _workspace(workspace, n_ws, codes.device, stream)
-        wp, n_ws = _dev_ptr(workspace, "workspace"), workspace.numel() * workspace.element_size()
-    _check(_lib.dense_fused_forward_mx4(h.ptr, *rows, B, _vector(bias, "bias", h.M), act, rp, ldr, yp, _type_of(y, "y"), ldy,
+        wp, n_ws = _dev_ptr(workspace, "workspace", device=dev), workspace.numel() * workspace.element_size()
+    _check(_lib.dense_fused_forward_mx4(h.ptr, *rows, B, _vector(bias, "bias", h.M, device=dev), act, rp, ldr, yp, _type_of(y, "y"), ldy,
                                         pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward_mx4")
 
 
@@ -658,21 +663,22 @@ def dense_fused_backward(h: DenseFused, dy: torch.Tensor, dx: torch.Tensor | Non
     """Gradients of dense_fused_forward with respect to x ([B, K]) and bias (float32 [M]); dy and pre
     are [B, M] of y's type."""
     B = dy.shape[0]
-    gp, ldg = _rows(dy, "dy", B, h.M)
+    dev = torch._C._cuda_getDevice()
+    gp, ldg = _rows(dy, "dy", B, h.M, dev)
     pp = xp = None
     ldp = ldx = 0
     y_type = x_type = _type_of(dy, "dy")
     if pre is not None:
-        pp, ldp = _rows(pre, "pre", B, h.M)
+        pp, ldp = _rows(pre, "pre", B, h.M, dev)
         if pre.dtype != dy.dtype:
             raise TypeError("pre must have dy's type")
     if dx is not None:
-        xp, ldx = _rows(dx, "dx", B, h.K)
+        xp, ldx = _rows(dx, "dx", B, h.K, dev)
         x_type = _type_of(dx, "dx")
     # (no size: the call refuses its arguments)
     ws = _workspace(workspace, max(0, int(_lib.dense_fused_workspace_bytes(h.ptr, B, y_type))), dy.device, stream)
     _check(_lib.dense_fused_backward(h.ptr, gp, y_type, ldg, pp, ldp, act, B, xp, x_type, ldx,
-                                     _vector(dbias, "dbias", h.M), _dev_ptr(ws, "workspace"),
+                                     _vector(dbias, "dbias", h.M, device=dev), _dev_ptr(ws, "workspace", device=dev),
                                      ws.numel() * ws.element_size(), _stream(stream)), "dense_fused_backward")
 
 
@@ -726,10 +732,10 @@ def head_draft_workspace_bytes(S: int, G: int, V: int) -> int:
     return n
 
 
-def _logit_rows(t: torch.Tensor, name: str, S: int, n: int, V: int):
+def _logit_rows(t: torch.Tensor, name: str, S: int, n: int, V: int, device: int | None = None):
     """(address, elements between rows) of logits [S, n, V] with evenly spaced rows."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
+    if not (t.is_cuda if device is None else t.get_device() == device):
+        _placed(t, name, device)
     if tuple(t.shape) != (S, n, V):
         raise ValueError(f"{name} must be [{S}, {n}, {V}], is {list(t.shape)}")
     seq, row, one = t.stride()
@@ -778,9 +784,9 @@ def head_logits_adjust(logits: torch.Tensor, out: torch.Tensor, ids: torch.Tenso
     ids: int32 [S, L]; n_ids, n_prompt: int32 [S]; drafts: int32 [S, n - 1]; repetition, presence, frequency: float32 [S];
     bias_ids int32, bias float32 [S, n_bias]; mask: int32 [S, n, ceil(V / 32)], a bit a token, set where it is allowed."""
     S, n, V = logits.shape
-    _on_current(logits, "logits")
-    xp, ldx = _logit_rows(logits, "logits", S, n, V)
-    op, ldo = _logit_rows(out, "out", S, n, V)
+    dev = torch._C._cuda_getDevice()
+    xp, ldx = _logit_rows(logits, "logits", S, n, V, dev)
+    op, ldo = _logit_rows(out, "out", S, n, V, dev)
     if out.dtype != logits.dtype:
         raise TypeError("out must have logits' type")
     i32 = torch.int32
@@ -789,22 +795,22 @@ def head_logits_adjust(logits: torch.Tensor, out: torch.Tensor, ids: torch.Tenso
         if ids.dtype != i32 or ids.dim() != 2:
             raise TypeError("ids must be int32 [S, L]")
         L = ids.shape[1]
-        ip, ldi = _rows(ids, "ids", S, L)
+        ip, ldi = _rows(ids, "ids", S, L, dev)
     bp, n_bias = None, 0
     if bias_ids is not None or bias is not None:
         if bias_ids is None or bias is None or bias_ids.dim() != 2:
             raise TypeError("bias_ids and bias must both be given, as [S, n_bias]")
         n_bias = bias_ids.shape[1]
-        bp = _vector(bias_ids, "bias_ids", S * n_bias, i32)
+        bp = _vector(bias_ids, "bias_ids", S * n_bias, i32, dev)
     mp, ldm = None, 0
     if mask is not None:
         if mask.dtype != i32:
             raise TypeError("mask must be int32 [S, n, ceil(V / 32)]")
-        mp, ldm = _logit_rows(mask, "mask", S, n, (V + 31) // 32)
-    _check(_lib.head_logits_adjust(xp, ldx, _type_of(logits, "logits"), S, n, V, ip, ldi, L, _vector(n_ids, "n_ids", S, i32),
-                                   _vector(n_prompt, "n_prompt", S, i32), _vector(drafts, "drafts", S * (n - 1), i32),
-                                   _vector(repetition, "repetition", S), _vector(presence, "presence", S),
-                                   _vector(frequency, "frequency", S), bp, _vector(bias, "bias", S * n_bias), n_bias, mp, ldm,
+        mp, ldm = _logit_rows(mask, "mask", S, n, (V + 31) // 32, dev)
+    _check(_lib.head_logits_adjust(xp, ldx, _type_of(logits, "logits"), S, n, V, ip, ldi, L, _vector(n_ids, "n_ids", S, i32, dev),
+                                   _vector(n_prompt, "n_prompt", S, i32, dev), _vector(drafts, "drafts", S * (n - 1), i32, dev),
+                                   _vector(repetition, "repetition", S, device=dev), _vector(presence, "presence", S, device=dev),
+                                   _vector(frequency, "frequency", S, device=dev), bp, _vector(bias, "bias", S * n_bias, device=dev), n_bias, mp, ldm,
                                    op, ldo, _stream(stream)), "head_logits_adjust")
 
 
@@ -838,15 +844,12 @@ def spike_clip_create(grads, outs=None) -> SpikeClip:
     in_ptrs, out_ptrs, types, sizes = (_p * n)(), (_p * n)(), (_i32 * n)(), (_i64 * n)()
     device = torch.device("cuda", torch.cuda.current_device())
     for i, (g, o) in enumerate(zip(grads, outs)):
-        for t in (g, o):
-            if isinstance(t, torch.Tensor):
-                _on_current(t, f"tensor {i}")
-        in_ptrs[i] = _dev_ptr(g, f"gradient {i}")
+        in_ptrs[i] = _dev_ptr(g, f"gradient {i}", device=device.index)
         types[i], sizes[i] = _type_of(g, f"gradient {i}"), g.numel()
         if o is not None:
             if o.dtype != g.dtype or o.numel() != g.numel():
                 raise TypeError(f"output {i} must have its gradient's type and size")
-            out_ptrs[i] = _dev_ptr(o, f"output {i}")
+            out_ptrs[i] = _dev_ptr(o, f"output {i}", device=device.index)
     out = _p()
     _check(_lib.spike_clip_create(in_ptrs, out_ptrs, types, sizes, n, ctypes.byref(out)), "spike_clip_create")
     return SpikeClip(out.value, (grads, outs), device)
@@ -865,8 +868,9 @@ def spike_clip_forward(h: SpikeClip, max_norm: float, result: torch.Tensor, work
                        stream=None) -> None:
     """Scale the handle's gradients by min(1, max_norm / norm) into its outputs (spike_clip.h); result: float32 [2], the
     norm and the factor."""
+    dev = torch._C._cuda_getDevice()
     ws = _workspace(workspace, h.workspace_bytes, h.device, stream)
-    _check(_lib.spike_clip_forward(h.ptr, max_norm, _vector(result, "result", 2), _dev_ptr(ws, "workspace"),
+    _check(_lib.spike_clip_forward(h.ptr, max_norm, _vector(result, "result", 2, device=dev), _dev_ptr(ws, "workspace", device=dev),
                                    ws.numel() * ws.element_size(), _stream(stream)), "spike_clip_forward")
 
 
