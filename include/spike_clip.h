@@ -14,7 +14,8 @@
  * in an order that depends on the sizes alone, so equal calls give equal bits;
  * the factor is rounded to FP32, products are FP32 and rounded once to the
  * tensor's type.  Where the norm is infinite or NaN, because a gradient is, out
- * is g unchanged, and the caller sees it in result.
+ * is g unchanged, and the caller sees it in result.  A norm of finite gradients is finite in
+ * 64 bits and clips by what it is there; beyond FP32's range result has infinity for it, beside its factor.
  *
  * spike_clip_create takes host arrays of n entries and keeps a table of them in
  * device memory; it reads no gradient, and the tensors stay the caller's and

@@ -83,3 +83,23 @@ def test_bf16_outputs_of_any_size_enter_exactly(sp, K, M, B, act, xk):
     want, _, _ = step.fused_backward(W, np.ones(M), host(dy), host(pre), act)
     assert torch.equal(dx.cpu(), torch.from_numpy(want.astype(np.float32)).to(TYPES[xk]))
     h.close()
+
+
+@pytest.mark.parametrize("K,M,B", SHAPES)
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+def test_rows_of_elements_of_unlike_sizes(sp, K, M, B, yk):
+    """Elements of a row from 2^-50 to 1 times its largest: each is held to 2^-23 of itself or 2^-39 of that, whichever is more."""
+    r = np.random.default_rng([43, K, M, B])
+    codes, scales = pairs(K, M)
+    W = so.mx4_values(codes, scales)
+    dy = dev(r.normal(size=(B, M)) * np.repeat(2.0 ** r.integers(-50, 1, (B, M // 2)), 2, axis=1), yk)
+    pre = dev(r.normal(size=(B, M)), yk)
+    h = handle(sp, codes, scales)
+    dx = torch.full((B, K), float("nan"), device="cuda")
+    sp.dense_fused_backward(h, dy, dx=dx, pre=pre, act=sp.DENSE_ACT_SILU)
+    torch.cuda.synchronize()
+    want, _, g = step.fused_backward(W, np.ones(M), host(dy), host(pre), "silu")
+    mass, slopes = np.abs(g) @ np.abs(W), 1e-6 * np.abs(host(dy)) @ np.abs(W)
+    lim = (2.0 ** -23 + 12 * U) * (mass + slopes) + slopes + 2 * 2.0 ** -39 * np.abs(g).max(axis=1, keepdims=True) + U * np.abs(want)
+    assert (np.abs(host(dx) - want) <= lim).all(), float(np.max(np.abs(host(dx) - want) / lim))
+    h.close()
