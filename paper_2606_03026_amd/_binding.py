@@ -136,9 +136,9 @@ def _check(rc: int, where: str) -> None:
         raise SpikeError(rc, where)
 
 
-def _stream(stream) -> int:
+def _stream(stream, device: int | None = None) -> int:
     if stream is None:  # the current stream, without building a Stream object (0.2 us against 2.9)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if device is None else device)
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -481,7 +481,7 @@ def spike_quantize_mx4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tenso
         vp, ldv = _rows(values, "values", M, K, dev)
         if values.dtype != x.dtype:
             raise TypeError("values must have x's type")
-    _check(_lib.spike_quantize_mx4(xp, _type_of(x, "x"), ldx, M, K, cp, ldc, sp_, lds, vp, ldv, _stream(stream)),
+    _check(_lib.spike_quantize_mx4(xp, _type_of(x, "x"), ldx, M, K, cp, ldc, sp_, lds, vp, ldv, _stream(stream, dev)),
            "spike_quantize_mx4")
 
 
@@ -606,7 +606,7 @@ def dense_fused_forward(h: DenseFused, x: torch.Tensor, y: torch.Tensor, bias: t
         workspace = _workspace(workspace, n_ws, x.device, stream)
         wp, n_ws = _dev_ptr(workspace, "workspace", device=dev), workspace.numel() * workspace.element_size()
     _check(_lib.dense_fused_forward(h.ptr, xp, x_type, ldx, B, _vector(bias, "bias", h.M, device=dev), act, rp, ldr, yp,
-                                    _type_of(y, "y"), ldy, pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward")
+                                    _type_of(y, "y"), ldy, pp, ldp, wp, n_ws, _stream(stream, dev)), "dense_fused_forward")
 
 
 def dense_fused_forward_workspace_bytes(h: DenseFused, x: torch.Tensor) -> int:
@@ -640,7 +640,7 @@ def dense_fused_forward_mx4(h: DenseFused, codes: torch.Tensor, scales: torch.Te
         workspace = _workspace(workspace, n_ws, codes.device, stream)
         wp, n_ws = _dev_ptr(workspace, "workspace", device=dev), workspace.numel() * workspace.element_size()
     _check(_lib.dense_fused_forward_mx4(h.ptr, *rows, B, _vector(bias, "bias", h.M, device=dev), act, rp, ldr, yp, _type_of(y, "y"), ldy,
-                                        pp, ldp, wp, n_ws, _stream(stream)), "dense_fused_forward_mx4")
+                                        pp, ldp, wp, n_ws, _stream(stream, dev)), "dense_fused_forward_mx4")
 
 
 def dense_fused_forward_mx4_workspace_bytes(h: DenseFused, codes: torch.Tensor, scales: torch.Tensor) -> int:
@@ -679,7 +679,7 @@ def dense_fused_backward(h: DenseFused, dy: torch.Tensor, dx: torch.Tensor | Non
     ws = _workspace(workspace, max(0, int(_lib.dense_fused_workspace_bytes(h.ptr, B, y_type))), dy.device, stream)
     _check(_lib.dense_fused_backward(h.ptr, gp, y_type, ldg, pp, ldp, act, B, xp, x_type, ldx,
                                      _vector(dbias, "dbias", h.M, device=dev), _dev_ptr(ws, "workspace", device=dev),
-                                     ws.numel() * ws.element_size(), _stream(stream)), "dense_fused_backward")
+                                     ws.numel() * ws.element_size(), _stream(stream, dev)), "dense_fused_backward")
 
 
 def spike_embed_forward(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
@@ -811,7 +811,7 @@ def head_logits_adjust(logits: torch.Tensor, out: torch.Tensor, ids: torch.Tenso
                                    _vector(n_prompt, "n_prompt", S, i32, dev), _vector(drafts, "drafts", S * (n - 1), i32, dev),
                                    _vector(repetition, "repetition", S, device=dev), _vector(presence, "presence", S, device=dev),
                                    _vector(frequency, "frequency", S, device=dev), bp, _vector(bias, "bias", S * n_bias, device=dev), n_bias, mp, ldm,
-                                   op, ldo, _stream(stream)), "head_logits_adjust")
+                                   op, ldo, _stream(stream, dev)), "head_logits_adjust")
 
 
 class SpikeClip:
@@ -871,7 +871,7 @@ def spike_clip_forward(h: SpikeClip, max_norm: float, result: torch.Tensor, work
     dev = torch._C._cuda_getDevice()
     ws = _workspace(workspace, h.workspace_bytes, h.device, stream)
     _check(_lib.spike_clip_forward(h.ptr, max_norm, _vector(result, "result", 2, device=dev), _dev_ptr(ws, "workspace", device=dev),
-                                   ws.numel() * ws.element_size(), _stream(stream)), "spike_clip_forward")
+                                   ws.numel() * ws.element_size(), _stream(stream, dev)), "spike_clip_forward")
 
 
 def spike_proj_abi_version() -> int:
