@@ -1044,7 +1044,8 @@ __device__ __forceinline__ void put_tile_straight(const FusedArgs& a, f32x4 (&ac
 // and 1272 TFLOP/s, 59%.
 // Codes widened by byte moves and packed F16 sums instead of conversions: no change.
 // Four-bit weights come two tiles a load, in half the bytes, and are widened by a third of the instructions: the same
-// 2500 FP32 rows 82 us and 1150 TFLOP/s; their gradient's copy, one plane, 8192 rows of 6144 -> 1536: 126 us, 1227 TFLOP/s.
+// 2500 FP32 rows 82 us and 1150 TFLOP/s; their gradient's copy, 8192 rows of 6144 -> 1536: one plane 126 us, 1227
+// TFLOP/s; two 236 to 263, 1180 to 1310, the matrix units busy 62%.
 template <typename OT, int NS, int MT, int NT, int WM, int WN, int D, int KS, int W>
 __global__ __launch_bounds__(64 * WM * WN * KS, KS == 1 ? 2 : KS) void k_fused_tile(FusedArgs a)
 {

@@ -74,7 +74,8 @@ __device__ inline float penalized(float x, float r) { return x > 0.0f ? x / r : 
 // history names (whole numbers, so the order of the atomics does not matter) and where the list of biases names them last; then a
 // thread holds what its 8 tokens have in registers and walks the rows, counting draft j - 1 before row j, with the next row's
 // loads on their way.  VEC: rows of logits and out start on 16-byte boundaries; a thread has 8 neighbouring
-// tokens, else every 256th.  Bound by memory where rows are many (64 sequences of 5 rows of 57,344 FP32: 42 us, 3.5 TB/s; 48 with the counts read and the drafts
+// tokens, else every 256th.  Bound by memory where rows are many (64 sequences of 5 rows of 57,344 FP32: 42 us, 3.5 TB/s; BF16 35; rows
+// off 16-byte boundaries 57 and 43; 48 with the counts read and the drafts
 // counted in LDS between the rows; fewer registers spill and take 53 to 69),
 // by the chain of reads where they are few.
 template <typename T, bool VEC>
